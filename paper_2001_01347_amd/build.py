@@ -3,14 +3,16 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", "zipline.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zipline.hip", "training.hip")]
 LIB = os.path.join(HERE, "libebsp_zipline.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
     "-I", os.path.join(ROOT, "include"),
@@ -18,9 +20,17 @@ HIPCC_FLAGS = [
 
 
 def build(verbose: bool = False) -> str:
-    """Compile csrc/*.hip into libebsp_zipline.so next to this file."""
+    """Compile csrc/*.hip, each source by itself, and link them into libebsp_zipline.so next to this file."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *SOURCES, "-o", LIB]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(lambda job: _run([hipcc, *HIPCC_FLAGS, "-c", job[0], "-o", job[1]], verbose), zip(SOURCES, objects)))
+        _run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB], verbose)
+    return LIB
+
+
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd))
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -30,7 +40,6 @@ def build(verbose: bool = False) -> str:
         raise RuntimeError("hipcc failed:\n" + err)
     if verbose and err.strip():
         print(err)
-    return LIB
 
 
 if __name__ == "__main__":

@@ -50,6 +50,7 @@
 
 #include "ebsp_zipline.h"
 #include "ebsp_zipline_bench.h"
+#include "zl_host.h"
 #include "zl_gridscan.h"    // pulls in the other device headers, in dependency order
 
 namespace {
@@ -57,32 +58,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // Host side.
 
-thread_local char g_err[256] = "";
-
-int fail(int code, const char* msg)
-{
-    snprintf(g_err, sizeof g_err, "%s", msg);
-    return code;
-}
-
-// The kernels are built for gfx950 only: refuse any other device by name instead of
-// letting a launch fail.  Asked once per device; the answer is kept.
-int check_device()
-{
-    constexpr int KNOWN = 64;
-    static std::atomic<signed char> seen[KNOWN];       // 0: not asked yet, 1: gfx950, -1: something else
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return fail(EBSP_ERR_DEVICE, "no current HIP device");
-    signed char state = dev >= 0 && dev < KNOWN ? seen[dev].load(std::memory_order_relaxed) : 0;
-    if (state == 0) {
-        hipDeviceProp_t prop;
-        if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return fail(EBSP_ERR_DEVICE, "hipGetDeviceProperties failed");
-        state = strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : -1;
-        if (dev >= 0 && dev < KNOWN) seen[dev].store(state, std::memory_order_relaxed);
-    }
-    if (state < 0) return fail(EBSP_ERR_DEVICE, "the current device is not a gfx950 (MI355X): this library has code for nothing else");
-    return EBSP_OK;
-}
+using namespace ebsp_host;
 
 enum KernelId { K_INSTANCE = 0, K_INSTANCE_GENERAL, K_BOUNDS, K_PARTITION, K_BINCOUNT, K_PLAN, K_WINDOW,
                 K_WINDOW_GENERAL, K_FINISH, K_COPY, K_RANGE_INSTANCE, K_RANGE_FAST, K_PARTITION_PRED, K_RANGE_WINDOW, K_ADVANCE, K_SWEEP, K_SWEEP_FINISH, K_GRIDSCAN, K_GRIDSCAN_FINISH, K_READ, K_INSTANCE_REG, K_RUN, K_DIRECT, K_DIRECT_FINISH, K_CELLS, K_COUNT };
