@@ -84,6 +84,88 @@ int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t 
                            void* dx, int64_t lddx, void* dwg, void* dwu, int64_t lddw,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* Status bit of a row of the distillation loss (status[n], beside EBSP_STATUS_OK). */
+#define EBSP_STATUS_RANGE      4   /* an index or a label is V or more: that entry or term is left out */
+
+#define EBSP_DISTILL_TOP_MAX 1024  /* most entries of a row */
+
+/*
+ * Distillation from a teacher's top logits.  A row holds the student's logits s
+ * over a vocabulary of V and the teacher's largest logits t_k with their places
+ * i_k, k < top.  With a temperature T, q = softmax(t / T) over the row's
+ * entries, p = softmax(s / T) and p1 = softmax(s):
+ *
+ *     loss = kl_weight * T^2 * sum_k q_k (log q_k - log p[i_k])
+ *            - ce_weight * log p1[label]
+ *     dloss/ds[j] = kl_weight * T * (p[j] - sum_{k: i_k = j} q_k)
+ *            + ce_weight * (p1[j] - [j = label])
+ *
+ *   logits    in  [N][V] of type dtype, rows ld apart
+ *   top_index in  [N][top], rows ldt apart; index_bytes says which: 4 or 8 (signed).
+ *                 Negative: padding, no entry.  Entries of one place add up.
+ *   top_logit in  [N][top] of type top_dtype, rows ldt apart; -inf weighs nothing
+ *   labels    in  [N] int64, or NULL: no second term; negative: none in this row
+ *   loss      out [N] float
+ *   stats     out [N][3] float: what ebsp_distill_backward needs of the
+ *                 forward pass; or NULL
+ *   dloss     in  [N] float: dL/dloss of every row
+ *   dlogits   out [N][V] of type dtype, rows ldd apart: dL/ds.  May be the
+ *                 logits themselves (same rows): they are overwritten then
+ *   status    out [N] int32, or NULL
+ *   workspace     at least ebsp_distill_workspace_bytes(N, V, dtype) bytes,
+ *                 256-byte aligned (may be NULL when that is 0)
+ * A row without entries has no first term and its gradient no p.  Logits of -inf
+ * (masked places) have p = 0, and where the teacher gives such a place weight the
+ * loss is +inf.  ebsp_distill_forward gives the loss, ebsp_distill_backward the
+ * gradient from its stats, ebsp_distill_loss_grad both in one pass where a step's
+ * dloss is known beforehand (1 / N for a mean).  top_index and top_logit may be
+ * NULL when top is 0.  N == 0 is a valid no-op; V is at least 1; more than some
+ * four million rows are refused (EBSP_ERR_SHAPE): split them.
+ */
+size_t ebsp_distill_workspace_bytes(int64_t N, int64_t V, int32_t dtype);
+int ebsp_distill_forward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                         const void* top_index, int32_t index_bytes, const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top,
+                         const int64_t* labels, float temperature, float kl_weight, float ce_weight,
+                         float* loss, float* stats, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+int ebsp_distill_backward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                          const void* top_index, int32_t index_bytes, const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top,
+                          const int64_t* labels, float temperature, float kl_weight, float ce_weight,
+                          const float* stats, const float* dloss, void* dlogits, int64_t ldd, void* stream);
+int ebsp_distill_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                           const void* top_index, int32_t index_bytes, const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top,
+                           const int64_t* labels, float temperature, float kl_weight, float ce_weight,
+                           const float* dloss, float* loss, void* dlogits, int64_t ldd, int32_t* status,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+#define EBSP_MERGE_WORKERS_MAX 4096   /* most workers of a merge */
+
+/*
+ * What the server does at a barrier (Section III): the workers' pushes, each the
+ * change of its weights since the last barrier, merged by the iterations that the
+ * search gave the workers (iters[b] of ebsp_zipline_batch and the others, still on
+ * the device), and applied to the server's weights:
+ *
+ *     c_p = iters[p] / sum iters     avg = sum_p c_p * push_p
+ *     v'  = momentum * v + avg       w'  = w + lr * (nesterov ? avg + momentum * v' : v')
+ *
+ * and without a velocity w' = w + lr * avg.  (The paper leaves the server's
+ * update open; weights by iterations are this library's reading, momentum the
+ * usual choice for merged local steps.)
+ *
+ *   pushes       in  [P][n] of type dtype, a worker's row `stride` after the one before
+ *   iters        in  [P] int32.  A worker with 0 or less has no part in the merge
+ *                    and its row is not read; with no worker left nothing changes
+ *   weights      in  [n] float;   weights_out  out [n] float, may be weights itself
+ *   velocity     in  [n] float;   velocity_out out [n] float, may be velocity
+ *                    itself; both NULL: no momentum
+ *   pull         out [n] of type pull_dtype: w' rounded, what the workers fetch; or NULL
+ * Sums run in the order of the workers in 32 bits: results do not vary.  P is 1 to
+ * EBSP_MERGE_WORKERS_MAX, n below 2^34.  n == 0 is a valid no-op.
+ */
+int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, int32_t dtype, const int32_t* iters,
+                      const float* weights, const float* velocity, float lr, float momentum, int32_t nesterov,
+                      float* weights_out, float* velocity_out, void* pull, int32_t pull_dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,8 @@
 //   tr_common.h    element types, loads and stores at any alignment
 //   tr_product.h   tiles of matrix products on the matrix cores
 //   tr_gated_ff.h  the gated feed-forward block and its backward pass
+//   tr_distill.h   the distillation loss and its gradient
+//   tr_merge.h     the merge of the workers' pushes
 // This file: the host side (checks, launches, the C entry points).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -12,14 +14,17 @@
 #include "ebsp_training.h"
 #include "zl_host.h"
 #include "tr_gated_ff.h"
+#include "tr_distill.h"
+#include "tr_merge.h"
 
 namespace {
 
 using namespace ebsp_host;
 
-#define LAUNCH(kernel, grid, block, ...)                                                   \
+#define LAUNCH(kernel, grid, block, ...) LAUNCH_LDS(kernel, grid, block, 0, __VA_ARGS__)
+#define LAUNCH_LDS(kernel, grid, block, lds, ...)                                          \
     do {                                                                                   \
-        hipLaunchKernelGGL(kernel, grid, block, 0, st, __VA_ARGS__);                       \
+        hipLaunchKernelGGL(kernel, grid, block, lds, st, __VA_ARGS__);                       \
         hipError_t e_ = hipGetLastError();                                                 \
         if (e_ != hipSuccess) {                                                            \
             snprintf(g_err, sizeof g_err, "%s: %s", #kernel, hipGetErrorString(e_));       \
@@ -54,11 +59,14 @@ int check_sizes(i64 M, i64 K, i64 F, int dtype, int act)
 
 bool stride_ok(i64 ld, i64 length) { return ld >= length && ld < (1ll << 40); }
 
+// A launch of so many workgroups: the runtime counts a grid's threads in 32 bits.
+bool launchable(i64 blocks, int threads) { return blocks * threads <= 0xffffffffll; }
+
 template <class TL, int PER_N>
 int tile_grid(i64 m, i64 n, dim3& grid, int z = 1)
 {
     const i64 tiles = ((m + TL::BM - 1) / TL::BM) * ((n + PER_N - 1) / PER_N);
-    if (tiles > 0x7fffffffll) return fail(EBSP_ERR_SHAPE, "the result is too large for one call");
+    if (!launchable(tiles, TL::NT)) return fail(EBSP_ERR_SHAPE, "the result is too large for one call");
     grid = dim3((unsigned)tiles, (unsigned)z);
     return EBSP_OK;
 }
@@ -74,12 +82,12 @@ int ff_forward(const FfForward& f, hipStream_t st)
 }
 
 template <class T, Layout LA>
-int ff_gradient(const FfGradient& f, int z, hipStream_t st)
+int ff_gradient(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
     using TL = Tile<T, 2, 2, 4, 4>;
     dim3 grid;
     if (int rc = tile_grid<TL, TL::BN>(f.a.index, f.b.index, grid, z)) return rc;
-    LAUNCH((tr_ff_gradient_kernel<T, TL, LA>), grid, dim3(TL::NT), f);
+    if (launch) LAUNCH((tr_ff_gradient_kernel<T, TL, LA>), grid, dim3(TL::NT), f);
     return EBSP_OK;
 }
 
@@ -91,21 +99,112 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
     const i64 ldd = padded_units(F, sizeof(T));
     T* dg = (T*)workspace;
     T* du = dg + M * ldd;
-    const i64 chunks = M * (ldd / PER_WORD4<T>);
-    if (chunks > 0) {
-        const i64 blocks = (chunks + 255) / 256;
-        LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, (const T*)g, (const T*)u,
-               ldg, dg, du, ldd, M, F, act);
+    const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0},
+                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2};
+    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, F, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
+                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1};
+    for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
+        const i64 chunks = M * (ldd / PER_WORD4<T>);
+        if (launch && chunks > 0) {
+            const i64 blocks = (chunks + 255) / 256;
+            LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, (const T*)g,
+                   (const T*)u, ldg, dg, du, ldd, M, F, act);
+        }
+        if (dx && M > 0)
+            if (int rc = ff_gradient<T, ROWS>(to_x, 1, launch, st)) return rc;
+        if (dwg && F > 0)
+            if (int rc = ff_gradient<T, COLS>(to_w, 2, launch, st)) return rc;
     }
-    if (dx && M > 0 && K > 0) {
-        FfGradient f = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0}, {wide_rows(dx, lddx, sizeof(T)), 0}, 2};
-        if (int rc = ff_gradient<T, ROWS>(f, 1, st)) return rc;
+    return EBSP_OK;
+}
+
+// Parts that a row is cut into: one where there are rows enough for every CU, else so many that there are two workgroups for each,
+// of no less than 512 words of 16 bytes.
+int distill_splits(i64 N, i64 V, int size)
+{
+    const i64 words = (V * size + 15) / 16;
+    i64 s = N >= 256 ? 1 : (512 + N - 1) / (N > 0 ? N : 1);
+    if (s > words / 512) s = words / 512;
+    return (int)(s < 1 ? 1 : s);
+}
+
+size_t distill_partial_bytes(i64 N, int splits) { return splits > 1 ? ((size_t)N * splits * 3 * sizeof(float) + 255) / 256 * 256 : 0; }
+
+template <class T>
+int distill_loss(Distill d, bool grad, hipStream_t st)
+{
+    const dim3 rows((unsigned)d.N);
+    const dim3 parts((unsigned)(d.N * d.splits));
+    if (d.splits == 1) {
+        const bool large = d.V / PER_WORD4<T> > 2048;
+        if (grad) {
+            if (large) LAUNCH((tr_distill_row_kernel<1024, T, true>), rows, dim3(1024), d);
+            else LAUNCH((tr_distill_row_kernel<256, T, true>), rows, dim3(256), d);
+        } else {
+            if (large) LAUNCH((tr_distill_row_kernel<1024, T, false>), rows, dim3(1024), d);
+            else LAUNCH((tr_distill_row_kernel<256, T, false>), rows, dim3(256), d);
+        }
+        return EBSP_OK;
     }
-    if (dwg && F > 0 && K > 0) {
-        FfGradient f = {{{dg, du}, {ldd, ldd}, F, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
-                        {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1};
-        if (int rc = ff_gradient<T, COLS>(f, 2, st)) return rc;
-    }
+    LAUNCH((tr_distill_part_kernel<256, T>), parts, dim3(256), d);
+    LAUNCH((tr_distill_join_kernel<256, T>), rows, dim3(256), d);
+    if (grad) LAUNCH((tr_distill_gradient_kernel<256, T>), parts, dim3(256), d);
+    return EBSP_OK;
+}
+
+template <class T>
+int distill_gradient(Distill d, hipStream_t st)
+{
+    LAUNCH((tr_distill_gradient_kernel<256, T>), dim3((unsigned)(d.N * d.splits)), dim3(256), d);
+    return EBSP_OK;
+}
+
+int check_distill(const Distill& d, int dtype, int index_bytes)
+{
+    if (!element_size(dtype) || !element_size(d.top_type)) return fail(EBSP_ERR_ARGUMENT, "dtype and top_dtype must be EBSP_BF16, EBSP_F16 or EBSP_F32");
+    if (index_bytes != 4 && index_bytes != 8) return fail(EBSP_ERR_ARGUMENT, "index_bytes must be 4 or 8");
+    if (d.N < 0 || d.N >= SIZE_MAX_DIM || d.V < 1 || d.V >= SIZE_MAX_DIM) return fail(EBSP_ERR_SHAPE, "invalid shape: N must be 0 and V 1 to 2^31 - 1");
+    if (d.top < 0 || d.top > TOP_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: top must be 0 to EBSP_DISTILL_TOP_MAX");
+    if (!(d.temperature > 0.f) || d.temperature > FLT_MAX) return fail(EBSP_ERR_ARGUMENT, "temperature must be a positive number");
+    if (d.N == 0) return EBSP_OK;
+    if (!d.logits || (d.top > 0 && (!d.top_index || !d.top_logit))) return fail(EBSP_ERR_NULL, "logits, top_index and top_logit must not be NULL");
+    if (!stride_ok(d.ld, d.V) || (d.top > 0 && !stride_ok(d.ldt, d.top))) return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");
+    if (!aligned(d.logits, element_size(dtype)) || !aligned(d.top_index, index_bytes) || !aligned(d.top_logit, element_size(d.top_type)) ||
+        !aligned(d.labels, 8) || !aligned(d.grad, element_size(dtype)) || !aligned(d.dloss, 4) || !aligned(d.loss, 4) || !aligned(d.stats, 4) ||
+        !aligned(d.status, 4))
+        return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
+    return EBSP_OK;
+}
+
+int check_gradient(const Distill& d)
+{
+    if (!d.grad || !d.dloss) return fail(EBSP_ERR_NULL, "dloss and dlogits must not be NULL");
+    if (!stride_ok(d.ldd, d.V)) return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");
+    if (d.grad == d.logits && d.ldd != d.ld) return fail(EBSP_ERR_ARGUMENT, "a gradient in the logits' place must have their row stride");
+    return EBSP_OK;
+}
+
+// Shared by the loss alone and with its gradient: the scratch, the launches.
+int run_distill(Distill& d, int dtype, bool grad, void* workspace, size_t workspace_bytes, hipStream_t st)
+{
+    const int size = element_size(dtype);
+    d.splits = distill_splits(d.N, d.V, size);
+    if (!launchable((i64)d.N * d.splits, 1024)) return fail(EBSP_ERR_SHAPE, "too many rows for one call");
+    const size_t need = ebsp_distill_workspace_bytes(d.N, d.V, dtype);
+    if (need && !workspace) return fail(EBSP_ERR_NULL, "workspace must not be NULL for this shape");
+    if (need && (workspace_bytes < need || !aligned(workspace, 256)))
+        return fail(EBSP_ERR_WORKSPACE, "workspace too small or not 256-byte aligned (ebsp_distill_workspace_bytes)");
+    if (int rc = check_device()) return rc;
+    d.partial = (float*)workspace;
+    if (grad && d.splits > 1) d.stats = (float*)((char*)workspace + distill_partial_bytes(d.N, d.splits));
+    return dtype == EBSP_BF16 ? distill_loss<__bf16>(d, grad, st) : dtype == EBSP_F16 ? distill_loss<_Float16>(d, grad, st) : distill_loss<float>(d, grad, st);
+}
+
+template <class T>
+int merge(const Merge& g, hipStream_t st)
+{
+    const i64 blocks = (g.n + 256 * PER_WORD4<T> - 1) / (256 * PER_WORD4<T>);
+    LAUNCH_LDS(tr_merge_kernel<T>, dim3((unsigned)blocks), dim3(256), g.P * sizeof(Share), g);
     return EBSP_OK;
 }
 
@@ -163,6 +262,79 @@ int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t 
     hipStream_t st = (hipStream_t)stream;
     auto run = dtype == EBSP_BF16 ? ff_backward<__bf16> : dtype == EBSP_F16 ? ff_backward<_Float16> : ff_backward<float>;
     return run(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldg, M, K, F, act, dx, lddx, dwg, dwu, lddw, workspace, st);
+}
+
+size_t ebsp_distill_workspace_bytes(int64_t N, int64_t V, int32_t dtype)
+{
+    const int size = element_size(dtype);
+    if (!size || N < 1 || N >= SIZE_MAX_DIM || V < 1 || V >= SIZE_MAX_DIM) return 0;
+    const int splits = distill_splits(N, V, size);
+    return splits > 1 ? distill_partial_bytes(N, splits) + ((size_t)N * 3 * sizeof(float) + 255) / 256 * 256 : 0;
+}
+
+int ebsp_distill_forward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const void* top_index, int32_t index_bytes,
+                         const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top, const int64_t* labels, float temperature,
+                         float kl_weight, float ce_weight, float* loss, float* stats, int32_t* status, void* workspace, size_t workspace_bytes,
+                         void* stream)
+{
+    Distill d = {logits, ld, N, V, top_index, top_logit, ldt, labels, nullptr, loss, stats, status, nullptr, 0, nullptr, top, top_dtype,
+                 index_bytes == 8, 1, temperature, kl_weight, ce_weight};
+    if (int rc = check_distill(d, dtype, index_bytes)) return rc;
+    if (N == 0) return EBSP_OK;
+    if (!loss) return fail(EBSP_ERR_NULL, "loss must not be NULL");
+    return run_distill(d, dtype, false, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int ebsp_distill_backward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const void* top_index, int32_t index_bytes,
+                          const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top, const int64_t* labels, float temperature,
+                          float kl_weight, float ce_weight, const float* stats, const float* dloss, void* dlogits, int64_t ldd, void* stream)
+{
+    Distill d = {logits, ld, N, V, top_index, top_logit, ldt, labels, dloss, nullptr, const_cast<float*>(stats), nullptr, dlogits, ldd, nullptr,
+                 top, top_dtype, index_bytes == 8, 1, temperature, kl_weight, ce_weight};
+    if (int rc = check_distill(d, dtype, index_bytes)) return rc;
+    if (N == 0) return EBSP_OK;
+    if (!stats) return fail(EBSP_ERR_NULL, "stats must not be NULL");
+    if (int rc = check_gradient(d)) return rc;
+    d.splits = distill_splits(N, V, element_size(dtype));
+    if (!launchable(N * d.splits, 1024)) return fail(EBSP_ERR_SHAPE, "too many rows for one call");
+    if (int rc = check_device()) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    return dtype == EBSP_BF16 ? distill_gradient<__bf16>(d, st) : dtype == EBSP_F16 ? distill_gradient<_Float16>(d, st) : distill_gradient<float>(d, st);
+}
+
+int ebsp_distill_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const void* top_index, int32_t index_bytes,
+                           const void* top_logit, int32_t top_dtype, int64_t ldt, int32_t top, const int64_t* labels, float temperature,
+                           float kl_weight, float ce_weight, const float* dloss, float* loss, void* dlogits, int64_t ldd, int32_t* status,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    Distill d = {logits, ld, N, V, top_index, top_logit, ldt, labels, dloss, loss, nullptr, status, dlogits, ldd, nullptr, top, top_dtype,
+                 index_bytes == 8, 1, temperature, kl_weight, ce_weight};
+    if (int rc = check_distill(d, dtype, index_bytes)) return rc;
+    if (N == 0) return EBSP_OK;
+    if (!loss) return fail(EBSP_ERR_NULL, "loss must not be NULL");
+    if (int rc = check_gradient(d)) return rc;
+    return run_distill(d, dtype, true, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, int32_t dtype, const int32_t* iters, const float* weights,
+                      const float* velocity, float lr, float momentum, int32_t nesterov, float* weights_out, float* velocity_out, void* pull,
+                      int32_t pull_dtype, void* stream)
+{
+    const int size = element_size(dtype);
+    if (!size || (pull && !element_size(pull_dtype))) return fail(EBSP_ERR_ARGUMENT, "dtype and pull_dtype must be EBSP_BF16, EBSP_F16 or EBSP_F32");
+    if (P < 1 || P > EBSP_MERGE_WORKERS_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: P must be 1 to EBSP_MERGE_WORKERS_MAX");
+    if (n < 0 || n >= 1ll << 34) return fail(EBSP_ERR_SHAPE, "invalid shape: n must be 0 to 2^34 - 1");
+    if (n == 0) return EBSP_OK;
+    if (!pushes || !iters || !weights || !weights_out) return fail(EBSP_ERR_NULL, "pushes, iters, weights and weights_out must not be NULL");
+    if (!velocity != !velocity_out) return fail(EBSP_ERR_NULL, "velocity and velocity_out must both be given or both be NULL");
+    if (P > 1 && !stride_ok(stride, n)) return fail(EBSP_ERR_ARGUMENT, "a worker's stride is shorter than its push, or 2^40 and more");
+    if (!aligned(pushes, size) || !aligned(iters, 4) || !aligned(weights, 4) || !aligned(velocity, 4) || !aligned(weights_out, 4) ||
+        !aligned(velocity_out, 4) || (pull && !aligned(pull, element_size(pull_dtype))))
+        return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
+    if (int rc = check_device()) return rc;
+    const Merge g = {pushes, stride, n, iters, weights, velocity, weights_out, velocity_out, pull, P, pull_dtype, nesterov, lr, momentum};
+    hipStream_t st = (hipStream_t)stream;
+    return dtype == EBSP_BF16 ? merge<__bf16>(g, st) : dtype == EBSP_F16 ? merge<_Float16>(g, st) : merge<float>(g, st);
 }
 
 }  // extern "C"

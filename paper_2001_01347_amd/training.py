@@ -1,8 +1,9 @@
-"""The training operators of libebsp_zipline.so (see include/ebsp_training.h): what a worker computes between two barriers.
+"""The training operators of libebsp_zipline.so (see include/ebsp_training.h): what a worker computes between two barriers
+and what the server does at one.
 
 ``ebsp_*`` bind the C ABI 1:1 like ``zipline`` does: argument checks, ``torch.empty`` for outputs that are not given, the
-current stream of the inputs' device, no synchronisation and no fallback.  ``gated_ff`` is the same operator as part of an
-autograd graph.
+current stream of the inputs' device, no synchronisation and no fallback.  ``gated_ff`` and ``distill_loss`` are the same
+operators as part of an autograd graph.
 """
 from __future__ import annotations
 
@@ -17,7 +18,11 @@ from .zipline import ZipLineError, _check_buffer, _check_workspace
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
-EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_workspace_bytes", "ebsp_gated_ff_backward")
+EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_workspace_bytes", "ebsp_gated_ff_backward", "ebsp_distill_workspace_bytes",
+           "ebsp_distill_forward", "ebsp_distill_backward", "ebsp_distill_loss_grad", "ebsp_merge_pushes")
+
+STATUS_RANGE = 4          # a row's index or label lies beyond the vocabulary
+TOP_MAX = 1024            # most teacher entries of a row
 
 _lib = None
 
@@ -35,6 +40,18 @@ def load() -> ctypes.CDLL:
         lib.ebsp_gated_ff_backward.restype = c_int
         lib.ebsp_gated_ff_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp,
                                                i64, vp, sz, vp]
+        f32 = ctypes.c_float
+        lib.ebsp_distill_workspace_bytes.restype = sz
+        lib.ebsp_distill_workspace_bytes.argtypes = [i64, i64, i32]
+        common = [vp, i64, i64, i64, i32, vp, i32, vp, i32, i64, i32, vp, f32, f32, f32]
+        lib.ebsp_distill_forward.restype = c_int
+        lib.ebsp_distill_forward.argtypes = common + [vp, vp, vp, vp, sz, vp]
+        lib.ebsp_distill_backward.restype = c_int
+        lib.ebsp_distill_backward.argtypes = common + [vp, vp, vp, i64, vp]
+        lib.ebsp_distill_loss_grad.restype = c_int
+        lib.ebsp_distill_loss_grad.argtypes = common + [vp, vp, vp, i64, vp, vp, sz, vp]
+        lib.ebsp_merge_pushes.restype = c_int
+        lib.ebsp_merge_pushes.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp, f32, f32, i32, vp, vp, vp, i32, vp]
         _lib = lib
     return _lib
 
@@ -141,6 +158,133 @@ def ebsp_gated_ff_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, 
     return dx, dwg, dwu
 
 
+def ebsp_distill_workspace_bytes(N: int, V: int, dtype: torch.dtype) -> int:
+    return int(load().ebsp_distill_workspace_bytes(N, V, DTYPES[dtype]))
+
+
+def _distill_operands(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight):
+    code = _dtype("logits", logits)
+    N, V = _matrix("logits", logits)
+    dev = logits.device
+    if V < 1:
+        raise ValueError("the vocabulary must not be empty")
+    ld = _rows("logits", logits, dev, logits.dtype, (N, V))
+    if not isinstance(top_index, torch.Tensor) or top_index.dim() != 2 or top_index.dtype not in (torch.int32, torch.int64):
+        raise ValueError("top_index must be an int32 or int64 tensor with two dimensions")
+    top = int(top_index.shape[1])
+    if top > TOP_MAX:
+        raise ValueError(f"top_index must have at most {TOP_MAX} entries a row")
+    top_code = _dtype("top_logit", top_logit)
+    ldt = _rows("top_index", top_index, dev, top_index.dtype, (N, top))
+    if _rows("top_logit", top_logit, dev, top_logit.dtype, (N, top)) != ldt:
+        raise ValueError("top_index and top_logit must have the same row stride")
+    if labels is not None:
+        _check_buffer("labels", labels, dev, torch.int64, (N,))
+    if not 0 < float(temperature) < float("inf"):
+        raise ValueError("temperature must be a positive number")
+    return N, V, dev, (logits.data_ptr(), ld, N, V, code, top_index.data_ptr(), top_index.element_size(), top_logit.data_ptr(), top_code, ldt,
+                       top, None if labels is None else labels.data_ptr(), float(temperature), float(kl_weight), float(ce_weight))
+
+
+def _distill_workspace(workspace, N, V, dtype, dev):
+    need = ebsp_distill_workspace_bytes(N, V, dtype)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev, need)
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+
+
+def ebsp_distill_forward(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, temperature: float = 1.0,
+                         kl_weight: float = 1.0, labels: Optional[torch.Tensor] = None, ce_weight: float = 0.0,
+                         loss: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The distillation loss of every row of ``logits`` [N, V] from the teacher's entries [N, top]; see the header.
+
+    Returns ``(loss[N], stats[N, 3], status[N])``; ``ebsp_distill_backward`` takes the stats.  Does not synchronise.
+    """
+    N, V, dev, args = _distill_operands(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight)
+    loss = _output("loss", loss, dev, torch.float32, (N,))
+    stats = _output("stats", stats, dev, torch.float32, (N, 3))
+    status = _output("status", status, dev, torch.int32, (N,))
+    ws = _distill_workspace(workspace, N, V, logits.dtype, dev)
+    _call("ebsp_distill_forward", dev, *args, loss.data_ptr(), stats.data_ptr(), status.data_ptr(), *ws)
+    return loss, stats, status
+
+
+def _gradient_place(logits: torch.Tensor, dlogits: Optional[torch.Tensor], dev):
+    """The gradient's tensor and row stride: a new one, a contiguous one, or the logits themselves."""
+    if dlogits is logits:
+        return logits, _rows("logits", logits, dev, logits.dtype, tuple(logits.shape))
+    return _output("dlogits", dlogits, dev, logits.dtype, tuple(logits.shape)), int(logits.shape[1])
+
+
+def ebsp_distill_backward(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, stats: torch.Tensor, dloss: torch.Tensor,
+                          temperature: float = 1.0, kl_weight: float = 1.0, labels: Optional[torch.Tensor] = None, ce_weight: float = 0.0,
+                          dlogits: Optional[torch.Tensor] = None):
+    """The gradient of ``ebsp_distill_forward`` for the rows' ``dloss`` [N]; ``dlogits`` may be ``logits``; see the header.
+
+    Returns ``dlogits[N, V]``.  Does not synchronise.
+    """
+    N, V, dev, args = _distill_operands(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight)
+    _check_buffer("stats", stats, dev, torch.float32, (N, 3))
+    _check_buffer("dloss", dloss, dev, torch.float32, (N,))
+    dlogits, ldd = _gradient_place(logits, dlogits, dev)
+    _call("ebsp_distill_backward", dev, *args, stats.data_ptr(), dloss.data_ptr(), dlogits.data_ptr(), ldd)
+    return dlogits
+
+
+def ebsp_distill_loss_grad(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, dloss: torch.Tensor,
+                           temperature: float = 1.0, kl_weight: float = 1.0, labels: Optional[torch.Tensor] = None, ce_weight: float = 0.0,
+                           loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                           status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Loss and gradient in one call, for a ``dloss`` [N] known beforehand; ``dlogits`` may be ``logits``; see the header.
+
+    Returns ``(loss[N], dlogits[N, V], status[N])``.  Does not synchronise.
+    """
+    N, V, dev, args = _distill_operands(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight)
+    _check_buffer("dloss", dloss, dev, torch.float32, (N,))
+    loss = _output("loss", loss, dev, torch.float32, (N,))
+    status = _output("status", status, dev, torch.int32, (N,))
+    dlogits, ldd = _gradient_place(logits, dlogits, dev)
+    ws = _distill_workspace(workspace, N, V, logits.dtype, dev)
+    _call("ebsp_distill_loss_grad", dev, *args, dloss.data_ptr(), loss.data_ptr(), dlogits.data_ptr(), ldd, status.data_ptr(), *ws)
+    return loss, dlogits, status
+
+
+def ebsp_merge_pushes(weights: torch.Tensor, pushes: torch.Tensor, iters: torch.Tensor, lr: float = 1.0, momentum: float = 0.0,
+                      nesterov: bool = False, velocity: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                      velocity_out: Optional[torch.Tensor] = None, pull=None):
+    """The server's weights after a barrier: ``pushes`` [P, n] merged by ``iters`` [P] as a search returns them; see the header.
+
+    ``weights`` and ``velocity`` are float32 [n]; ``out`` and ``velocity_out`` may be the same tensors.  ``pull`` is the type of
+    the rounded copy that the workers fetch, or a tensor for it, or None.  Returns ``(out, velocity_out, pull)``, None in the
+    place of what there is not.  Does not synchronise.
+    """
+    code = _dtype("pushes", pushes)
+    P, n = _matrix("pushes", pushes)
+    dev = pushes.device
+    stride = _rows("pushes", pushes, dev, pushes.dtype, (P, n))
+    _check_buffer("weights", weights, dev, torch.float32, (n,))
+    _check_buffer("iters", iters, dev, torch.int32, (P,))
+    out = _output("out", out, dev, torch.float32, (n,))
+    if velocity is not None:
+        _check_buffer("velocity", velocity, dev, torch.float32, (n,))
+        velocity_out = _output("velocity_out", velocity_out, dev, torch.float32, (n,))
+    elif velocity_out is not None or momentum != 0 or nesterov:
+        raise ValueError("momentum needs a velocity")
+    if isinstance(pull, torch.Tensor):
+        _dtype("pull", pull)
+        _check_buffer("pull", pull, dev, pull.dtype, (n,))
+    elif pull is not None:
+        if pull not in DTYPES:
+            raise ValueError("pull must be bfloat16, float16, float32 or a tensor of one of them")
+        pull = torch.empty((n,), dtype=pull, device=dev)
+    ptr = [None if t is None else t.data_ptr() for t in (velocity, velocity_out, pull)]
+    _call("ebsp_merge_pushes", dev, pushes.data_ptr(), stride, P, n, code, iters.data_ptr(), weights.data_ptr(), ptr[0], float(lr),
+          float(momentum), 1 if nesterov else 0, out.data_ptr(), ptr[1], ptr[2], 0 if pull is None else DTYPES[pull.dtype])
+    return out, velocity_out, pull
+
+
 class _GatedFF(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, wg, wu, act):
@@ -170,5 +314,37 @@ def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "si
     """``act(x wg^T) * (x wu^T)`` for x [..., K], with gradients for all three tensors."""
     if not isinstance(x, torch.Tensor) or x.dim() < 1:
         raise ValueError("x must be a tensor of shape [..., K]")
-    rows = _plain_rows(x.reshape(-1, x.shape[-1]) if x.shape[-1] > 0 else x.reshape(x.shape[:-1].numel(), 0))
+    rows = _plain_rows(x.reshape(x.shape[:-1].numel(), x.shape[-1]))
     return _GatedFF.apply(rows, wg, wu, act).reshape(*x.shape[:-1], wg.shape[0])
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight):
+        loss, stats, _ = ebsp_distill_forward(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight)
+        ctx.save_for_backward(logits, top_index, top_logit, stats, labels)
+        ctx.args = temperature, kl_weight, ce_weight
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        logits, top_index, top_logit, stats, labels = ctx.saved_tensors
+        temperature, kl_weight, ce_weight = ctx.args
+        grad = ebsp_distill_backward(logits, top_index, top_logit, stats, dloss.contiguous(), temperature, kl_weight, labels, ce_weight)
+        return grad, None, None, None, None, None, None
+
+
+def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, temperature: float = 1.0, kl_weight: float = 1.0,
+                 labels: Optional[torch.Tensor] = None, ce_weight: float = 0.0) -> torch.Tensor:
+    """The distillation loss of every row [...], for logits [..., V] and teacher entries [..., top], with the logits' gradient.
+
+    The teacher's tensors get none.  Indices and labels must lie in the vocabulary or be negative; those that do not are left
+    out (``ebsp_distill_forward`` flags them)."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() < 1:
+        raise ValueError("logits must be a tensor of shape [..., V]")
+    lead = logits.shape[:-1]
+    rows = _plain_rows(logits.reshape(lead.numel(), logits.shape[-1]))
+    entries = [t.reshape(lead.numel(), t.shape[-1]).contiguous() for t in (top_index, top_logit)]
+    flat = None if labels is None else labels.reshape(lead.numel()).contiguous()
+    return _Distill.apply(rows, *entries, temperature, kl_weight, flat, ce_weight).reshape(lead)

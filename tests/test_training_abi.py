@@ -100,3 +100,76 @@ def test_binding_refuses_cpu_tensors():
         training.ebsp_gated_ff_forward(x, w, w)
     with pytest.raises(ValueError):
         training.gated_ff(x, w, w)
+
+
+def _distill(lib, name="forward", logits=ONE, ld=100, N=4, V=100, dtype=BF16, index=ONE, index_bytes=8, values=ONE, top_dtype=BF16, ldt=8, top=8,
+             labels=NULL, T=1.0, loss=ONE, stats=ONE, status=NULL, dloss=ONE, grad=ONE, ldd=100, workspace=NULL, nbytes=0):
+    common = (logits, ld, N, V, dtype, index, index_bytes, values, top_dtype, ldt, top, labels, T, 1.0, 0.0)
+    if name == "forward":
+        return lib.ebsp_distill_forward(*common, loss, stats, status, workspace, nbytes, NULL)
+    if name == "backward":
+        return lib.ebsp_distill_backward(*common, stats, dloss, grad, ldd, NULL)
+    return lib.ebsp_distill_loss_grad(*common, dloss, loss, grad, ldd, status, workspace, nbytes, NULL)
+
+
+def test_distill_refuses(lib):
+    need = lib.ebsp_distill_workspace_bytes(2, 100000, BF16)
+    assert need > 0 and need % 256 == 0
+    wide = dict(N=2, V=100000, ld=100000, ldd=100000)
+    for bad, rc in ((dict(N=-1), -2), (dict(V=0), -2), (dict(V=1 << 31), -2), (dict(top=-1), -2), (dict(top=1025, ldt=1025), -2), (dict(dtype=3), -6),
+                    (dict(top_dtype=3), -6), (dict(index_bytes=2), -6), (dict(T=0.0), -6), (dict(T=-1.0), -6), (dict(T=float("nan")), -6),
+                    (dict(T=float("inf")), -6), (dict(logits=NULL), -1), (dict(index=NULL), -1), (dict(values=NULL), -1), (dict(ld=99), -6),
+                    (dict(ldt=7), -6), (dict(logits=ctypes.c_void_p(257)), -6), (dict(labels=ctypes.c_void_p(260)), -6),
+                    (dict(index=ctypes.c_void_p(260)), -6)):
+        for name in ("forward", "backward", "both"):
+            assert _distill(lib, name, **bad) == rc, (name, bad)
+            assert _error()
+    for name, bad, rc in (("forward", dict(loss=NULL), -1), ("both", dict(loss=NULL), -1), ("backward", dict(stats=NULL), -1),
+                          ("backward", dict(dloss=NULL), -1), ("backward", dict(grad=NULL), -1), ("both", dict(dloss=NULL), -1),
+                          ("both", dict(grad=NULL), -1), ("both", dict(ldd=99), -6), ("backward", dict(ldd=99), -6),
+                          ("backward", dict(logits=ONE, grad=ONE, ld=100, ldd=101), -6), ("forward", wide, -1),
+                          ("forward", dict(workspace=ONE, nbytes=need - 1, **wide), -3), ("both", dict(workspace=ONE, nbytes=need - 1, **wide), -3),
+                          ("both", dict(workspace=ctypes.c_void_p(264), nbytes=need, **wide), -3)):
+        assert _distill(lib, name, **bad) == rc, (name, bad)
+    for name in ("forward", "backward", "both"):
+        assert _distill(lib, name, N=0, logits=NULL, loss=NULL, grad=NULL) == 0                      # nothing to do
+        assert _distill(lib, name, N=(1 << 31) - 1, V=2, ld=2, ldd=2, top=0) == -2                   # more than a launch holds
+    ws = lib.ebsp_distill_workspace_bytes
+    assert ws(4096, 128000, BF16) == 0 and ws(0, 1000, BF16) == 0 and ws(1, 100, BF16) == 0 and ws(1, 0, BF16) == 0 and ws(1, 100, 3) == 0
+
+
+def _merge(lib, pushes=ONE, stride=100, P=4, n=100, dtype=BF16, iters=ONE, weights=ONE, velocity=NULL, out=ONE, velocity_out=NULL, pull=NULL,
+           pull_dtype=BF16):
+    return lib.ebsp_merge_pushes(pushes, stride, P, n, dtype, iters, weights, velocity, 1.0, 0.0, 0, out, velocity_out, pull, pull_dtype, NULL)
+
+
+def test_merge_refuses(lib):
+    for bad, rc in ((dict(P=0), -2), (dict(P=4097), -2), (dict(n=-1), -2), (dict(n=1 << 34, stride=1 << 34), -2), (dict(dtype=3), -6),
+                    (dict(pull=ONE, pull_dtype=3), -6), (dict(pushes=NULL), -1), (dict(iters=NULL), -1), (dict(weights=NULL), -1),
+                    (dict(out=NULL), -1), (dict(velocity=ONE), -1), (dict(velocity_out=ONE), -1), (dict(stride=99), -6),
+                    (dict(stride=1 << 40), -6), (dict(pushes=ctypes.c_void_p(257)), -6), (dict(iters=ctypes.c_void_p(258)), -6),
+                    (dict(pull=ctypes.c_void_p(258), pull_dtype=F32), -6)):
+        assert _merge(lib, **bad) == rc, bad
+        assert _error()
+    assert _merge(lib, n=0, pushes=NULL) == 0
+
+
+def test_valid_calls_of_the_others_without_a_gfx950_fail_loudly(lib):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    for name in ("forward", "backward", "both"):
+        assert _distill(lib, name) == -5
+    assert _merge(lib) == -5
+
+
+def test_binding_refuses_cpu_tensors_of_the_others():
+    import torch
+    from paper_2001_01347_amd import training
+    logits, index, values = torch.zeros((2, 8)), torch.zeros((2, 3), dtype=torch.int64), torch.zeros((2, 3))
+    with pytest.raises(ValueError):
+        training.ebsp_distill_forward(logits, index, values)
+    with pytest.raises(ValueError):
+        training.distill_loss(logits, index, values)
+    with pytest.raises(ValueError):
+        training.ebsp_merge_pushes(torch.zeros(8), torch.zeros((2, 8)), torch.ones(2, dtype=torch.int32))
