@@ -54,15 +54,15 @@ extern "C" {
  *   x       in  [M][K], rows ldx apart
  *   wg, wu  in  [F][K], rows ldwg and ldwu apart
  *   h       out [M][F], rows ldh apart
- *   g, u    out [M][F], rows ldg apart: what ebsp_gated_ff_backward needs.
- *               Both NULL where there will be no backward pass; h alone is
- *               written then.
- * All of one element type `dtype`; sums are held in 32 bits and rounded once.
+ *   g, u    out [M][F] float, rows ldg apart: what ebsp_gated_ff_backward
+ *               needs.  Both NULL where there will be no backward pass; h
+ *               alone is written then.
+ * The others of one element type `dtype`; sums are held in 32 bits and rounded once.
  * M == 0 or F == 0 is a valid no-op, K == 0 gives zero products.
  */
 int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu, int64_t ldwu,
                           int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
-                          void* h, int64_t ldh, void* g, void* u, int64_t ldg, void* stream);
+                          void* h, int64_t ldh, float* g, float* u, int64_t ldg, void* stream);
 
 /*
  * Its backward pass: from dh = dL/dh,
@@ -79,7 +79,7 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
  */
 size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype);
 int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
-                           const void* wu, int64_t ldwu, const void* g, const void* u, int64_t ldg,
+                           const void* wu, int64_t ldwu, const float* g, const float* u, int64_t ldg,
                            int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
                            void* dx, int64_t lddx, void* dwg, void* dwu, int64_t lddw,
                            void* workspace, size_t workspace_bytes, void* stream);

@@ -60,14 +60,15 @@ __device__ __forceinline__ void activation_both(int act, float g, float& a, floa
 
 struct FfForward {
     Operand x, w;                                                            // w: gate and up
-    void *h, *g, *u;                                                         // g, u: NULL where nothing is kept for a backward pass
+    void* h;
+    float *g, *u;                                                            // NULL where nothing is kept for a backward pass
     i64 ldh, ldg;
     int act, wide_h, wide_g;
 };
 
 // Gate and up of the same units lie in one wave's squares, so h is formed in registers: one read of x for both products, and
 // neither product goes to memory unless a backward pass will want it.
-template <class T, class TL>
+template <class T, class TL, bool DIRECT>
 __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
 {
     __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
@@ -77,8 +78,8 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
     tile_of(blockIdx.x, tm, tn, bm, bn);
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * (TL::BN / 2);
     Float4 acc[FN][FM];
-    product_tile<T, TL, ROWS, ROWS, FN>(acc, lds, f.x, f.w, 1, m0, n0);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    product_tile<T, TL, ROWS, ROWS, FN, DIRECT>(acc, lds, f.x, f.w, 1, m0, n0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -95,34 +96,39 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
             for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
             store4((T*)f.h + m * f.ldh + n, h, have, f.wide_h);
             if (f.g) {
-                store4((T*)f.g + m * f.ldg + n, g, have, f.wide_g);
-                store4((T*)f.u + m * f.ldg + n, u, have, f.wide_g);
+                store4(f.g + m * f.ldg + n, g, have, f.wide_g);
+                store4(f.u + m * f.ldg + n, u, have, f.wide_g);
             }
         }
     }
 }
 
 // dg = dh * u * act'(g) and du = dh * act(g), rows padded with zeros to a multiple of 16 bytes.  They are rounded to the inputs' type,
-// which is what the matrix cores multiply; the sums over them stay in 32 bits.
+// which is what the matrix cores multiply; the sums over them stay in 32 bits.  g and u come as the forward pass summed them: rounding
+// them too would make the gradients' error 1.8 times that of rounding the results alone, as it is 1.4 times.
 template <class T>
-__global__ void __launch_bounds__(256) tr_ff_units_kernel(const T* dh, i64 lddh, const T* g, const T* u, i64 ldg, T* dg, T* du, i64 ldd,
+__global__ void __launch_bounds__(256) tr_ff_units_kernel(const T* dh, i64 lddh, const float* g, const float* u, i64 ldg, T* dg, T* du, i64 ldd,
                                                           i64 M, i64 F, int act)
 {
     constexpr int N = PER_WORD4<T>;
     const i64 chunks = ldd / N, all = M * chunks;
     for (i64 at = (i64)blockIdx.x * 256 + threadIdx.x; at < all; at += (i64)gridDim.x * 256) {
         const i64 m = at / chunks, f = (at - m * chunks) * N;
-        Pack<T> ph, pg, pu, og, ou;
+        Pack<T> ph, og, ou;
+        Pack<float> pg[N / 4], pu[N / 4];
         ph.raw = load_some(dh + m * lddh + f, F - f);
-        pg.raw = load_some(g + m * ldg + f, F - f);
-        pu.raw = load_some(u + m * ldg + f, F - f);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            pg[i].raw = load_some(g + m * ldg + f + 4 * i, F - f - 4 * i);
+            pu[i].raw = load_some(u + m * ldg + f + 4 * i, F - f - 4 * i);
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, d;
-            activation_both(act, to_float(pg.v[i]), a, d);
+            activation_both(act, pg[i / 4].v[i % 4], a, d);
             const float h = to_float(ph.v[i]);
             const bool in = f + i < F;
-            og.v[i] = from_float<T>(in ? h * to_float(pu.v[i]) * d : 0.f);
+            og.v[i] = from_float<T>(in ? h * pu[i / 4].v[i % 4] * d : 0.f);
             ou.v[i] = from_float<T>(in ? h * a : 0.f);
         }
         *reinterpret_cast<Word4*>(dg + m * ldd + f) = og.raw;
@@ -136,15 +142,16 @@ struct FfGradient {
     i64 ld[2];
     int wide[2];
     int segments;                                                            // dx: 2, the sum runs over gate and up
+    i64 rows;                                                                // of the result (a.index counts the padded ones too)
 };
 
 // dx = dg Wg + du Wu (A in rows, two segments) and dW = dg^T x, du^T x (A in columns, a half of the grid each).
-template <class T, class TL, Layout LA>
+template <class T, class TL, Layout LA, bool DIRECT>
 __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
 {
     __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
     constexpr int FM = TL::FM, FN = TL::FN;
-    const u32 tm = (u32)((f.a.index + TL::BM - 1) / TL::BM), tn = (u32)((f.b.index + TL::BN - 1) / TL::BN);
+    const u32 tm = (u32)((f.rows + TL::BM - 1) / TL::BM), tn = (u32)((f.b.index + TL::BN - 1) / TL::BN);
     u32 bm, bn;
     tile_of(blockIdx.x, tm, tn, bm, bn);
     const int z = blockIdx.y;
@@ -152,13 +159,13 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
     if (LA == COLS && z) a.p[0] = a.p[1];
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * TL::BN;
     Float4 acc[FN][FM];
-    product_tile<T, TL, LA, COLS, 0>(acc, lds, a, f.b, f.segments, m0, n0);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    product_tile<T, TL, LA, COLS, 0, DIRECT>(acc, lds, a, f.b, f.segments, m0, n0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const i64 m = m0 + (wm * FM + i) * 16 + (lane & 15);
-        if (m >= f.a.index) continue;
+        if (m >= f.rows) continue;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const i64 n = n0 + (wn * FN + j) * 16 + (lane >> 4) * 4;

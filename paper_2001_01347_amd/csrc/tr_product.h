@@ -85,6 +85,55 @@ __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0
     }
 }
 
+// The same tile straight from memory to shared memory, no registers between: the shared side of such a load is 16 bytes a lane in
+// lane order, so the lanes' order is permuted on the memory side.  Rows (columns) beyond the operand repeat its last ones; what comes
+// of them is not stored.  Needs whole 16-byte chunks: operand_direct() on the host.
+template <class T, Layout L, int BI, int NT, int PAIRED>
+struct DirectTile {
+    static constexpr int P = BI * 8 / NT, N = PER_WORD4<T>;
+    const char* base[2];
+    i64 step;                                                                // bytes to the next step's part
+    u32 off[P];
+
+    __device__ __forceinline__ void init(const Operand& o, i64 i0)
+    {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            int row, chunk, which = 0;
+            tile_source<T, L, BI>(i * NT + (int)threadIdx.x, row, chunk);
+            if constexpr (L == ROWS) {
+                if constexpr (PAIRED > 0) row = paired_row<PAIRED>(row, which);
+                const i64 last = o.index - 1 - i0;
+                off[i] = (u32)((i64)(row < last ? row : last) * o.ld[which] * (i64)sizeof(T)) + chunk * 16;
+            } else {
+                const i64 last = o.index - N - i0, col = (i64)chunk * N;
+                off[i] = (u32)((i64)row * o.ld[0] * (i64)sizeof(T) + (col < last ? col : last) * (i64)sizeof(T));
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) base[w] = (const char*)o.p[w] + (L == ROWS ? i0 * o.ld[w] : i0) * (i64)sizeof(T);
+        step = L == ROWS ? 128 : (i64)(128 / sizeof(T)) * o.ld[0] * (i64)sizeof(T);
+    }
+
+    // The part at contraction step `s` of segment `seg` into the tile at `lds`.
+    __device__ __forceinline__ void bring(char* lds, int seg, int s, int wave) const
+    {
+        typedef __attribute__((address_space(1))) const void GlobalAny;
+        typedef __attribute__((address_space(3))) void LdsAny;
+        const i64 at = s * step;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const char* b = base[0];
+            if constexpr (PAIRED > 0) {
+                if ((i * (NT / 8) + wave * 8) % (PAIRED * 16) >= PAIRED * 8) b = base[1];
+            } else {
+                if (seg) b = base[1];
+            }
+            __builtin_amdgcn_global_load_lds((GlobalAny*)(b + at + off[i]), (LdsAny*)(lds + (i * NT + wave * 64) * 16), 16, 0, 0);
+        }
+    }
+};
+
 // A lane's 16 bytes of the square at `base` (a multiple of 16) for half `ks` of a step: index base + lane % 16, contraction
 // (lane / 16) * 16 bytes and on.
 template <class T, Layout L, int BI>
@@ -140,14 +189,33 @@ __device__ __forceinline__ void tile_of(u32 id, u32 tm, u32 tn, u32& m, u32& n)
     n = in / rows;
 }
 
+// One step's products out of shared memory.
+template <class T, class TL, Layout LA, Layout LB>
+__device__ __forceinline__ void step_products(Float4 (&acc)[TL::FN][TL::FM], const char* ta, const char* tb, int wm, int wn, int lane)
+{
+    constexpr int FM = TL::FM, FN = TL::FN;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+        Word4 fm[FM], fn[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fn[j] = read_square<T, LB, TL::BN>(tb, (wn * FN + j) * 16, ks, lane);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) fm[i] = read_square<T, LA, TL::BM>(ta, (wm * FM + i) * 16, ks, lane);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) square_product<T>(acc[j][i], fn[j], fm[i]);
+    }
+}
+
 // The sums of the tile at (m0, n0) over `segments` matrices of each operand one after the other (PAIRED > 0: over one, B's
 // two alternating in the tile).
-template <class T, class TL, Layout LA, Layout LB, int PAIRED>
+template <class T, class TL, Layout LA, Layout LB, int PAIRED, bool DIRECT>
 __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char* lds, const Operand& a, const Operand& b, int segments, i64 m0, i64 n0)
 {
     constexpr int FM = TL::FM, FN = TL::FN, NT = TL::NT, BM = TL::BM, BN = TL::BN, BK = TL::BK;
     constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;                        // 16-byte positions a thread brings of each operand
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -156,6 +224,7 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
 
     const i64 depth = a.depth > b.depth ? a.depth : b.depth;
     const int steps = (int)((depth + BK - 1) / BK), total = steps * segments;
+    if (total == 0) return;
     Word4 ra[PA], rb[PB];
     auto fetch = [&](int s) {
         const int seg = s >= steps;
@@ -172,28 +241,42 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
 #pragma unroll
         for (int i = 0; i < PB; ++i) *reinterpret_cast<Word4*>(at + BM * 128 + (i * NT + tid) * 16) = rb[i];
     };
-    if (total == 0) return;
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int s = 0; s < total; ++s) {
-        const char* ta = lds + (s & 1) * (BM + BN) * 128;
-        const char* tb = ta + BM * 128;
-        if (s + 1 < total) fetch(s + 1);
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            Word4 fm[FM], fn[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) fm[i] = read_square<T, LA, BM>(ta, (wm * FM + i) * 16, ks, lane);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) fn[j] = read_square<T, LB, BN>(tb, (wn * FN + j) * 16, ks, lane);
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int i = 0; i < FM; ++i) square_product<T>(acc[j][i], fn[j], fm[i]);
-        }
-        if (s + 1 < total) put(s + 1);                                       // the half that nothing reads any more
+    if constexpr (DIRECT) {
+        DirectTile<T, LA, BM, NT, 0> da;
+        DirectTile<T, LB, BN, NT, PAIRED> db;
+        da.init(a, m0);
+        db.init(b, n0);
+        const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK);   // steps of which nothing lies outside; the last may be another
+        auto bring = [&](int s) {
+            const int seg = s >= steps, k = s - seg * steps;
+            if (k < whole) {
+                char* at = lds + (s & 1) * (BM + BN) * 128;
+                da.bring(at, seg, k, wave);
+                db.bring(at + BM * 128, seg, k, wave);
+            } else {
+                fetch(s);
+                put(s);
+            }
+        };
+        bring(0);
         __syncthreads();
+        for (int s = 0; s < total; ++s) {
+            const char* ta = lds + (s & 1) * (BM + BN) * 128;
+            if (s + 1 < total) bring(s + 1);
+            step_products<T, TL, LA, LB>(acc, ta, ta + BM * 128, wm, wn, lane);
+            __syncthreads();
+        }
+    } else {
+        fetch(0);
+        put(0);
+        __syncthreads();
+        for (int s = 0; s < total; ++s) {
+            const char* ta = lds + (s & 1) * (BM + BN) * 128;
+            if (s + 1 < total) fetch(s + 1);
+            step_products<T, TL, LA, LB>(acc, ta, ta + BM * 128, wm, wn, lane);
+            if (s + 1 < total) put(s + 1);                                   // the half that nothing reads any more
+            __syncthreads();
+        }
     }
 }
 

@@ -71,44 +71,72 @@ int tile_grid(i64 m, i64 n, dim3& grid, int z = 1)
     return EBSP_OK;
 }
 
+// Whole 16-byte chunks all along, and offsets inside a tile that fit 31 bits: what loads straight to shared memory need.
+bool operand_direct(const Operand& o, Layout l, int size)
+{
+    const i64 n = 16 / size;
+    for (int w = 0; w < 2; ++w)
+        if (o.p[w] && (!aligned(o.p[w], 16) || o.ld[w] % n || o.ld[w] * size * 256 > 0x7fffffffll)) return false;
+    return (l == ROWS ? o.depth : o.index) % n == 0;
+}
+
+template <class T, class TL>
+int ff_forward_tiles(const FfForward& f, hipStream_t st)
+{
+    const bool direct = operand_direct(f.x, ROWS, sizeof(T)) && operand_direct(f.w, ROWS, sizeof(T));
+    dim3 grid;
+    if (int rc = tile_grid<TL, TL::BN / 2>(f.x.index, f.w.index, grid)) return rc;
+    if (direct) LAUNCH((tr_ff_forward_kernel<T, TL, true>), grid, dim3(TL::NT), f);
+    else LAUNCH((tr_ff_forward_kernel<T, TL, false>), grid, dim3(TL::NT), f);
+    return EBSP_OK;
+}
+
+i64 tiles_of(i64 m, i64 n, int bm, int bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); }
+
 template <class T>
 int ff_forward(const FfForward& f, hipStream_t st)
 {
-    using TL = Tile<T, 2, 2, 4, 4>;
+    if (tiles_of(f.x.index, f.w.index, 256, 128) >= 192) return ff_forward_tiles<T, Tile<T, 2, 4, 8, 4>>(f, st);
+    return ff_forward_tiles<T, Tile<T, 2, 2, 4, 4>>(f, st);
+}
+
+template <class T, class TL, Layout LA>
+int ff_gradient_tiles(const FfGradient& f, int z, bool launch, hipStream_t st)
+{
+    const bool direct = operand_direct(f.a, LA, sizeof(T)) && operand_direct(f.b, COLS, sizeof(T));
     dim3 grid;
-    if (int rc = tile_grid<TL, TL::BN / 2>(f.x.index, f.w.index, grid)) return rc;
-    LAUNCH((tr_ff_forward_kernel<T, TL>), grid, dim3(TL::NT), f);
+    if (int rc = tile_grid<TL, TL::BN>(f.rows, f.b.index, grid, z)) return rc;
+    if (!launch) return EBSP_OK;
+    if (direct) LAUNCH((tr_ff_gradient_kernel<T, TL, LA, true>), grid, dim3(TL::NT), f);
+    else LAUNCH((tr_ff_gradient_kernel<T, TL, LA, false>), grid, dim3(TL::NT), f);
     return EBSP_OK;
 }
 
 template <class T, Layout LA>
 int ff_gradient(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
-    using TL = Tile<T, 2, 2, 4, 4>;
-    dim3 grid;
-    if (int rc = tile_grid<TL, TL::BN>(f.a.index, f.b.index, grid, z)) return rc;
-    if (launch) LAUNCH((tr_ff_gradient_kernel<T, TL, LA>), grid, dim3(TL::NT), f);
-    return EBSP_OK;
+    if (tiles_of(f.rows, f.b.index, 256, 256) * z >= 192) return ff_gradient_tiles<T, Tile<T, 2, 4, 8, 4>, LA>(f, z, launch, st);
+    return ff_gradient_tiles<T, Tile<T, 2, 2, 4, 4>, LA>(f, z, launch, st);
 }
 
 template <class T>
-int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg, i64 ldwg, const void* wu, i64 ldwu, const void* g,
-                const void* u, i64 ldg, i64 M, i64 K, i64 F, int act, void* dx, i64 lddx, void* dwg, void* dwu, i64 lddw, void* workspace,
+int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg, i64 ldwg, const void* wu, i64 ldwu, const float* g,
+                const float* u, i64 ldg, i64 M, i64 K, i64 F, int act, void* dx, i64 lddx, void* dwg, void* dwu, i64 lddw, void* workspace,
                 hipStream_t st)
 {
     const i64 ldd = padded_units(F, sizeof(T));
     T* dg = (T*)workspace;
     T* du = dg + M * ldd;
     const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0},
-                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2};
-    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, F, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
-                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1};
+                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2, M};
+    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
+                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1, F};
     for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
         const i64 chunks = M * (ldd / PER_WORD4<T>);
         if (launch && chunks > 0) {
             const i64 blocks = (chunks + 255) / 256;
-            LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, (const T*)g,
-                   (const T*)u, ldg, dg, du, ldd, M, F, act);
+            LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, g, u,
+                   ldg, dg, du, ldd, M, F, act);
         }
         if (dx && M > 0)
             if (int rc = ff_gradient<T, ROWS>(to_x, 1, launch, st)) return rc;
@@ -213,7 +241,8 @@ int merge(const Merge& g, hipStream_t st)
 extern "C" {
 
 int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu, int64_t ldwu, int64_t M, int64_t K,
-                          int64_t F, int32_t dtype, int32_t act, void* h, int64_t ldh, void* g, void* u, int64_t ldg, void* stream)
+                          int64_t F, int32_t dtype, int32_t act, void* h, int64_t ldh, float* g, float* u, int64_t ldg,
+                          void* stream)
 {
     if (int rc = check_sizes(M, K, F, dtype, act)) return rc;
     if (M == 0 || F == 0) return EBSP_OK;
@@ -222,11 +251,11 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
     if (!stride_ok(ldx, K) || !stride_ok(ldwg, K) || !stride_ok(ldwu, K) || !stride_ok(ldh, F) || (g && !stride_ok(ldg, F)))
         return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");
     const int size = element_size(dtype);
-    if (!aligned(x, size) || !aligned(wg, size) || !aligned(wu, size) || !aligned(h, size) || !aligned(g, size) || !aligned(u, size))
+    if (!aligned(x, size) || !aligned(wg, size) || !aligned(wu, size) || !aligned(h, size) || !aligned(g, 4) || !aligned(u, 4))
         return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
     if (int rc = check_device()) return rc;
     FfForward f = {{{x, x}, {ldx, ldx}, M, K}, {{wg, wu}, {ldwg, ldwu}, F, K}, h, g, u, ldh, ldg, act,
-                   wide_rows(h, ldh, size), g ? wide_rows(g, ldg, size) && wide_rows(u, ldg, size) : 0};
+                   wide_rows(h, ldh, size), g ? wide_rows(g, ldg, 4) && wide_rows(u, ldg, 4) : 0};
     hipStream_t st = (hipStream_t)stream;
     return dtype == EBSP_BF16 ? ff_forward<__bf16>(f, st) : dtype == EBSP_F16 ? ff_forward<_Float16>(f, st) : ff_forward<float>(f, st);
 }
@@ -239,7 +268,7 @@ size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype)
 }
 
 int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu,
-                           int64_t ldwu, const void* g, const void* u, int64_t ldg, int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
+                           int64_t ldwu, const float* g, const float* u, int64_t ldg, int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
                            void* dx, int64_t lddx, void* dwg, void* dwu, int64_t lddw, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (int rc = check_sizes(M, K, F, dtype, act)) return rc;
@@ -253,9 +282,9 @@ int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t 
         (dwg && !stride_ok(lddw, K)))
         return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");
     const int size = element_size(dtype);
-    const void* all[] = {dh, x, wg, wu, g, u, dx, dwg, dwu};
+    const void* all[] = {dh, x, wg, wu, dx, dwg, dwu};
     for (const void* p : all)
-        if (!aligned(p, size)) return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
+        if (!aligned(p, size) || !aligned(g, 4) || !aligned(u, 4)) return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
     if (units && (workspace_bytes < ebsp_gated_ff_workspace_bytes(M, F, dtype) || !aligned(workspace, 256)))
         return fail(EBSP_ERR_WORKSPACE, "workspace too small or not 256-byte aligned (ebsp_gated_ff_workspace_bytes)");
     if (int rc = check_device()) return rc;

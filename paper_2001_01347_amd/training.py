@@ -114,14 +114,14 @@ def ebsp_gated_ff_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, a
                           h: Optional[torch.Tensor] = None, g: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None):
     """``act(x wg^T) * (x wu^T)`` for x [M, K] and weights [F, K]; see the header.
 
-    Returns ``(h[M, F], g, u)``; with ``save`` g and u are the products [M, F] that ``ebsp_gated_ff_backward`` takes,
+    Returns ``(h[M, F], g, u)``; with ``save`` g and u are the products [M, F], float32, that ``ebsp_gated_ff_backward`` takes,
     otherwise None.  Rows of the operands may lie any distance apart.  Does not synchronise.
     """
     code, M, K, F, dev, dt, operands = _ff_operands(x, wg, wu)
     act = _activation(act)
     h = _output("h", h, dev, dt, (M, F))
     if save or g is not None or u is not None:
-        g, u = _output("g", g, dev, dt, (M, F)), _output("u", u, dev, dt, (M, F))
+        g, u = _output("g", g, dev, torch.float32, (M, F)), _output("u", u, dev, torch.float32, (M, F))
     _call("ebsp_gated_ff_forward", dev, *operands, M, K, F, code, act, h.data_ptr(), F,
           None if g is None else g.data_ptr(), None if u is None else u.data_ptr(), F)
     return h, g, u
@@ -142,8 +142,8 @@ def ebsp_gated_ff_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, 
     code, M, K, F, dev, dt, operands = _ff_operands(x, wg, wu)
     act = _activation(act)
     lddh = _rows("dh", dh, dev, dt, (M, F))
-    ldg = _rows("g", g, dev, dt, (M, F))
-    if _rows("u", u, dev, dt, (M, F)) != ldg:
+    ldg = _rows("g", g, dev, torch.float32, (M, F))
+    if _rows("u", u, dev, torch.float32, (M, F)) != ldg:
         raise ValueError("g and u must have the same row stride")
     dx = _output("dx", dx, dev, dt, (M, K)) if want_dx else None
     dwg = _output("dwg", dwg, dev, dt, (F, K)) if want_dw else None

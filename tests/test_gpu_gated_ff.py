@@ -3,8 +3,8 @@
 Tolerances.  A result is rounded once to its type: half a step, ``finfo.eps / 2`` of its size, ``u`` below.  Sums of n
 products are held in 32 bits: an error of at most ``2 (n + 8) 2^-24`` of the sum of the products' sizes (each addition rounds
 once, the matrix cores may round twice).  The activations are off by at most ``2^-20 (1 + |g|)``.  The backward pass starts from g and u
-rounded to the type and rounds dg and du to it: half a step each, the one of g through the activation's curvature (at most 1
-in size, for all of them).  These bounds hold element by element; as rounding errors are of either sign, their sums' norm is also held to a few u."""
+as they were summed (an error of g goes through the activation's curvature, at most 1 in size for all of them) and rounds dg and
+du to the type: half a step each.  These bounds hold element by element; as rounding errors are of either sign, their sums' norm is also held to a few u."""
 import math
 
 import pytest
@@ -64,7 +64,7 @@ class Reference:
         if dh is None:
             return
         dh = dh.double()
-        rg, ru = eg + u_t * g.abs() + tiny, eu + u_t * u.abs() + tiny       # g and u as they are saved
+        rg, ru = eg, eu
         ed = rg + 2.0 ** -20 * (1 + g.abs())
         if act == "relu":
             ed = torch.where(g.abs() <= rg, 1.0, 0.0)                       # the step may be taken on either side
@@ -89,7 +89,7 @@ def _compare(got, ref, names, norms=True):
         if norms and value.dtype != torch.float32 and want.numel() > 64:
             u_t = torch.finfo(value.dtype).eps / 2
             rel = (off.norm() / want.norm().clamp(min=1e-30)).item()
-            assert rel <= (1.1 if name == "h" else 4.0) * u_t, f"{name}: the error's norm is {rel / u_t:.3g} half steps"
+            assert rel <= (1.1 if name == "h" else 2.0) * u_t, f"{name}: the error's norm is {rel / u_t:.3g} half steps"
 
 
 def _inputs(M, K, F, dtype, seed=0, pad=0):
@@ -274,7 +274,7 @@ def test_binding_refuses(tr):
         tr.ebsp_gated_ff_forward(x, wg, wu, "tanh")
     with pytest.raises(ValueError):
         tr.ebsp_gated_ff_forward(x, wg, wu, h=torch.empty((8, 25), dtype=torch.bfloat16, device="cuda"))
-    for args in ((dh[:, :8], x, wg, wu, g, u), (dh, x, wg, wu, g.float(), u), (dh, x, wg, wu, g, u[:4])):
+    for args in ((dh[:, :8], x, wg, wu, g, u), (dh, x, wg, wu, g.half(), u), (dh, x, wg, wu, g, u[:4])):
         with pytest.raises(ValueError):
             tr.ebsp_gated_ff_backward(*args)
     with pytest.raises(ValueError):
