@@ -66,8 +66,9 @@ __device__ __forceinline__ int paired_row(int row, int& which)
     return row / (FN * 16) * (FN * 8) + (which ? q - FN * 8 : q);
 }
 
-// The 16 bytes of position `pos`, through registers, whatever the alignment; what lies outside the operand reads as zero.
-template <class T, Layout L, int BI, int PAIRED>
+// The 16 bytes of position `pos`, through registers; what lies outside the operand reads as zero.  WHOLE: chunks lie inside or
+// outside as a whole, at multiples of 16 bytes; otherwise whatever the alignment.
+template <class T, Layout L, int BI, int PAIRED, bool WHOLE>
 __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0, i64 k0, int pos)
 {
     int row, chunk;
@@ -76,12 +77,14 @@ __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0
     if constexpr (L == ROWS) {
         if constexpr (PAIRED > 0) row = paired_row<PAIRED>(row, which);
         const i64 i = i0 + row, k = k0 + chunk * N;
-        if (i >= o.index) return Word4{0, 0, 0, 0};
-        return load_some((const T*)o.p[which] + i * o.ld[which] + k, o.depth - k);
+        const T* p = (const T*)o.p[which] + i * o.ld[which] + k;
+        if constexpr (WHOLE) return i < o.index && k < o.depth ? *reinterpret_cast<const Word4*>(p) : Word4{0, 0, 0, 0};
+        return i < o.index ? load_some(p, o.depth - k) : Word4{0, 0, 0, 0};
     } else {
         const i64 k = k0 + row, i = i0 + chunk * N;
-        if (k >= o.depth) return Word4{0, 0, 0, 0};
-        return load_some((const T*)o.p[which] + k * o.ld[which] + i, o.index - i);
+        const T* p = (const T*)o.p[which] + k * o.ld[which] + i;
+        if constexpr (WHOLE) return i < o.index && k < o.depth ? *reinterpret_cast<const Word4*>(p) : Word4{0, 0, 0, 0};
+        return k < o.depth ? load_some(p, o.index - i) : Word4{0, 0, 0, 0};
     }
 }
 
@@ -230,9 +233,9 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         const int seg = s >= steps;
         const i64 k0 = (i64)(s - seg * steps) * BK;
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = fetch_chunk<T, LA, BM, 0>(a, seg, m0, k0, i * NT + tid);
+        for (int i = 0; i < PA; ++i) ra[i] = fetch_chunk<T, LA, BM, 0, DIRECT>(a, seg, m0, k0, i * NT + tid);
 #pragma unroll
-        for (int i = 0; i < PB; ++i) rb[i] = fetch_chunk<T, LB, BN, PAIRED>(b, seg, n0, k0, i * NT + tid);
+        for (int i = 0; i < PB; ++i) rb[i] = fetch_chunk<T, LB, BN, PAIRED, DIRECT>(b, seg, n0, k0, i * NT + tid);
     };
     auto put = [&](int s) {
         char* at = lds + (s & 1) * (BM + BN) * 128;
@@ -259,12 +262,43 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
             }
         };
         bring(0);
+        if (total > 1) bring(1);
+        __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
+        // A step is 2 FM groups, one square row of A times all of B's squares each.  A's squares are read AHEAD groups before their
+        // products, B's of the other half of the step as early; when the last read of a step is through, its half of the shared memory is
+        // given to the step after the next, and the last groups read the next step's first squares.  So products never wait for a
+        // read that was just issued, and a load has almost a whole step to arrive.
+        constexpr int GROUPS = 2 * FM, AHEAD = 4;
+        static_assert(FM % AHEAD == 0 && FN <= AHEAD, "the squares of a step are read before its last groups");
+        Word4 fm[GROUPS], fn[2][FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fn[0][j] = read_square<T, LB, BN>(lds + BM * 128, (wn * FN + j) * 16, 0, lane);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fm[i] = read_square<T, LA, BM>(lds, (wm * FM + i) * 16, 0, lane);
         for (int s = 0; s < total; ++s) {
             const char* ta = lds + (s & 1) * (BM + BN) * 128;
-            if (s + 1 < total) bring(s + 1);
-            step_products<T, TL, LA, LB>(acc, ta, ta + BM * 128, wm, wn, lane);
-            __syncthreads();
+            const char* next = lds + (~s & 1) * (BM + BN) * 128;
+#pragma unroll
+            for (int q = 0; q < GROUPS; ++q) {
+                if (q == GROUPS - AHEAD) {
+                    __builtin_amdgcn_s_waitcnt(0);
+                    __syncthreads();
+                    if (s + 2 < total) bring(s + 2);
+                }
+                if (q < GROUPS - AHEAD) {
+                    const int r = q + AHEAD;
+                    fm[r] = read_square<T, LA, BM>(ta, (wm * FM + r % FM) * 16, r / FM, lane);
+                    if (q < FN) fn[1][q] = read_square<T, LB, BN>(ta + BM * 128, (wn * FN + q) * 16, 1, lane);
+                } else {                                                     // (behind the last step: read, and not used)
+                    const int r = q - (GROUPS - AHEAD);
+                    fm[r] = read_square<T, LA, BM>(next, (wm * FM + r) * 16, 0, lane);
+                    if (r < FN) fn[0][r] = read_square<T, LB, BN>(next + BM * 128, (wn * FN + r) * 16, 0, lane);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) square_product<T>(acc[j][q % FM], fn[q / FM][j], fm[q]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     } else {
         fetch(0);
