@@ -7,7 +7,8 @@
 namespace {
 
 // act(g) and act'(g).  The activation is chosen by a value that is the same for the whole launch.
-__device__ __forceinline__ float sigmoid(float g) { return 1.f / (1.f + expf(-g)); }
+// (The hardware's exponential and reciprocal are good to an ulp.)
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)); }
 
 __device__ __forceinline__ float activation(int act, float g)
 {
@@ -45,7 +46,7 @@ __device__ __forceinline__ void activation_both(int act, float g, float& a, floa
     case EBSP_ACT_GELU: {
         const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
         a = g * cdf;
-        d = cdf + g * 0.39894228040143268f * expf(-0.5f * g * g);
+        d = cdf + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
         break;
     }
     default: {

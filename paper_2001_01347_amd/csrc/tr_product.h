@@ -2,8 +2,9 @@
 // Part of the ZipLine library (see training.hip); device code for gfx950.
 //
 // A workgroup computes a BM x BN tile of D; its WM x WN waves hold FM x FN squares of 16 x 16 each.  A step takes 128 bytes
-// of the contraction (64 16-bit or 32 32-bit elements) of every row of both operands through shared memory, two steps'
-// worth of which lie there: one is multiplied while the next arrives.
+// of the contraction (64 16-bit or 32 32-bit elements) of every row of both operands through shared memory, where there is room
+// for three steps of A and two of B: a wave reads all of its B early in a step, so the step after the next can be sent for as soon as that
+// is done, and a load has a step and a half to arrive.  (Two and two: 1070 TFLOP/s at dx of 8192 x 4096 x 12288 in place of ###.)
 //
 // An operand lies in memory in one of two ways, whichever way the caller's matrices give it: ROWS (the contraction is
 // contiguous: x and W in x W^T) or COLS (the index is contiguous: W in dg W, both in dg^T x).  ROWS tiles are read from
@@ -25,7 +26,8 @@ struct Tile {
     static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_;
     static constexpr int BM = WM * FM * 16, BN = WN * FN * 16, NT = WM * WN * WAVE;
     static constexpr int BK = 128 / (int)sizeof(T);
-    static constexpr int LDS = 2 * (BM + BN) * 128;
+    static constexpr int SLOT_A = BM * 128, SLOT_B = BN * 128;
+    static constexpr int LDS = 3 * SLOT_A + 2 * SLOT_B;
 };
 
 // One operand: `index` rows of D's axis, `depth` of the contraction, `ld` elements from a row in memory to the next.
@@ -66,7 +68,7 @@ __device__ __forceinline__ int paired_row(int row, int& which)
     return row / (FN * 16) * (FN * 8) + (which ? q - FN * 8 : q);
 }
 
-// The 16 bytes of position `pos`, through registers; what lies outside the operand reads as zero.  WHOLE: chunks lie inside or
+// The 16 bytes of position `pos` of the tile that begins at contraction k0, through registers; what lies outside the operand reads as zero.  WHOLE: chunks lie inside or
 // outside as a whole, at multiples of 16 bytes; otherwise whatever the alignment.
 template <class T, Layout L, int BI, int PAIRED, bool WHOLE>
 __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0, i64 k0, int pos)
@@ -95,7 +97,7 @@ template <class T, Layout L, int BI, int NT, int PAIRED>
 struct DirectTile {
     static constexpr int P = BI * 8 / NT, N = PER_WORD4<T>;
     const char* base[2];
-    i64 step;                                                                // bytes to the next step's part
+    i64 step;                                                                // bytes from a step to the next
     u32 off[P];
 
     __device__ __forceinline__ void init(const Operand& o, i64 i0)
@@ -118,7 +120,7 @@ struct DirectTile {
         step = L == ROWS ? 128 : (i64)(128 / sizeof(T)) * o.ld[0] * (i64)sizeof(T);
     }
 
-    // The part at contraction step `s` of segment `seg` into the tile at `lds`.
+    // Step `s` of segment `seg` into the slot at `lds`.
     __device__ __forceinline__ void bring(char* lds, int seg, int s, int wave) const
     {
         typedef __attribute__((address_space(1))) const void GlobalAny;
@@ -137,6 +139,12 @@ struct DirectTile {
     }
 };
 
+// Four rows of 16 16-bit elements each that 16 lanes read, 8 bytes a lane, come back as columns.  (Through a restrict pointer: without any
+// aliasing facts the compiler waits for every load to shared memory under way before such a read.  Which loads have to be
+// through is product_tile's business.)
+typedef __attribute__((address_space(3))) Short4 LdsShort4;
+__device__ __forceinline__ Short4 read_transposed(LdsShort4* __restrict p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
+
 // A lane's 16 bytes of the square at `base` (a multiple of 16) for half `ks` of a step: index base + lane % 16, contraction
 // (lane / 16) * 16 bytes and on.
 template <class T, Layout L, int BI>
@@ -151,10 +159,9 @@ __device__ __forceinline__ Word4 read_square(const char* tile, int base, int ks,
         const int r = (lane >> 2) & 3, g = lane >> 4;
         const int block = (base >> 4) ^ ((r | (g << 2)) & (RB / 32 - 1));
         const char* at = tile + (ks * 32 + g * 8 + r) * RB + block * 32 + (lane & 3) * 8;
-        typedef __attribute__((address_space(3))) Short4 LdsShort4;
         union { Word4 w; Short4 s[2]; } u;
-        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)at);
-        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(at + 4 * RB));
+        u.s[0] = read_transposed((LdsShort4*)at);
+        u.s[1] = read_transposed((LdsShort4*)(at + 4 * RB));
         return u.w;
     } else {
         constexpr int RB = BI * 4;
@@ -192,23 +199,25 @@ __device__ __forceinline__ void tile_of(u32 id, u32 tm, u32 tn, u32& m, u32& n)
     n = in / rows;
 }
 
-// One step's products out of shared memory.
-template <class T, class TL, Layout LA, Layout LB>
-__device__ __forceinline__ void step_products(Float4 (&acc)[TL::FN][TL::FM], const char* ta, const char* tb, int wm, int wn, int lane)
+// Waits until no more than VM loads to shared memory are under way.
+template <int VM>
+__device__ __forceinline__ void wait_loads()
 {
-    constexpr int FM = TL::FM, FN = TL::FN;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-        Word4 fm[FM], fn[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) fn[j] = read_square<T, LB, TL::BN>(tb, (wn * FN + j) * 16, ks, lane);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) fm[i] = read_square<T, LA, TL::BM>(ta, (wm * FM + i) * 16, ks, lane);
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) square_product<T>(acc[j][i], fn[j], fm[i]);
-    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | (15 << 8) | ((VM >> 4) << 14));
+    asm volatile("" ::: "memory");
+}
+
+// Waits until no more than VM loads to shared memory and LGKM reads of it are under way, then for the other waves.  Nothing moves across.
+template <int VM, int LGKM>
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | (LGKM << 8) | ((VM >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
 }
 
 // The sums of the tile at (m0, n0) over `segments` matrices of each operand one after the other (PAIRED > 0: over one, B's
@@ -217,7 +226,8 @@ template <class T, class TL, Layout LA, Layout LB, int PAIRED, bool DIRECT>
 __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char* lds, const Operand& a, const Operand& b, int segments, i64 m0, i64 n0)
 {
     constexpr int FM = TL::FM, FN = TL::FN, NT = TL::NT, BM = TL::BM, BN = TL::BN, BK = TL::BK;
-    constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;                        // 16-byte positions a thread brings of each operand
+    constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;                        // 16-byte positions a thread brings
+    static_assert(PA > 0 && PB > 0, "every thread brings something of both operands");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
@@ -226,92 +236,128 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         for (int i = 0; i < FM; ++i) acc[j][i] = Float4{0, 0, 0, 0};
 
     const i64 depth = a.depth > b.depth ? a.depth : b.depth;
-    const int steps = (int)((depth + BK - 1) / BK), total = steps * segments;
-    if (total == 0) return;
+    const int steps = (int)((depth + BK - 1) / BK);
     Word4 ra[PA], rb[PB];
-    auto fetch = [&](int s) {
-        const int seg = s >= steps;
-        const i64 k0 = (i64)(s - seg * steps) * BK;
+    auto fetch = [&](int seg, int s) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = fetch_chunk<T, LA, BM, 0, DIRECT>(a, seg, m0, k0, i * NT + tid);
+        for (int i = 0; i < PA; ++i) ra[i] = fetch_chunk<T, LA, BM, 0, DIRECT>(a, seg, m0, (i64)s * BK, i * NT + tid);
 #pragma unroll
-        for (int i = 0; i < PB; ++i) rb[i] = fetch_chunk<T, LB, BN, PAIRED, DIRECT>(b, seg, n0, k0, i * NT + tid);
+        for (int i = 0; i < PB; ++i) rb[i] = fetch_chunk<T, LB, BN, PAIRED, DIRECT>(b, seg, n0, (i64)s * BK, i * NT + tid);
     };
-    auto put = [&](int s) {
-        char* at = lds + (s & 1) * (BM + BN) * 128;
+    auto place_a = [&](int slot) { return lds + slot * TL::SLOT_A; };
+    auto place_b = [&](int slot) { return lds + 3 * TL::SLOT_A + slot * TL::SLOT_B; };
+    auto put = [&](int slot) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) *reinterpret_cast<Word4*>(at + (i * NT + tid) * 16) = ra[i];
+        for (int i = 0; i < PA; ++i) *reinterpret_cast<Word4*>(place_a(slot) + (i * NT + tid) * 16) = ra[i];
 #pragma unroll
-        for (int i = 0; i < PB; ++i) *reinterpret_cast<Word4*>(at + BM * 128 + (i * NT + tid) * 16) = rb[i];
+        for (int i = 0; i < PB; ++i) *reinterpret_cast<Word4*>(place_b(slot) + (i * NT + tid) * 16) = rb[i];
     };
-    if constexpr (DIRECT) {
+    auto square_a = [&](int slot, int i, int ks) { return read_square<T, LA, BM>(place_a(slot), (wm * FM + i) * 16, ks, lane); };
+    auto square_b = [&](int slot, int j, int ks) { return read_square<T, LB, BN>(place_b(slot), (wn * FN + j) * 16, ks, lane); };
+    auto products = [&](int slot) {
+#pragma unroll 1
+        for (int ks = 0; ks < 2; ++ks) {
+            Word4 fn[FN];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fn[j] = square_b(slot, j, ks);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const Word4 fm = square_a(slot, i, ks);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) square_product<T>(acc[j][i], fn[j], fm);
+            }
+        }
+    };
+    if constexpr (!DIRECT) {
+        const int total = steps * segments;
+        if (total == 0) return;
+        fetch(0, 0);
+        put(0);
+        __syncthreads();
+        for (int s = 0; s < total; ++s) {
+            const int next = s + 1 >= steps ? s + 1 - steps : s + 1;
+            if (s + 1 < total) fetch(s + 1 >= steps, next);
+            products(s & 1);
+            if (s + 1 < total) put(~s & 1);                                  // what nothing reads any more
+            __syncthreads();
+        }
+        return;
+    }
+    // Whole steps of all segments first, then the parts of a step that are left.
+    const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK), total = whole * segments;
+    if (total > 0) {
         DirectTile<T, LA, BM, NT, 0> da;
         DirectTile<T, LB, BN, NT, PAIRED> db;
         da.init(a, m0);
         db.init(b, n0);
-        const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK);   // steps of which nothing lies outside; the last may be another
-        auto bring = [&](int s) {
-            const int seg = s >= steps, k = s - seg * steps;
-            if (k < whole) {
-                char* at = lds + (s & 1) * (BM + BN) * 128;
-                da.bring(at, seg, k, wave);
-                db.bring(at + BM * 128, seg, k, wave);
-            } else {
-                fetch(s);
-                put(s);
-            }
+        auto bring = [&](int s, int slot_a, int slot_b) {
+            const int seg = s >= whole, k = s - seg * whole;
+            da.bring(place_a(slot_a), seg, k, wave);
+            db.bring(place_b(slot_b), seg, k, wave);
         };
-        bring(0);
-        if (total > 1) bring(1);
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
+        constexpr int LOADS = PA + PB;
+        bring(0, 0, 0);
+        if (total > 1) {
+            bring(1, 1, 1);
+            wait_and_meet<LOADS, 15>();
+        } else {
+            wait_and_meet<0, 15>();
+        }
         // A step is 2 FM groups, one square row of A times all of B's squares each.  A's squares are read AHEAD groups before their
-        // products, B's of the other half of the step as early; when the last read of a step is through, its half of the shared memory is
-        // given to the step after the next, and the last groups read the next step's first squares.  So products never wait for a
-        // read that was just issued, and a load has almost a whole step to arrive.
-        constexpr int GROUPS = 2 * FM, AHEAD = 4;
-        static_assert(FM % AHEAD == 0 && FN <= AHEAD, "the squares of a step are read before its last groups");
+        // products; B's of the second half at once, and the last groups read the next step's first squares: products never wait for a
+        // read that was just issued.
+        constexpr int GROUPS = 2 * FM, AHEAD = 4, SEND = FN / 2 + 1;
+        static_assert(FM % AHEAD == 0 && FN == AHEAD && SEND < GROUPS - AHEAD, "the squares of a step are read before its last groups");
         Word4 fm[GROUPS], fn[2][FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fn[0][j] = read_square<T, LB, BN>(lds + BM * 128, (wn * FN + j) * 16, 0, lane);
+        for (int j = 0; j < FN; ++j) fn[0][j] = square_b(0, j, 0);
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) fm[i] = read_square<T, LA, BM>(lds, (wm * FM + i) * 16, 0, lane);
+        for (int i = 0; i < AHEAD; ++i) fm[i] = square_a(0, i, 0);
+        int sa = 0;                                                          // s % 3
         for (int s = 0; s < total; ++s) {
-            const char* ta = lds + (s & 1) * (BM + BN) * 128;
-            const char* next = lds + (~s & 1) * (BM + BN) * 128;
+            const int sa1 = sa == 2 ? 0 : sa + 1, sa2 = sa == 0 ? 2 : sa - 1, sb = s & 1;
 #pragma unroll
             for (int q = 0; q < GROUPS; ++q) {
-                if (q == GROUPS - AHEAD) {
-                    __builtin_amdgcn_s_waitcnt(0);
-                    __syncthreads();
-                    if (s + 2 < total) bring(s + 2);
+                if (q == SEND) {                                             // B has been read by all: a group and its read of A later
+                    wait_and_meet<63, 1>();
+                    if (s + 2 < total) bring(s + 2, sa2, sb);
+                }
+                if (q == GROUPS - AHEAD) {                                   // the next step has arrived; the one behind it is on its way
+                    if (s + 2 < total) wait_loads<LOADS>();
+                    else wait_loads<0>();
+                    wait_and_meet<63, 15>();
                 }
                 if (q < GROUPS - AHEAD) {
+                    if (q < FN / 2) {
+                        fn[1][2 * q] = square_b(sb, 2 * q, 1);
+                        fn[1][2 * q + 1] = square_b(sb, 2 * q + 1, 1);
+                    }
                     const int r = q + AHEAD;
-                    fm[r] = read_square<T, LA, BM>(ta, (wm * FM + r % FM) * 16, r / FM, lane);
-                    if (q < FN) fn[1][q] = read_square<T, LB, BN>(ta + BM * 128, (wn * FN + q) * 16, 1, lane);
-                } else {                                                     // (behind the last step: read, and not used)
-                    const int r = q - (GROUPS - AHEAD);
-                    fm[r] = read_square<T, LA, BM>(next, (wm * FM + r) * 16, 0, lane);
-                    if (r < FN) fn[0][r] = read_square<T, LB, BN>(next + BM * 128, (wn * FN + r) * 16, 0, lane);
+                    fm[r] = square_a(sa, r % FM, r / FM);
+                } else {                                                     // all of B's before the first of A's: the first products need them
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {                            // (behind the last step: read, and not used)
+                        const int r = 2 * (q - (GROUPS - AHEAD)) + e;
+                        if (r < FN) fn[0][r] = square_b(sb ^ 1, r, 0);
+                        else fm[r - FN] = square_a(sa1, r - FN, 0);
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < FN; ++j) square_product<T>(acc[j][q % FM], fn[q / FM][j], fm[q]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        }
-    } else {
-        fetch(0);
-        put(0);
-        __syncthreads();
-        for (int s = 0; s < total; ++s) {
-            const char* ta = lds + (s & 1) * (BM + BN) * 128;
-            if (s + 1 < total) fetch(s + 1);
-            step_products<T, TL, LA, LB>(acc, ta, ta + BM * 128, wm, wn, lane);
-            if (s + 1 < total) put(s + 1);                                   // the half that nothing reads any more
-            __syncthreads();
+            sa = sa1;
         }
     }
+    if (whole < steps)
+#pragma unroll 1
+        for (int seg = 0; seg < segments; ++seg) {
+            fetch(seg, whole);
+            __syncthreads();                                                 // everything before has been read
+            put(0);
+            __syncthreads();
+            products(0);
+        }
 }
 
 // Four neighbouring results of one row, rounded once; `have` of them exist.  `wide`: the row's stride and address let four
