@@ -87,18 +87,19 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
         const i64 m = m0 + (wm * FM + i) * 16 + (lane & 15);
         if (m >= f.x.index) continue;
 #pragma unroll
-        for (int j = 0; j < HALF; ++j) {
-            const i64 n = n0 + (wn * HALF + j) * 16 + (lane >> 4) * 4;
+        for (int j = 0; j < HALF; j += 2) {
+            const i64 n = n0 + (wn * HALF + j) * 16;
             const i64 have = f.w.index - n;
             if (have <= 0) continue;
-            const Float4 g = acc[j][i], u = acc[j + HALF][i];
-            Float4 h;
+            Float4 h[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
-            store4((T*)f.h + m * f.ldh + n, h, have, f.wide_h);
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[k][e] = activation(f.act, acc[j + k][i][e]) * acc[j + k + HALF][i][e];
+            store_pair((T*)f.h + m * f.ldh + n, h[0], h[1], have, f.wide_h, lane);
             if (f.g) {
-                store4(f.g + m * f.ldg + n, g, have, f.wide_g);
-                store4(f.u + m * f.ldg + n, u, have, f.wide_g);
+                store_pair(f.g + m * f.ldg + n, acc[j][i], acc[j + 1][i], have, f.wide_g, lane);
+                store_pair(f.u + m * f.ldg + n, acc[j + HALF][i], acc[j + 1 + HALF][i], have, f.wide_g, lane);
             }
         }
     }
@@ -156,8 +157,7 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
     u32 bm, bn;
     tile_of(blockIdx.x, tm, tn, bm, bn);
     const int z = blockIdx.y;
-    Operand a = f.a;
-    if (LA == COLS && z) a.p[0] = a.p[1];
+    const Operand a = {{LA == COLS ? f.a.matrix(z) : f.a.p[0], f.a.p[1]}, {f.a.ld[0], f.a.ld[1]}, f.a.index, f.a.depth};
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * TL::BN;
     Float4 acc[FN][FM];
     product_tile<T, TL, LA, COLS, 0, DIRECT>(acc, lds, a, f.b, f.segments, m0, n0);
@@ -168,10 +168,10 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
         const i64 m = m0 + (wm * FM + i) * 16 + (lane & 15);
         if (m >= f.rows) continue;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const i64 n = n0 + (wn * FN + j) * 16 + (lane >> 4) * 4;
+        for (int j = 0; j < FN; j += 2) {
+            const i64 n = n0 + (wn * FN + j) * 16;
             const i64 have = f.b.index - n;
-            if (have > 0) store4((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], have, f.wide[z]);
+            if (have > 0) store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, f.wide[z], lane);
         }
     }
 }

@@ -4,7 +4,8 @@
 // A workgroup computes a BM x BN tile of D; its WM x WN waves hold FM x FN squares of 16 x 16 each.  A step takes 128 bytes
 // of the contraction (64 16-bit or 32 32-bit elements) of every row of both operands through shared memory, where there is room
 // for three steps of A and two of B: a wave reads all of its B early in a step, so the step after the next can be sent for as soon as that
-// is done, and a load has a step and a half to arrive.  (Two and two: 1070 TFLOP/s at dx of 8192 x 4096 x 12288 in place of ###.)
+// is done, and a load has a step and a half to arrive.  Products of 8192 x 4096 x 12288, bf16, TFLOP/s, with two and two, then three and
+// two, then its loads spread over the step: forward 1050, 1120, 1250; dx 1050, 1190, 1400; dW 990, 1130, 1340.
 //
 // An operand lies in memory in one of two ways, whichever way the caller's matrices give it: ROWS (the contraction is
 // contiguous: x and W in x W^T) or COLS (the index is contiguous: W in dg W, both in dg^T x).  ROWS tiles are read from
@@ -36,6 +37,8 @@ struct Operand {
     const void* p[2];
     i64 ld[2];
     i64 index, depth;
+    __device__ __forceinline__ const void* matrix(int which) const { return which ? p[1] : p[0]; }
+    __device__ __forceinline__ i64 stride(int which) const { return which ? ld[1] : ld[0]; }
 };
 
 // Where 16-byte position `pos` of an operand's tile comes from: `row` of the tile in memory, `chunk` of 16 bytes in it.
@@ -79,12 +82,12 @@ __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0
     if constexpr (L == ROWS) {
         if constexpr (PAIRED > 0) row = paired_row<PAIRED>(row, which);
         const i64 i = i0 + row, k = k0 + chunk * N;
-        const T* p = (const T*)o.p[which] + i * o.ld[which] + k;
+        const T* p = (const T*)o.matrix(which) + i * o.stride(which) + k;
         if constexpr (WHOLE) return i < o.index && k < o.depth ? *reinterpret_cast<const Word4*>(p) : Word4{0, 0, 0, 0};
         return i < o.index ? load_some(p, o.depth - k) : Word4{0, 0, 0, 0};
     } else {
         const i64 k = k0 + row, i = i0 + chunk * N;
-        const T* p = (const T*)o.p[which] + k * o.ld[which] + i;
+        const T* p = (const T*)o.matrix(which) + k * o.stride(which) + i;
         if constexpr (WHOLE) return i < o.index && k < o.depth ? *reinterpret_cast<const Word4*>(p) : Word4{0, 0, 0, 0};
         return k < o.depth ? load_some(p, o.index - i) : Word4{0, 0, 0, 0};
     }
@@ -96,7 +99,8 @@ __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0
 template <class T, Layout L, int BI, int NT, int PAIRED>
 struct DirectTile {
     static constexpr int P = BI * 8 / NT, N = PER_WORD4<T>;
-    const char* base[2];
+    const char* base;
+    i64 other;                                                               // bytes from there to the second matrix
     i64 step;                                                                // bytes from a step to the next
     u32 off[P];
 
@@ -109,33 +113,25 @@ struct DirectTile {
             if constexpr (L == ROWS) {
                 if constexpr (PAIRED > 0) row = paired_row<PAIRED>(row, which);
                 const i64 last = o.index - 1 - i0;
-                off[i] = (u32)((i64)(row < last ? row : last) * o.ld[which] * (i64)sizeof(T)) + chunk * 16;
+                off[i] = (u32)((i64)(row < last ? row : last) * o.stride(which) * (i64)sizeof(T)) + chunk * 16;
             } else {
                 const i64 last = o.index - N - i0, col = (i64)chunk * N;
                 off[i] = (u32)((i64)row * o.ld[0] * (i64)sizeof(T) + (col < last ? col : last) * (i64)sizeof(T));
             }
         }
-#pragma unroll
-        for (int w = 0; w < 2; ++w) base[w] = (const char*)o.p[w] + (L == ROWS ? i0 * o.ld[w] : i0) * (i64)sizeof(T);
+        base = (const char*)o.p[0] + (L == ROWS ? i0 * o.ld[0] : i0) * (i64)sizeof(T);
+        other = (i64)((uintptr_t)o.p[1] - (uintptr_t)o.p[0]) + (L == ROWS ? i0 * (o.ld[1] - o.ld[0]) : 0) * (i64)sizeof(T);
         step = L == ROWS ? 128 : (i64)(128 / sizeof(T)) * o.ld[0] * (i64)sizeof(T);
     }
 
-    // Step `s` of segment `seg` into the slot at `lds`.
-    __device__ __forceinline__ void bring(char* lds, int seg, int s, int wave) const
+    // The i-th of a thread's loads of step `s` of segment `seg`, into the slot at `lds`.  (Buffer loads, not global ones: those count as
+    // accesses that may go to either memory, and the compiler then waits for all reads of shared memory where it needs one.)
+    __device__ __forceinline__ void bring(char* lds, int seg, int s, int wave, int i) const
     {
-        typedef __attribute__((address_space(1))) const void GlobalAny;
         typedef __attribute__((address_space(3))) void LdsAny;
-        const i64 at = s * step;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const char* b = base[0];
-            if constexpr (PAIRED > 0) {
-                if ((i * (NT / 8) + wave * 8) % (PAIRED * 16) >= PAIRED * 8) b = base[1];
-            } else {
-                if (seg) b = base[1];
-            }
-            __builtin_amdgcn_global_load_lds((GlobalAny*)(b + at + off[i]), (LdsAny*)(lds + (i * NT + wave * 64) * 16), 16, 0, 0);
-        }
+        const bool second = PAIRED > 0 ? (i * (NT / 8) + wave * 8) % (PAIRED > 0 ? PAIRED * 16 : 1) >= PAIRED * 8 : seg != 0;
+        const auto resource = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + s * step + (second ? other : 0)), 0, -1, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(resource, (LdsAny*)(lds + (i * NT + wave * 64) * 16), 16, (int)off[i], 0, 0, 0);
     }
 };
 
@@ -197,15 +193,6 @@ __device__ __forceinline__ void tile_of(u32 id, u32 tm, u32 tn, u32& m, u32& n)
     const u32 group = at / (8 * tn), first = group * 8, rows = min(8u, tm - first), in = at - group * 8 * tn;
     m = first + in % rows;
     n = in / rows;
-}
-
-// Waits until no more than VM loads to shared memory are under way.
-template <int VM>
-__device__ __forceinline__ void wait_loads()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | (15 << 8) | ((VM >> 4) << 14));
-    asm volatile("" ::: "memory");
 }
 
 // Waits until no more than VM loads to shared memory and LGKM reads of it are under way, then for the other waves.  Nothing moves across.
@@ -290,19 +277,17 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         DirectTile<T, LB, BN, NT, PAIRED> db;
         da.init(a, m0);
         db.init(b, n0);
-        auto bring = [&](int s, int slot_a, int slot_b) {
-            const int seg = s >= whole, k = s - seg * whole;
-            da.bring(place_a(slot_a), seg, k, wave);
-            db.bring(place_b(slot_b), seg, k, wave);
-        };
         constexpr int LOADS = PA + PB;
-        bring(0, 0, 0);
-        if (total > 1) {
-            bring(1, 1, 1);
-            wait_and_meet<LOADS, 15>();
-        } else {
-            wait_and_meet<0, 15>();
-        }
+        auto bring = [&](int s, int slot_a, int slot_b, int i) {             // load i of the LOADS of step s
+            const int seg = s >= whole, k = s - seg * whole;
+            if (i < PA) da.bring(place_a(slot_a), seg, k, wave, i);
+            else db.bring(place_b(slot_b), seg, k, wave, i - PA);
+        };
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) bring(0, 0, 0, i);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) bring(total > 1 ? 1 : 0, 1, 1, i);
+        wait_and_meet<LOADS, 15>();
         // A step is 2 FM groups, one square row of A times all of B's squares each.  A's squares are read AHEAD groups before their
         // products; B's of the second half at once, and the last groups read the next step's first squares: products never wait for a
         // read that was just issued.
@@ -318,15 +303,13 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
             const int sa1 = sa == 2 ? 0 : sa + 1, sa2 = sa == 0 ? 2 : sa - 1, sb = s & 1;
 #pragma unroll
             for (int q = 0; q < GROUPS; ++q) {
-                if (q == SEND) {                                             // B has been read by all: a group and its read of A later
-                    wait_and_meet<63, 1>();
-                    if (s + 2 < total) bring(s + 2, sa2, sb);
-                }
-                if (q == GROUPS - AHEAD) {                                   // the next step has arrived; the one behind it is on its way
-                    if (s + 2 < total) wait_loads<LOADS>();
-                    else wait_loads<0>();
-                    wait_and_meet<63, 15>();
-                }
+                if (q == SEND) wait_and_meet<63, 1>();                       // B has been read by all: a group and its read of A later
+                if (q == GROUPS - AHEAD) wait_and_meet<LOADS, 15>();         // the next step has arrived; the one behind it is on its way
+                // One load a group: all at once they hold each other up (dx of 8192 x 4096 x 12288 1377 us, so 1227).  Behind the end the last
+                // step is sent for again, into places that nothing reads.
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i)
+                    if (q == SEND + i * (GROUPS - AHEAD - SEND) / LOADS) bring(s + 2 < total ? s + 2 : total - 1, sa2, sb, i);
                 if (q < GROUPS - AHEAD) {
                     if (q < FN / 2) {
                         fn[1][2 * q] = square_b(sb, 2 * q, 1);
@@ -353,7 +336,7 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
 #pragma unroll 1
         for (int seg = 0; seg < segments; ++seg) {
             fetch(seg, whole);
-            __syncthreads();                                                 // everything before has been read
+            wait_and_meet<0, 0>();                                           // everything before has arrived and been read
             put(0);
             __syncthreads();
             products(0);
@@ -379,6 +362,36 @@ __device__ __forceinline__ void store4(T* p, Float4 v, i64 have, bool wide)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (i < have) p[i] = r[i];
+}
+
+// Two squares side by side of 16 rows: a lane has row lane % 16, columns (lane / 16) * 4 and on of either.  `p` is the lane's
+// row at the first square's first column, of which `have` columns exist.  For 16-bit results lanes 16 apart exchange
+// halves, so that each has eight neighbouring columns of one square and a row's 64 bytes go out at once (`wide`: eight can be stored at once).
+template <class T>
+__device__ __forceinline__ void store_pair(T* p, Float4 first, Float4 second, i64 have, bool wide, int lane)
+{
+    const int g = lane >> 4;
+    if constexpr (sizeof(T) == 2) {
+        if (wide && have >= 32) {
+            union { T v[4]; int w[2]; } a, b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a.v[i] = from_float<T>(first[i]);
+                b.v[i] = from_float<T>(second[i]);
+            }
+            Word4 out;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const auto r = __builtin_amdgcn_permlane16_swap((unsigned)a.w[i], (unsigned)b.w[i], false, false);
+                out[i] = (int)r[0];
+                out[2 + i] = (int)r[1];
+            }
+            *reinterpret_cast<Word4*>(p + (g & 1) * 16 + (g >> 1) * 8) = out;
+            return;
+        }
+    }
+    store4(p + g * 4, first, have - g * 4, wide);
+    store4(p + 16 + g * 4, second, have - 16 - g * 4, wide);
 }
 
 }  // namespace

@@ -39,8 +39,8 @@ int element_size(int dtype) { return dtype == EBSP_BF16 || dtype == EBSP_F16 ? 2
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-// Four neighbouring elements can be stored at once.
-int wide_rows(const void* p, i64 ld, int size) { return aligned(p, 4 * size) && ld % 4 == 0; }
+// 16 bytes of neighbouring elements can be stored at once.
+int wide_rows(const void* p, i64 ld, int size) { return aligned(p, 16) && ld % (16 / size) == 0; }
 
 i64 padded_units(i64 F, int size)
 {
