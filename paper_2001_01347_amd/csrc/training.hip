@@ -228,12 +228,22 @@ int run_distill(Distill& d, int dtype, bool grad, void* workspace, size_t worksp
     return dtype == EBSP_BF16 ? distill_loss<__bf16>(d, grad, st) : dtype == EBSP_F16 ? distill_loss<_Float16>(d, grad, st) : distill_loss<float>(d, grad, st);
 }
 
+template <class T, int SPLIT>
+int merge_split(const Merge& g, hipStream_t st)
+{
+    const i64 per = (SPLIT == 1 ? 256 : 64) * PER_WORD4<T>;
+    LAUNCH_LDS((tr_merge_kernel<T, SPLIT>), dim3((unsigned)((g.n + per - 1) / per)), dim3(SPLIT == 1 ? 256 : SPLIT * 64), g.P * sizeof(Share), g);
+    return EBSP_OK;
+}
+
+// The workers are split over a workgroup's waves where the chunks alone make too few waves to keep memory busy.
 template <class T>
 int merge(const Merge& g, hipStream_t st)
 {
-    const i64 blocks = (g.n + 256 * PER_WORD4<T> - 1) / (256 * PER_WORD4<T>);
-    LAUNCH_LDS(tr_merge_kernel<T>, dim3((unsigned)blocks), dim3(256), g.P * sizeof(Share), g);
-    return EBSP_OK;
+    const i64 waves = (g.n + 64 * PER_WORD4<T> - 1) / (64 * PER_WORD4<T>);
+    if (waves < 1024 && g.P >= 64) return merge_split<T, 16>(g, st);
+    if (waves < 4096 && g.P >= 16) return merge_split<T, 4>(g, st);
+    return merge_split<T, 1>(g, st);
 }
 
 }  // namespace
