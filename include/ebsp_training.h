@@ -159,7 +159,8 @@ int ebsp_distill_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V,
  *   velocity     in  [n] float;   velocity_out out [n] float, may be velocity
  *                    itself; both NULL: no momentum
  *   pull         out [n] of type pull_dtype: w' rounded, what the workers fetch; or NULL
- * Sums run in the order of the workers in 32 bits: results do not vary.  P is 1 to
+ * Sums are held in 32 bits and run in an order that P and n fix: results do not
+ * vary.  P is 1 to
  * EBSP_MERGE_WORKERS_MAX, n below 2^34.  n == 0 is a valid no-op.
  */
 int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, int32_t dtype, const int32_t* iters,

@@ -53,14 +53,14 @@ __device__ __forceinline__ int list_shares(const Merge& g, Share* list, int* sha
     return *shared;
 }
 
-// The sum of worker list[k]'s share times its push for k from k0 up to k1, for the N elements at `base` (those behind `have` read as zero).  AHEAD rows
-// are under way at a time; where a row is, every lane knows alike.
+// The sum of worker list[k]'s share times its push for k from k0 up to k1, for the N elements from `at` on (WHOLE; otherwise those behind `have` read as
+// zero).  AHEAD rows are under way at a time; where a row is, every lane knows alike.
 template <class T, bool WHOLE>
-__device__ __forceinline__ void add_pushes(float (&avg)[PER_WORD4<T>], const Merge& g, const T* base, const Share* list, int k0, int k1, i64 have)
+__device__ __forceinline__ void add_pushes(float (&avg)[PER_WORD4<T>], const Merge& g, const Share* list, int k0, int k1, i64 at, i64 have)
 {
     constexpr int N = PER_WORD4<T>, AHEAD = 8;
     auto row = [&](int k) {
-        const T* p = base + (i64)__builtin_amdgcn_readfirstlane(list[k].worker) * g.stride;
+        const T* p = (const T*)g.pushes + (i64)__builtin_amdgcn_readfirstlane(list[k].worker) * g.stride + at;
         return WHOLE ? load_loose(p) : load_some(p, have);
     };
     auto add = [&](Word4 raw, int k) {
@@ -148,8 +148,9 @@ __device__ __forceinline__ void apply_step(const Merge& g, float (&avg)[N], i64 
     }
 }
 
-// 16 bytes of a row a thread; SPLIT > 1: each wave of a workgroup takes a part of the workers for the same 64 chunks, and the first adds the
-// parts up in their order.
+// 16 bytes of a row a lane.  SPLIT > 1: each wave of a workgroup takes a part of the workers for the same 64 chunks, and the first adds the parts up in
+// their order.  The lane of the last, partial chunk reads the last 16 bytes of the rows and moves its sums afterwards: element by element
+// that one lane would take longer than all others together (435 in place of 200 us at 1024 workers x 524309 weights).
 template <class T, int SPLIT>
 __global__ void __launch_bounds__(SPLIT == 1 ? 256 : SPLIT * 64) tr_merge_kernel(Merge g)
 {
@@ -157,29 +158,37 @@ __global__ void __launch_bounds__(SPLIT == 1 ? 256 : SPLIT * 64) tr_merge_kernel
     __shared__ int shared;
     constexpr int N = PER_WORD4<T>, NT = SPLIT == 1 ? 256 : SPLIT * 64;
     const int count = list_shares<NT>(g, list, &shared);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const i64 at = SPLIT == 1 ? ((i64)blockIdx.x * 256 + threadIdx.x) * N : ((i64)blockIdx.x * 64 + (threadIdx.x & 63)) * N;
-    const i64 have = g.n - at;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const i64 at = ((i64)blockIdx.x * (SPLIT == 1 ? NT : 64) + (SPLIT == 1 ? (int)threadIdx.x : lane)) * N, have = g.n - at;
     float avg[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) avg[i] = 0.f;
     const int k0 = SPLIT == 1 ? 0 : wave * count / SPLIT, k1 = SPLIT == 1 ? count : (wave + 1) * count / SPLIT;
-    const T* base = (const T*)g.pushes + at;
-    if (have >= N) add_pushes<T, true>(avg, g, base, list, k0, k1, have);
-    else if (have > 0) add_pushes<T, false>(avg, g, base, list, k0, k1, have);
+    if (g.n >= N) {
+        if (have > 0) add_pushes<T, true>(avg, g, list, k0, k1, have < N ? g.n - N : at, N);
+    } else if (have > 0) {
+        add_pushes<T, false>(avg, g, list, k0, k1, at, have);
+    }
     if constexpr (SPLIT > 1) {
         __shared__ float part[SPLIT - 1][N][64];
         if (wave > 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) part[wave - 1][i][threadIdx.x & 63] = avg[i];
+            for (int i = 0; i < N; ++i) part[wave - 1][i][lane] = avg[i];
         __syncthreads();
         if (wave > 0) return;
         for (int p = 0; p < SPLIT - 1; ++p)
 #pragma unroll
-            for (int i = 0; i < N; ++i) avg[i] += part[p][i][threadIdx.x];
+            for (int i = 0; i < N; ++i) avg[i] += part[p][i][lane];
     }
-    if (have >= N) apply_step<N, true>(g, avg, at, have, count > 0);
-    else if (have > 0) apply_step<N, false>(g, avg, at, have, count > 0);
+    if (have >= N) {
+        apply_step<N, true>(g, avg, at, have, count > 0);
+    } else if (have > 0) {
+        if (g.n >= N)
+            for (int moves = N - (int)have; moves > 0; --moves)
+#pragma unroll
+                for (int i = 0; i < N - 1; ++i) avg[i] = avg[i + 1];
+        apply_step<N, false>(g, avg, at, have, count > 0);
+    }
 }
 
 }  // namespace
