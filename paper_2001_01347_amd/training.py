@@ -56,28 +56,40 @@ def load() -> ctypes.CDLL:
     return _lib
 
 
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)         # the same, without an object around it
+
+
 def _call(name: str, dev: torch.device, *args) -> None:
-    with torch.cuda.device(dev):
-        rc = getattr(load(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+    fn = getattr(_lib or load(), name)
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(*args, _current_stream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _current_stream(dev.index))
     if rc != zipline.EBSP_OK:
         raise ZipLineError(f"{name} failed ({rc}): {zipline.ebsp_last_error()}")
 
 
 def _dtype(name: str, t: torch.Tensor) -> int:
-    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
+    code = DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None:
         raise ValueError(f"{name} must be a bfloat16, float16 or float32 tensor")
-    return DTYPES[t.dtype]
+    return code
 
 
-def _rows(name: str, t: torch.Tensor, dev: torch.device, dtype: torch.dtype, shape) -> int:
+def _rows(name: str, t: torch.Tensor, dev: torch.device, dtype: torch.dtype, shape: Tuple[int, int]) -> int:
     """Check a matrix operand; the distance between its rows, in elements."""
-    if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {dev}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {shape} on {dev}")
+    rows, length = shape
+    if t.is_contiguous():
+        return length
+    if length > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have unit stride along its rows")
-    if t.shape[0] <= 1 or t.shape[1] == 0:
-        return t.shape[1]
-    if t.stride(0) < t.shape[1]:
+    if rows <= 1 or length == 0:
+        return length
+    if t.stride(0) < length:
         raise ValueError(f"the rows of {name} overlap (an expanded tensor: make it contiguous)")
     return t.stride(0)
 
@@ -85,7 +97,7 @@ def _rows(name: str, t: torch.Tensor, dev: torch.device, dtype: torch.dtype, sha
 def _matrix(name: str, t: torch.Tensor) -> Tuple[int, int]:
     if not isinstance(t, torch.Tensor) or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor with two dimensions")
-    return int(t.shape[0]), int(t.shape[1])
+    return tuple(t.shape)
 
 
 def _output(name: str, t: Optional[torch.Tensor], dev, dtype, shape) -> torch.Tensor:
