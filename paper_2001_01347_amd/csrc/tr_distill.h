@@ -78,7 +78,7 @@ __device__ __forceinline__ T block_reduce(T v, T* shared, F&& join)
 // A row's entries in shared memory.
 struct Entries {
     int index[TOP_MAX];                          // -1: padding
-    float q[TOP_MAX], s[TOP_MAX];                // the teacher's weight, the student's logit
+    float q[TOP_MAX], s[TOP_MAX];                // the teacher's logit, later its weight; the student's logit
     Sums sums[16];
     float scalar[16];
 };
@@ -87,6 +87,7 @@ struct Row {
     i64 n;
     int label;                                   // -1: none
     bool any;                                    // some entry has weight
+    float label_logit;
 };
 
 template <class T>
@@ -96,17 +97,19 @@ __device__ __forceinline__ float top_logit(const Distill& d, i64 at)
          : d.top_type == EBSP_F16 ? to_float(((const _Float16*)d.top_logit)[at]) : to_float(((const __bf16*)d.top_logit)[at]);
 }
 
-// Entries and label of row n, checked: what does not lie in the vocabulary is left out and flagged.  The student's logits are
-// fetched for those from `v0` up to `v1`.
+// The larger of two, or the one that is no number: a NaN among a row's entries comes through, its results are not those of the others.
+__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
+
+// Entries and label of row n, checked: what does not lie in the vocabulary is left out and counted as bad.  The student's logits are
+// fetched for those from `v0` up to `v1`.  Each thread keeps to its own entries until the next barrier; `top` is the largest of them.
 template <int NT, class T>
-__device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1, Entries& e, bool flag)
+__device__ __forceinline__ Row read_entries(const Distill& d, i64 n, i64 v0, i64 v1, Entries& e, float& top, bool& bad)
 {
     Row row;
     row.n = n;
-    bool bad = false;
-    const float ct = LOG2E / d.temperature;
+    bad = false;
+    top = -INFINITY;
     const T* s = (const T*)d.logits + n * d.ld;
-    float tm = -INFINITY;
     for (int k = threadIdx.x; k < d.top; k += NT) {
         const i64 at = n * d.ldt + k;
         const i64 i = d.index_wide ? ((const i64*)d.top_index)[at] : (i64)((const int*)d.top_index)[at];
@@ -116,7 +119,7 @@ __device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1,
         e.index[k] = in ? (int)i : -1;
         e.q[k] = t;
         e.s[k] = in && i >= v0 && i < v1 ? to_float(s[i]) : 0.f;
-        tm = t > tm || t != t ? t : tm;
+        top = larger(t, top);
     }
     row.label = -1;
     if (d.labels) {
@@ -124,22 +127,46 @@ __device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1,
         bad |= l >= d.V;
         if (l >= 0 && l < d.V && d.ce != 0.f) row.label = (int)l;
     }
-    if (flag) {
-        const float any_bad = block_reduce<NT>(bad ? 1.f : 0.f, e.scalar, [](float a, float b) { return fmaxf(a, b); });
-        if (threadIdx.x == 0 && d.status) d.status[n] = any_bad > 0.f ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
-    }
-    // a NaN among the entries comes through: the row's results are NaN, not those of the other entries
-    tm = block_reduce<NT>(tm, e.scalar, [](float a, float b) { return a > b || a != a ? a : b; });
-    row.any = tm != -INFINITY && d.kl != 0.f;
+    row.label_logit = row.label >= v0 && row.label < v1 ? to_float(s[row.label]) : 0.f;
+    return row;
+}
+
+// The entries' weights, not yet divided by their sum, which is returned for the thread's own.
+template <int NT>
+__device__ __forceinline__ float weigh_entries(const Distill& d, const Row& row, Entries& e, float top)
+{
     float sum = 0.f;
     for (int k = threadIdx.x; k < d.top; k += NT) {
-        const float w = row.any && e.index[k] >= 0 ? exp2_fast((e.q[k] - tm) * ct) : 0.f;
+        const float w = row.any && e.index[k] >= 0 ? exp2_fast((e.q[k] - top) * (LOG2E / d.temperature)) : 0.f;
         e.q[k] = w;
         sum += w;
     }
-    sum = block_reduce<NT>(sum, e.scalar, [](float a, float b) { return a + b; });
+    return sum;
+}
+
+template <int NT>
+__device__ __forceinline__ void share_entries(const Distill& d, const Row& row, Entries& e, float sum)
+{
     const float inv = row.any ? 1.f / sum : 0.f;
     for (int k = threadIdx.x; k < d.top; k += NT) e.q[k] *= inv;
+}
+
+__device__ __forceinline__ bool has_entries(const Distill& d, float top) { return top != -INFINITY && d.kl != 0.f; }
+
+// All of it for kernels that take a row's sums from elsewhere.
+template <int NT, class T>
+__device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1, Entries& e, bool flag)
+{
+    struct Found { float top, bad; };
+    bool bad;
+    float top;
+    Row row = read_entries<NT, T>(d, n, v0, v1, e, top, bad);
+    const Found f = block_reduce<NT>(Found{top, bad ? 1.f : 0.f}, reinterpret_cast<Found*>(e.sums),
+                                     [](Found a, Found b) { return Found{larger(a.top, b.top), fmaxf(a.bad, b.bad)}; });
+    if (flag && threadIdx.x == 0 && d.status) d.status[n] = f.bad > 0.f ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    row.any = has_entries(d, f.top);
+    const float sum = block_reduce<NT>(weigh_entries<NT>(d, row, e, f.top), e.scalar, [](float a, float b) { return a + b; });
+    share_entries<NT>(d, row, e, sum);
     __syncthreads();
     return row;
 }
@@ -149,7 +176,7 @@ __device__ __forceinline__ float log2_sum(float s) { return s == 0.f ? 0.f : log
 
 // The row's loss, from its statistics.
 template <int NT, class T>
-__device__ __forceinline__ float row_loss(const Distill& d, const Row& row, Entries& e, float m, float lt, float l1, float label_logit)
+__device__ __forceinline__ float row_loss(const Distill& d, const Row& row, Entries& e, float m, float lt, float l1)
 {
     const float ct = LOG2E / d.temperature;
     float sum = 0.f;
@@ -162,35 +189,71 @@ __device__ __forceinline__ float row_loss(const Distill& d, const Row& row, Entr
     }
     sum = block_reduce<NT>(sum, e.scalar, [](float a, float b) { return a + b; });
     float loss = row.any ? d.kl * d.temperature * d.temperature * (LN2 * sum) : 0.f;
-    if (row.label >= 0) loss -= d.ce * (label_logit == -INFINITY ? label_logit : LN2 * ((label_logit - m) * LOG2E - l1));
+    const float s = row.label_logit;
+    if (row.label >= 0) loss -= d.ce * (s == -INFINITY ? s : LN2 * ((s - m) * LOG2E - l1));
     return loss;
 }
 
-// The factors of p and p1 in a row's gradient; 0 where the row has no such term.
-__device__ __forceinline__ void row_factors(const Distill& d, const Row& row, float& a, float& b)
+// p1 beside p: not wanted or of the same temperature, its square (temperature 2: an exponential takes four times as long as a product),
+// or by itself.
+enum Second { ONE, SQUARE, APART };
+
+__host__ __device__ __forceinline__ Second second_of(const Distill& d)
 {
-    const float w = d.dloss[row.n];
-    a = row.any ? w * d.kl * d.temperature : 0.f;
-    b = row.label >= 0 ? w * d.ce : 0.f;
+    return !d.labels || d.ce == 0.f || d.temperature == 1.f ? ONE : d.temperature == 2.f ? SQUARE : APART;
 }
 
-__device__ __forceinline__ float gradient(float s, float m, float ct, float lt, float l1, float a, float b)
+// A row's gradient away from its entries and label: a p + b p1, and what it takes.  A term whose factor is 0 is left out, whatever the logits.
+struct Slope {
+    float m, ct, lt, l1, a, b;
+    float c;                                     // b p1 = c p^T where p1 is p or its square
+    int how;                                     // -1: nothing; 0: p alone; 1: p1 alone; 2: both
+};
+
+__device__ __forceinline__ Slope slope_of(const Distill& d, const Row& row, float m, float lt, float l1)
 {
-    const float x = s - m;
-    float g = 0.f;
-    if (a != 0.f) g = a * exp2_fast(x * ct - lt);
-    if (b != 0.f) g += b * exp2_fast(x * LOG2E - l1);
+    const float w = d.dloss[row.n];
+    Slope g = {m, LOG2E / d.temperature, lt, l1, row.any ? w * d.kl * d.temperature : 0.f, row.label >= 0 ? w * d.ce : 0.f, 0.f, -1};
+    if (g.a != 0.f) g.how = 0;
+    if (g.b != 0.f) g.how = g.a != 0.f ? 2 : 1;
+    g.c = g.how == 2 ? g.b * exp2_fast(d.temperature * lt - l1) : 0.f;
     return g;
+}
+
+template <Second S, int HOW>
+__device__ __forceinline__ float slope_at(const Slope& g, float s)
+{
+    const float x = s - g.m;
+    if constexpr (HOW == 0) return g.a * exp2_fast(x * g.ct - g.lt);
+    if constexpr (HOW == 1) return g.b * exp2_fast(x * LOG2E - g.l1);
+    const float p = exp2_fast(x * g.ct - g.lt);
+    if constexpr (S == APART) return g.a * p + g.b * exp2_fast(x * LOG2E - g.l1);
+    if constexpr (S == SQUARE) return p * fmaf(g.c, p, g.a);
+    return (g.a + g.c) * p;
+}
+
+template <class T, Second S>
+__device__ __forceinline__ Word4 slope_word(const Slope& g, Word4 raw)
+{
+    Pack<T> w;
+    w.raw = raw;
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < PER_WORD4<T>; ++i) w.v[i] = from_float<T>(f(to_float(w.v[i])));
+    };
+    if (g.how == 2) each([&](float s) { return slope_at<S, 2>(g, s); });
+    else if (g.how == 0) each([&](float s) { return slope_at<S, 0>(g, s); });
+    else if (g.how == 1) each([&](float s) { return slope_at<S, 1>(g, s); });
+    else each([](float) { return 0.f; });
+    return w.raw;
 }
 
 // The places of the entries and of the label, whose gradients have further terms, written over what stands there.  Entries of
 // one index add up, in the order of k, and all write the same value.
-template <int NT, class T>
-__device__ __forceinline__ void write_places(const Distill& d, const Row& row, const Entries& e, i64 v0, i64 v1, float m, float lt, float l1,
-                                             float a, float b, float label_logit)
+template <int NT, class T, Second S>
+__device__ __forceinline__ void write_places(const Distill& d, const Row& row, const Entries& e, i64 v0, i64 v1, const Slope& g)
 {
-    if (a == 0.f && b == 0.f) return;
-    const float ct = LOG2E / d.temperature;
+    if (g.how < 0) return;
     T* grad = (T*)d.grad + row.n * d.ldd;
     for (int k = threadIdx.x; k <= d.top; k += NT) {
         const bool own = k == d.top;                                         // the label's turn
@@ -198,9 +261,11 @@ __device__ __forceinline__ void write_places(const Distill& d, const Row& row, c
         if (i < v0 || i >= v1) continue;
         float q = 0.f;
         for (int j = 0; j < d.top; ++j) q += e.index[j] == i ? e.q[j] : 0.f;
-        float g = gradient(own ? label_logit : e.s[k], m, ct, lt, l1, a, b) - a * q;
-        if (i == row.label) g -= b;
-        grad[i] = from_float<T>(g);
+        const float s = own ? row.label_logit : e.s[k];
+        float x = g.how == 2 ? slope_at<S, 2>(g, s) : g.how == 0 ? slope_at<S, 0>(g, s) : slope_at<S, 1>(g, s);
+        if (g.a != 0.f) x -= g.a * q;
+        if (i == row.label) x -= g.b;
+        grad[i] = from_float<T>(x);
     }
 }
 
@@ -213,52 +278,66 @@ __device__ __forceinline__ Word4 lowest_word()
     return w.raw;
 }
 
-// 16 bytes of a row from element v on; -inf behind its end.
+// 16 bytes of a row from element v on; -inf behind its end.  The word that passes the end is read from where it fits and moved: element
+// by element its one lane would hold up the row.
 template <class T>
 __device__ __forceinline__ Word4 read_logits(const T* s, i64 v, i64 end)
 {
     constexpr int N = PER_WORD4<T>;
     if (v + N <= end) return load_loose(s + v);
     Pack<T> w;
-    w.raw = lowest_word<T>();
+    if (end >= N) {
+        w.raw = load_loose(s + end - N);
+        for (i64 moves = v + N - end; moves > 0; --moves) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (v + i < end) w.v[i] = s[v + i];
+            for (int i = 0; i < N - 1; ++i) w.v[i] = w.v[i + 1];
+            w.v[N - 1] = (T)-INFINITY;
+        }
+    } else {
+        w.raw = lowest_word<T>();
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (v + i < end) w.v[i] = s[v + i];
+    }
     return w.raw;
 }
 
-template <class T>
-__device__ __forceinline__ void add_word(Sums& s, Word4 raw, float ct, bool two)
+// The sums of a word's exponentials, from a maximum that stands.
+template <class T, Second S>
+__device__ __forceinline__ void add_exponentials(Sums& s, Word4 raw, float m, float ct)
 {
-    constexpr int N = PER_WORD4<T>;
     Pack<T> w;
     w.raw = raw;
-    float x[N], high = s.m;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = to_float(w.v[i]);
-        high = fmaxf(high, x[i]);
+    for (int i = 0; i < PER_WORD4<T>; ++i) {
+        const float x = to_float(w.v[i]) - m, e = exp2_fast(x * ct);
+        s.st += e;
+        if constexpr (S == SQUARE) s.s1 = fmaf(e, e, s.s1);
+        if constexpr (S == APART) s.s1 += exp2_fast(x * LOG2E);
     }
+}
+
+template <class T>
+__device__ __forceinline__ float largest(Word4 raw, float m)
+{
+    Pack<T> w;
+    w.raw = raw;
+#pragma unroll
+    for (int i = 0; i < PER_WORD4<T>; ++i) m = fmaxf(m, to_float(w.v[i]));
+    return m;
+}
+
+// A word more, whose values may pass the maximum so far.
+template <class T, Second S>
+__device__ __forceinline__ void add_word(Sums& s, Word4 raw, float ct)
+{
+    const float high = largest<T>(raw, s.m);
     if (high > s.m) {
         s.st *= exp2_fast((s.m - high) * ct);
         s.s1 *= exp2_fast((s.m - high) * LOG2E);
         s.m = high;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) s.st += exp2_fast((x[i] - s.m) * ct);
-    if (two)
-#pragma unroll
-        for (int i = 0; i < N; ++i) s.s1 += exp2_fast((x[i] - s.m) * LOG2E);
-}
-
-template <class T>
-__device__ __forceinline__ Word4 gradient_word(Word4 raw, float m, float ct, float lt, float l1, float a, float b)
-{
-    Pack<T> w;
-    w.raw = raw;
-#pragma unroll
-    for (int i = 0; i < PER_WORD4<T>; ++i) w.v[i] = from_float<T>(gradient(to_float(w.v[i]), m, ct, lt, l1, a, b));
-    return w.raw;
+    add_exponentials<T, S>(s, raw, s.m, ct);
 }
 
 template <class T>
@@ -276,54 +355,127 @@ __device__ __forceinline__ void write_gradient(T* g, i64 v, i64 end, Word4 raw)
         if (v + i < end) g[v + i] = w.v[i];
 }
 
-// Whether p1 is needed beside p: at T = 1 they are one.
-__device__ __forceinline__ bool two_sums(const Distill& d) { return d.labels && d.temperature != 1.f; }
-
-template <int NT, class T>
-__device__ __forceinline__ Sums part_sums(const Distill& d, const T* s, i64 v0, i64 v1, Sums* shared)
+template <int NT, class T, Second S>
+__device__ __forceinline__ Sums part_sums(const Distill& d, const T* s, i64 v0, i64 v1)
 {
-    constexpr int N = PER_WORD4<T>;
+    constexpr int N = PER_WORD4<T>, AHEAD = 4;
     const float ct = LOG2E / d.temperature;
-    const bool two = two_sums(d);
     Sums sums = {-FLT_MAX, 0.f, 0.f};
-    for (i64 v = v0 + (i64)threadIdx.x * N; v < v1; v += NT * N) add_word<T>(sums, read_logits(s, v, v1), ct, two);
-    sums = block_reduce<NT>(sums, shared, [ct](Sums x, Sums y) { return joined(x, y, ct); });
-    if (!two) sums.s1 = sums.st;                                             // (only read where T is 1)
+    i64 v = v0 + (i64)threadIdx.x * N;
+    for (; v + (AHEAD - 1) * NT * N + N <= v1; v += AHEAD * NT * N) {
+        Word4 w[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) w[j] = load_loose(s + v + j * NT * N);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) add_word<T, S>(sums, w[j], ct);
+    }
+    for (; v < v1; v += NT * N) add_word<T, S>(sums, read_logits(s, v, v1), ct);
     return sums;
 }
 
-// Loss and statistics, and with GRAD the gradient too: one workgroup a row.
-template <int NT, class T, bool GRAD>
+// The launch's choice of S, as a type for the kernels' bodies.
+template <Second S> struct SecondTag { static constexpr Second value = S; };
+template <class F>
+__device__ __forceinline__ void with_second(const Distill& d, F&& f)
+{
+    switch (second_of(d)) {
+    case ONE: f(SecondTag<ONE>()); break;
+    case SQUARE: f(SecondTag<SQUARE>()); break;
+    default: f(SecondTag<APART>());
+    }
+}
+
+__device__ __forceinline__ void write_loss(const Distill& d, i64 n, float loss, float m, float lt, float l1)
+{
+    if (threadIdx.x) return;
+    d.loss[n] = loss;
+    if (d.stats) {
+        d.stats[n * 3] = m;
+        d.stats[n * 3 + 1] = lt;
+        d.stats[n * 3 + 2] = l1;
+    }
+}
+
+// Packed words stay packed: without this the compiler keeps the floats of one use for the next, twice the registers.
+template <int N>
+__device__ __forceinline__ void forget_floats(Word4 (&w)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
+}
+
+// Loss and statistics, and with GRAD the gradient too: one workgroup a row.  The row's first NT x HELD words stay in registers from the one load to
+// the gradient, a row of 128000 16-bit logits in half of a CU's; only what lies behind is read twice.  While one CU computes others load and
+// store; with the labels' term the vector ALU is busy half of the time, memory two thirds (4096 rows of 128000, bf16: 602 us, with two reads and
+// a running maximum 704).
+template <int NT, class T, bool GRAD, Second S>
 __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
 {
+    constexpr int N = PER_WORD4<T>, HELD = 16;
+    constexpr u32 STEP = NT * N;
     __shared__ Entries e;
-    constexpr int N = PER_WORD4<T>;
     const i64 n = blockIdx.x;
     const T* s = (const T*)d.logits + n * d.ld;
-    const Row row = read_row<NT, T>(d, n, 0, d.V, e, true);
-    const float label_logit = row.label >= 0 ? to_float(s[row.label]) : 0.f;
-    const Sums sums = part_sums<NT, T>(d, s, 0, d.V, e.sums);
-    const float lt = log2_sum(sums.st), l1 = log2_sum(sums.s1), ct = LOG2E / d.temperature;
-    const float loss = row_loss<NT, T>(d, row, e, sums.m, lt, l1, label_logit);
-    if (threadIdx.x == 0) {
-        d.loss[n] = loss;
-        if (d.stats) {
-            d.stats[n * 3] = sums.m;
-            d.stats[n * 3 + 1] = lt;
-            d.stats[n * 3 + 2] = l1;
+    const float ct = LOG2E / d.temperature;
+    Sums rest = {-FLT_MAX, 0.f, 0.f};
+    if (HELD * STEP < d.V) rest = part_sums<NT, T, S>(d, s, HELD * STEP, d.V);
+    __builtin_amdgcn_sched_barrier(0);                                       // (before the registers fill)
+    // A word belongs to the row as a whole, or is the part that is left, which one thread has besides.
+    const u32 v0 = threadIdx.x * N, whole = (u32)(d.V / N * N), end = min(whole, HELD * STEP);
+    const bool has_last = whole < (u32)d.V && whole < HELD * STEP && whole % STEP == v0;
+    Word4 held[HELD];
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) held[j] = v0 + j * STEP < end ? load_loose(s + j * STEP + v0) : lowest_word<T>();
+    Word4 last = lowest_word<T>();
+    if (has_last) last = read_logits(s, whole, d.V);
+    float top;
+    bool bad;
+    Row row = read_entries<NT, T>(d, n, 0, d.V, e, top, bad);
+    struct Found { float top, bad, m; };
+    Found f = {top, bad ? 1.f : 0.f, rest.m};
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (j * STEP < end) {
+            f.m = largest<T>(held[j], f.m);
+            __builtin_amdgcn_sched_barrier(0);                               // word by word: the registers are full
         }
-    }
+    if (has_last) f.m = largest<T>(last, f.m);
+    forget_floats(held);
+    f = block_reduce<NT>(f, reinterpret_cast<Found*>(e.sums),
+                         [](Found a, Found b) { return Found{larger(a.top, b.top), fmaxf(a.bad, b.bad), fmaxf(a.m, b.m)}; });
+    if (threadIdx.x == 0 && d.status) d.status[n] = f.bad > 0.f ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    row.any = has_entries(d, f.top);
+    Sums sums = joined(rest, Sums{f.m, 0.f, 0.f}, ct);                       // (f.m is the larger)
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (j * STEP < end) {
+            add_exponentials<T, S>(sums, held[j], f.m, ct);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    if (has_last) add_exponentials<T, S>(sums, last, f.m, ct);
+    struct Totals { float q, st, s1; };
+    Totals t = {weigh_entries<NT>(d, row, e, f.top), sums.st, sums.s1};
+    t = block_reduce<NT>(t, reinterpret_cast<Totals*>(e.sums), [](Totals a, Totals b) { return Totals{a.q + b.q, a.st + b.st, a.s1 + b.s1}; });
+    if constexpr (S == ONE) t.s1 = t.st;                                     // (read where the temperature is 1)
+    share_entries<NT>(d, row, e, t.q);
+    const float m = f.m, lt = log2_sum(t.st), l1 = log2_sum(t.s1);
+    write_loss(d, n, row_loss<NT, T>(d, row, e, m, lt, l1), m, lt, l1);
     if constexpr (GRAD) {
-        float a, b;
-        row_factors(d, row, a, b);
-        T* g = (T*)d.grad + n * d.ldd;
+        const Slope g = slope_of(d, row, m, lt, l1);
+        T* out = (T*)d.grad + n * d.ldd;
+        forget_floats(held);
         __builtin_amdgcn_s_waitcnt(0);                                       // in place: the logits of the places have been read
         __syncthreads();
-        for (i64 v = (i64)threadIdx.x * N; v < d.V; v += NT * N)
-            write_gradient(g, v, d.V, gradient_word<T>(read_logits(s, v, d.V), sums.m, ct, lt, l1, a, b));
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            if (v0 + j * STEP < end) store_loose(out + j * STEP + v0, slope_word<T, S>(g, held[j]));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (has_last) write_gradient(out, whole, d.V, slope_word<T, S>(g, last));
+        for (i64 v = v0 + HELD * STEP; v < d.V; v += STEP) write_gradient(out, v, d.V, slope_word<T, S>(g, read_logits(s, v, d.V)));
         __builtin_amdgcn_s_waitcnt(0);                                       // stores to one address arrive in this order
         __syncthreads();
-        write_places<NT, T>(d, row, e, 0, d.V, sums.m, lt, l1, a, b, label_logit);
+        write_places<NT, T, S>(d, row, e, 0, d.V, g);
     }
 }
 
@@ -341,9 +493,12 @@ __global__ void __launch_bounds__(NT) tr_distill_part_kernel(Distill d)
     __shared__ Sums shared[16];
     const i64 n = blockIdx.x / d.splits;
     const int part = blockIdx.x % d.splits;
+    const float ct = LOG2E / d.temperature;
     i64 v0, v1;
     part_range(d, part, PER_WORD4<T>, v0, v1);
-    const Sums sums = part_sums<NT, T>(d, (const T*)d.logits + n * d.ld, v0, v1, shared);
+    Sums sums;
+    with_second(d, [&](auto s) { sums = part_sums<NT, T, decltype(s)::value>(d, (const T*)d.logits + n * d.ld, v0, v1); });
+    sums = block_reduce<NT>(sums, shared, [ct](Sums x, Sums y) { return joined(x, y, ct); });
     if (threadIdx.x == 0) {
         float* out = d.partial + (n * d.splits + part) * 3;
         out[0] = sums.m;
@@ -358,25 +513,17 @@ __global__ void __launch_bounds__(NT) tr_distill_join_kernel(Distill d)
 {
     __shared__ Entries e;
     const i64 n = blockIdx.x;
-    const T* s = (const T*)d.logits + n * d.ld;
     const Row row = read_row<NT, T>(d, n, 0, d.V, e, true);
-    const float label_logit = row.label >= 0 ? to_float(s[row.label]) : 0.f, ct = LOG2E / d.temperature;
+    const float ct = LOG2E / d.temperature;
     Sums sums = {-FLT_MAX, 0.f, 0.f};
     for (int p = threadIdx.x; p < d.splits; p += NT) {
         const float* in = d.partial + (n * d.splits + p) * 3;
         sums = joined(sums, Sums{in[0], in[1], in[2]}, ct);
     }
     sums = block_reduce<NT>(sums, e.sums, [ct](Sums x, Sums y) { return joined(x, y, ct); });
+    if (second_of(d) == ONE) sums.s1 = sums.st;                 // (read where the temperature is 1)
     const float lt = log2_sum(sums.st), l1 = log2_sum(sums.s1);
-    const float loss = row_loss<NT, T>(d, row, e, sums.m, lt, l1, label_logit);
-    if (threadIdx.x == 0) {
-        d.loss[n] = loss;
-        if (d.stats) {
-            d.stats[n * 3] = sums.m;
-            d.stats[n * 3 + 1] = lt;
-            d.stats[n * 3 + 2] = l1;
-        }
-    }
+    write_loss(d, n, row_loss<NT, T>(d, row, e, sums.m, lt, l1), sums.m, lt, l1);
 }
 
 // The gradient from statistics: every row in `splits` parts.
@@ -390,18 +537,17 @@ __global__ void __launch_bounds__(NT) tr_distill_gradient_kernel(Distill d)
     part_range(d, blockIdx.x % d.splits, N, v0, v1);
     const T* s = (const T*)d.logits + n * d.ld;
     const Row row = read_row<NT, T>(d, n, v0, v1, e, false);
-    const float label_logit = row.label >= v0 && row.label < v1 ? to_float(s[row.label]) : 0.f, ct = LOG2E / d.temperature;
-    const float m = d.stats[n * 3], lt = d.stats[n * 3 + 1], l1 = d.stats[n * 3 + 2];
-    float a, b;
-    row_factors(d, row, a, b);
-    T* g = (T*)d.grad + n * d.ldd;
+    const Slope g = slope_of(d, row, d.stats[n * 3], d.stats[n * 3 + 1], d.stats[n * 3 + 2]);
+    T* out = (T*)d.grad + n * d.ldd;
     __builtin_amdgcn_s_waitcnt(0);                                           // in place: the logits of the places have been read
     __syncthreads();
-    for (i64 v = v0 + (i64)threadIdx.x * N; v < v1; v += NT * N)
-        write_gradient(g, v, v1, gradient_word<T>(read_logits(s, v, v1), m, ct, lt, l1, a, b));
-    __builtin_amdgcn_s_waitcnt(0);                                           // stores to one address arrive in this order
-    __syncthreads();
-    write_places<NT, T>(d, row, e, v0, v1, m, lt, l1, a, b, label_logit);
+    with_second(d, [&](auto second) {
+        constexpr Second S = decltype(second)::value;
+        for (i64 v = v0 + (i64)threadIdx.x * N; v < v1; v += NT * N) write_gradient(out, v, v1, slope_word<T, S>(g, read_logits(s, v, v1)));
+        __builtin_amdgcn_s_waitcnt(0);                                       // stores to one address arrive in this order
+        __syncthreads();
+        write_places<NT, T, S>(d, row, e, v0, v1, g);
+    });
 }
 
 }  // namespace

@@ -158,22 +158,27 @@ int distill_splits(i64 N, i64 V, int size)
 
 size_t distill_partial_bytes(i64 N, int splits) { return splits > 1 ? ((size_t)N * splits * 3 * sizeof(float) + 255) / 256 * 256 : 0; }
 
+template <int NT, class T, bool GRAD>
+int distill_rows(const Distill& d, hipStream_t st)
+{
+    const dim3 rows((unsigned)d.N);
+    switch (second_of(d)) {
+    case ONE: LAUNCH((tr_distill_row_kernel<NT, T, GRAD, ONE>), rows, dim3(NT), d); break;
+    case SQUARE: LAUNCH((tr_distill_row_kernel<NT, T, GRAD, SQUARE>), rows, dim3(NT), d); break;
+    default: LAUNCH((tr_distill_row_kernel<NT, T, GRAD, APART>), rows, dim3(NT), d);
+    }
+    return EBSP_OK;
+}
+
 template <class T>
 int distill_loss(Distill d, bool grad, hipStream_t st)
 {
-    const dim3 rows((unsigned)d.N);
-    const dim3 parts((unsigned)(d.N * d.splits));
     if (d.splits == 1) {
         const bool large = d.V / PER_WORD4<T> > 2048;
-        if (grad) {
-            if (large) LAUNCH((tr_distill_row_kernel<1024, T, true>), rows, dim3(1024), d);
-            else LAUNCH((tr_distill_row_kernel<256, T, true>), rows, dim3(256), d);
-        } else {
-            if (large) LAUNCH((tr_distill_row_kernel<1024, T, false>), rows, dim3(1024), d);
-            else LAUNCH((tr_distill_row_kernel<256, T, false>), rows, dim3(256), d);
-        }
-        return EBSP_OK;
+        if (grad) return large ? distill_rows<1024, T, true>(d, st) : distill_rows<256, T, true>(d, st);
+        return large ? distill_rows<1024, T, false>(d, st) : distill_rows<256, T, false>(d, st);
     }
+    const dim3 rows((unsigned)d.N), parts((unsigned)(d.N * d.splits));
     LAUNCH((tr_distill_part_kernel<256, T>), parts, dim3(256), d);
     LAUNCH((tr_distill_join_kernel<256, T>), rows, dim3(256), d);
     if (grad) LAUNCH((tr_distill_gradient_kernel<256, T>), parts, dim3(256), d);
