@@ -146,17 +146,33 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
     return EBSP_OK;
 }
 
-// Parts that a row is cut into: one where there are rows enough for every CU, else so many that there are two workgroups for each,
-// of no less than 512 words of 16 bytes.
+// Parts that a row is cut into for its sums: several only where rows are few and long, since they take two launches more.  bf16, loss / loss and
+// gradient, us in a graph, in one part and in as many as here: 1 x 32000 7.9 / 14.0 and (16) 7.7 / 13.4; 1 x 128000 13.5 / 25 and (31)
+// 8.0 / 14.5; 64 x 128000 14.1 / 28 and (8) 11.1 / 23; 128 x 128000 14.9 / 31.5 and (4) 15.2 / 32.6.
 int distill_splits(i64 N, i64 V, int size)
 {
     const i64 words = (V * size + 15) / 16;
-    i64 s = N >= 256 ? 1 : (512 + N - 1) / (N > 0 ? N : 1);
-    if (s > words / 512) s = words / 512;
+    if (N > 96 || words <= 4096) return 1;
+    const i64 s = 512 / (N > 0 ? N : 1), most = words / 512;
+    return (int)(s < most ? s : most);
+}
+
+// Parts for a gradient from statistics, which need no scratch: about four workgroups a CU, of no less than 512 words.
+int gradient_splits(i64 N, i64 V, int size)
+{
+    const i64 most = (V * size + 15) / 16 / 512, s = 1024 / (N > 0 ? N : 1) < most ? 1024 / (N > 0 ? N : 1) : most;
     return (int)(s < 1 ? 1 : s);
 }
 
 size_t distill_partial_bytes(i64 N, int splits) { return splits > 1 ? ((size_t)N * splits * 3 * sizeof(float) + 255) / 256 * 256 : 0; }
+
+template <class T>
+int distill_gradient(Distill d, hipStream_t st)
+{
+    d.splits = gradient_splits(d.N, d.V, sizeof(T));
+    LAUNCH((tr_distill_gradient_kernel<256, T>), dim3((unsigned)(d.N * d.splits)), dim3(256), d);
+    return EBSP_OK;
+}
 
 template <int NT, class T, bool GRAD>
 int distill_rows(const Distill& d, hipStream_t st)
@@ -174,22 +190,15 @@ template <class T>
 int distill_loss(Distill d, bool grad, hipStream_t st)
 {
     if (d.splits == 1) {
+        // A gradient wants the whole row in registers.  The loss alone of many rows runs better from several small workgroups a CU, whatever
+        // of a row they have to stream (600 x 128000 52 -> 35 us).
         const bool large = d.V / PER_WORD4<T> > 2048;
         if (grad) return large ? distill_rows<1024, T, true>(d, st) : distill_rows<256, T, true>(d, st);
-        return large ? distill_rows<1024, T, false>(d, st) : distill_rows<256, T, false>(d, st);
+        return large && d.N <= 256 ? distill_rows<1024, T, false>(d, st) : distill_rows<256, T, false>(d, st);
     }
-    const dim3 rows((unsigned)d.N), parts((unsigned)(d.N * d.splits));
-    LAUNCH((tr_distill_part_kernel<256, T>), parts, dim3(256), d);
-    LAUNCH((tr_distill_join_kernel<256, T>), rows, dim3(256), d);
-    if (grad) LAUNCH((tr_distill_gradient_kernel<256, T>), parts, dim3(256), d);
-    return EBSP_OK;
-}
-
-template <class T>
-int distill_gradient(Distill d, hipStream_t st)
-{
-    LAUNCH((tr_distill_gradient_kernel<256, T>), dim3((unsigned)(d.N * d.splits)), dim3(256), d);
-    return EBSP_OK;
+    LAUNCH((tr_distill_part_kernel<256, T>), dim3((unsigned)(d.N * d.splits)), dim3(256), d);
+    LAUNCH((tr_distill_join_kernel<256, T>), dim3((unsigned)d.N), dim3(256), d);
+    return grad ? distill_gradient<T>(d, st) : EBSP_OK;
 }
 
 int check_distill(const Distill& d, int dtype, int index_bytes)
@@ -342,8 +351,7 @@ int ebsp_distill_backward(const void* logits, int64_t ld, int64_t N, int64_t V, 
     if (N == 0) return EBSP_OK;
     if (!stats) return fail(EBSP_ERR_NULL, "stats must not be NULL");
     if (int rc = check_gradient(d)) return rc;
-    d.splits = distill_splits(N, V, element_size(dtype));
-    if (!launchable(N * d.splits, 1024)) return fail(EBSP_ERR_SHAPE, "too many rows for one call");
+    if (!launchable(N * gradient_splits(N, V, element_size(dtype)), 256)) return fail(EBSP_ERR_SHAPE, "too many rows for one call");
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
     return dtype == EBSP_BF16 ? distill_gradient<__bf16>(d, st) : dtype == EBSP_F16 ? distill_gradient<_Float16>(d, st) : distill_gradient<float>(d, st);
