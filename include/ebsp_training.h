@@ -74,10 +74,15 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
  *   dx       out [M][K], rows lddx apart, or NULL: not wanted
  *   dwg, dwu out [F][K], rows lddw apart, or both NULL: not wanted
  *   workspace    at least ebsp_gated_ff_workspace_bytes(M, F, dtype) bytes,
- *                256-byte aligned (it holds dg and du, rounded to dtype).
+ *                256-byte aligned (it holds dg and du, rounded to dtype).  With
+ *                ebsp_gated_ff_split_workspace_bytes(M, K, F, dtype) bytes, where
+ *                that is more, long sums of small results run in several parts
+ *                side by side, which is faster (dx where tokens are few, the
+ *                weights' gradients where tokens are many and matrices small).
  * M == 0 gives zero weight gradients, F == 0 a zero dx.
  */
 size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype);
+size_t ebsp_gated_ff_split_workspace_bytes(int64_t M, int64_t K, int64_t F, int32_t dtype);
 int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
                            const void* wu, int64_t ldwu, const float* g, const float* u, int64_t ldg,
                            int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,

@@ -145,9 +145,15 @@ struct FfGradient {
     int wide[2];
     int segments;                                                            // dx: 2, the sum runs over gate and up
     i64 rows;                                                                // of the result (a.index counts the padded ones too)
+    float* partial;                                                          // sums in parts: [result][parts][rows][columns, padded to 4]
+    int parts, large;                                                        // large: tiles of 256 x 256
 };
 
-// dx = dg Wg + du Wu (A in rows, two segments) and dW = dg^T x, du^T x (A in columns, a half of the grid each).
+__host__ __device__ __forceinline__ i64 partial_ld(i64 columns) { return (columns + 3) / 4 * 4; }
+
+// dx = dg Wg + du Wu (A in rows, two segments) and dW = dg^T x, du^T x (A in columns, a half of the grid each).  dx has few tiles and
+// long sums where tokens are few, dW where the matrices are small and tokens many; the grid's second axis cuts the sums then, and
+// the parts go to memory unrounded.
 template <class T, class TL, Layout LA, bool DIRECT>
 __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
 {
@@ -156,11 +162,11 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
     const u32 tm = (u32)((f.rows + TL::BM - 1) / TL::BM), tn = (u32)((f.b.index + TL::BN - 1) / TL::BN);
     u32 bm, bn;
     tile_of(blockIdx.x, tm, tn, bm, bn);
-    const int z = blockIdx.y;
+    const int parts = f.parts, z = LA == COLS ? blockIdx.y / parts : 0, part = blockIdx.y - z * parts;
     const Operand a = {{LA == COLS ? f.a.matrix(z) : f.a.p[0], f.a.p[1]}, {f.a.ld[0], f.a.ld[1]}, f.a.index, f.a.depth};
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * TL::BN;
     Float4 acc[FN][FM];
-    product_tile<T, TL, LA, COLS, 0, DIRECT>(acc, lds, a, f.b, f.segments, m0, n0);
+    product_tile<T, TL, LA, COLS, 0, DIRECT>(acc, lds, a, f.b, f.segments, m0, n0, part, parts);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
@@ -171,7 +177,110 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
         for (int j = 0; j < FN; j += 2) {
             const i64 n = n0 + (wn * FN + j) * 16;
             const i64 have = f.b.index - n;
-            if (have > 0) store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, f.wide[z], lane);
+            if (have <= 0) continue;
+            if (parts > 1) {
+                const i64 ld = partial_ld(f.b.index);
+                float* p = f.partial + (((i64)z * parts + part) * f.rows + m) * ld + n + (lane >> 4) * 4;
+                if (n + (lane >> 4) * 4 < ld) *reinterpret_cast<Float4*>(p) = acc[j][i];
+                if (n + (lane >> 4) * 4 + 16 < ld) *reinterpret_cast<Float4*>(p + 16) = acc[j + 1][i];
+            } else {
+                store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, f.wide[z], lane);
+            }
+        }
+    }
+}
+
+// The parts of a result, added up in their order and rounded.
+template <class T>
+__global__ void __launch_bounds__(256) tr_ff_join_kernel(FfGradient f)
+{
+    const int z = blockIdx.y;
+    const i64 columns = f.b.index, ld = partial_ld(columns), all = f.rows * (ld / 4);
+    const float* partial = f.partial + (i64)z * f.parts * f.rows * ld;
+    for (i64 at = (i64)blockIdx.x * 256 + threadIdx.x; at < all; at += (i64)gridDim.x * 256) {
+        const i64 m = at / (ld / 4), n = (at - m * (ld / 4)) * 4;
+        Float4 sum = *reinterpret_cast<const Float4*>(partial + at * 4);
+        for (int p = 1; p < f.parts; ++p) sum += *reinterpret_cast<const Float4*>(partial + (p * f.rows * ld + at * 4));
+        store4((T*)f.out[z] + m * f.ld[z] + n, sum, columns - n, f.wide[z]);
+    }
+}
+
+// Few tokens: one read of the weights is all there is to it (1 token of 4096 x 12288 in bf16: 201 MB in 37 us, 5.4 TB/s).  They go from memory
+// straight to the matrix cores, 128 bytes of a row by each wave in turn; a workgroup has 16 units (gate and up), its waves share the
+// contraction and add up through shared memory.  Tokens fill FM squares; those that are not there repeat the last.
+template <int FM_>
+struct Few {
+    static constexpr int FM = FM_, WAVES = 8, NT = WAVES * WAVE, SUMS = 2 * FM;
+};
+
+template <class T, class TF, bool GUARD, int HALVES>
+__device__ __forceinline__ void few_products(Float4 (&acc)[TF::SUMS], const T* const (&w)[2], const T* const (&x)[TF::FM], i64 k, i64 depth)
+{
+    constexpr int N = PER_WORD4<T>;
+    Word4 rw[HALVES][2], rx[HALVES][TF::FM];
+    auto load = [&](const T* p, int h) { return GUARD ? load_some(p + k + h * 4 * N, depth - k - h * 4 * N) : load_loose(p + k + h * 4 * N); };
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+        // (k counts from the lane's own position; a wave's steps lie WAVES x 128 bytes apart, the halves of one side by side)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) rw[h][j] = load(w[j], h % 2 + h / 2 * 2 * TF::WAVES);
+#pragma unroll
+        for (int i = 0; i < TF::FM; ++i) rx[h][i] = load(x[i], h % 2 + h / 2 * 2 * TF::WAVES);
+    }
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < TF::FM; ++i) square_product<T>(acc[j * TF::FM + i], rw[h][j], rx[h][i]);
+}
+
+template <class T, class TF>
+__global__ void __launch_bounds__(TF::NT, 4) tr_ff_few_kernel(FfForward f)
+{
+    constexpr int FM = TF::FM, W = TF::WAVES, SUMS = TF::SUMS, N = PER_WORD4<T>;
+    constexpr int STEP = 8 * N, HALVES = FM == 1 ? 8 : 4;                    // a step: 128 bytes of a row
+    __shared__ Float4 part[W / 2][SUMS][WAVE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const i64 n0 = (i64)blockIdx.x * 16, m0 = (i64)blockIdx.y * (FM * 16);
+    const i64 unit = min(n0 + (lane & 15), f.w.index - 1);
+    const T *w[2] = {(const T*)f.w.p[0] + unit * f.w.ld[0], (const T*)f.w.p[1] + unit * f.w.ld[1]}, *x[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) x[i] = (const T*)f.x.p[0] + min(m0 + i * 16 + (lane & 15), f.x.index - 1) * f.x.ld[0];
+    Float4 acc[SUMS];
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) acc[i] = Float4{0, 0, 0, 0};
+    const i64 depth = f.x.depth;
+    i64 k = (i64)wave * STEP;                                                // the same for the whole wave
+    const int mine = (lane >> 4) * N;
+    constexpr i64 BATCH = (i64)(HALVES / 2 - 1) * W * STEP + STEP;           // from a wave's first step to behind its last
+    for (; k + BATCH <= depth; k += HALVES / 2 * W * STEP) few_products<T, TF, false, HALVES>(acc, w, x, k + mine, depth);
+    for (; k + STEP <= depth; k += W * STEP) few_products<T, TF, false, 2>(acc, w, x, k + mine, depth);
+    if (k < depth) few_products<T, TF, true, 2>(acc, w, x, k + mine, depth);
+    // Half of the waves hand their sums to the others, those put theirs beside each other, and the squares are shared out.
+    if (wave >= W / 2)
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) part[wave - W / 2][i][lane] = acc[i];
+    __syncthreads();
+    if (wave < W / 2)
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) part[wave][i][lane] += acc[i];
+    __syncthreads();
+    if (wave < FM) {
+        const i64 m = m0 + wave * 16 + (lane & 15), n = n0 + (lane >> 4) * 4, have = f.w.index - n;
+        if (m >= f.x.index || have <= 0) return;
+        Float4 g = part[0][wave][lane], u = part[0][FM + wave][lane], h;
+#pragma unroll
+        for (int p = 1; p < W / 2; ++p) {
+            g += part[p][wave][lane];
+            u += part[p][FM + wave][lane];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
+        store4((T*)f.h + m * f.ldh + n, h, have, f.wide_h);
+        if (f.g) {
+            store4(f.g + m * f.ldg + n, g, have, f.wide_g);
+            store4(f.u + m * f.ldg + n, u, have, f.wide_g);
         }
     }
 }

@@ -208,9 +208,10 @@ __device__ __forceinline__ void wait_and_meet()
 }
 
 // The sums of the tile at (m0, n0) over `segments` matrices of each operand one after the other (PAIRED > 0: over one, B's
-// two alternating in the tile).
+// two alternating in the tile), or over the `part`-th of `parts` stretches of their steps.
 template <class T, class TL, Layout LA, Layout LB, int PAIRED, bool DIRECT>
-__device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char* lds, const Operand& a, const Operand& b, int segments, i64 m0, i64 n0)
+__device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char* lds, const Operand& a, const Operand& b, int segments, i64 m0, i64 n0,
+                                             int part = 0, int parts = 1)
 {
     constexpr int FM = TL::FM, FN = TL::FN, NT = TL::NT, BM = TL::BM, BN = TL::BN, BK = TL::BK;
     constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;                        // 16-byte positions a thread brings
@@ -256,30 +257,31 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         }
     };
     if constexpr (!DIRECT) {
-        const int total = steps * segments;
+        const int all = steps * segments, from = (int)((i64)all * part / parts), total = (int)((i64)all * (part + 1) / parts) - from;
         if (total == 0) return;
-        fetch(0, 0);
+        auto fetch_step = [&](int s) { fetch(s >= steps, s >= steps ? s - steps : s); };
+        fetch_step(from);
         put(0);
         __syncthreads();
         for (int s = 0; s < total; ++s) {
-            const int next = s + 1 >= steps ? s + 1 - steps : s + 1;
-            if (s + 1 < total) fetch(s + 1 >= steps, next);
+            if (s + 1 < total) fetch_step(from + s + 1);
             products(s & 1);
             if (s + 1 < total) put(~s & 1);                                  // what nothing reads any more
             __syncthreads();
         }
         return;
     }
-    // Whole steps of all segments first, then the parts of a step that are left.
-    const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK), total = whole * segments;
+    // Whole steps of all segments first, then (in the last stretch) the parts of a step that are left.
+    const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK), all = whole * segments;
+    const int from = (int)((i64)all * part / parts), total = (int)((i64)all * (part + 1) / parts) - from;
     if (total > 0) {
         DirectTile<T, LA, BM, NT, 0> da;
         DirectTile<T, LB, BN, NT, PAIRED> db;
         da.init(a, m0);
         db.init(b, n0);
         constexpr int LOADS = PA + PB;
-        auto bring = [&](int s, int slot_a, int slot_b, int i) {             // load i of the LOADS of step s
-            const int seg = s >= whole, k = s - seg * whole;
+        auto bring = [&](int s, int slot_a, int slot_b, int i) {             // load i of the LOADS of step s of the stretch
+            const int at = from + s, seg = at >= whole, k = at - seg * whole;
             if (i < PA) da.bring(place_a(slot_a), seg, k, wave, i);
             else db.bring(place_b(slot_b), seg, k, wave, i - PA);
         };
@@ -332,7 +334,7 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
             sa = sa1;
         }
     }
-    if (whole < steps)
+    if (whole < steps && part == parts - 1)
 #pragma unroll 1
         for (int seg = 0; seg < segments; ++seg) {
             fetch(seg, whole);

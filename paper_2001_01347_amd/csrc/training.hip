@@ -93,9 +93,27 @@ int ff_forward_tiles(const FfForward& f, hipStream_t st)
 
 i64 tiles_of(i64 m, i64 n, int bm, int bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); }
 
+template <class T, int FM>
+int ff_few(const FfForward& f, hipStream_t st)
+{
+    using TF = Few<FM>;
+    const i64 blocks = (f.w.index + 15) / 16, rows = (f.x.index + FM * 16 - 1) / (FM * 16);
+    if (!launchable(blocks * rows, TF::NT)) return fail(EBSP_ERR_SHAPE, "the result is too large for one call");
+    LAUNCH((tr_ff_few_kernel<T, TF>), dim3((unsigned)blocks, (unsigned)rows), dim3(TF::NT), f);
+    return EBSP_OK;
+}
+
+// Tiles want workgroups enough and long sums in each: where rows or units are few the kernel that shares a sum out among its waves is faster.
+// us, it / tiles of 128 x 64 (M x K x F): bf16 1 x 4096 x 12288 37 / 49, 16 x 4096 x 2048 13 / 32, 16 x 4096 x 12288 47 / 45, 24 x 1024 x 6144 10 / 12,
+// 64 x 4096 x 4096 28 / 42, 64 x 1024 x 6144 14 / 14, 100 x 4096 x 3000 43 / 42, 192 x 4096 x 1024 24 / 34, 256 x 2048 x 2048 25 / 20; f32
+// 64 x 4096 x 4096 62 / 250, 256 x 1024 x 2816 49 / 67, 384 x 4096 x 4096 357 / 252.  Its squares hold 64 rows, or 32 where that makes too few workgroups
+// (64 x 4096 x 1024 18, so 24).
 template <class T>
 int ff_forward(const FfForward& f, hipStream_t st)
 {
+    const i64 M = f.x.index, groups = tiles_of(M, f.w.index, 64, 16);
+    if (M <= 16) return ff_few<T, 1>(f, st);
+    if (groups <= (sizeof(T) == 4 ? 768 : 352)) return M <= 32 || groups <= 128 ? ff_few<T, 2>(f, st) : ff_few<T, 4>(f, st);
     if (tiles_of(f.x.index, f.w.index, 256, 128) >= 192) return ff_forward_tiles<T, Tile<T, 2, 4, 8, 4>>(f, st);
     return ff_forward_tiles<T, Tile<T, 2, 2, 4, 4>>(f, st);
 }
@@ -105,7 +123,7 @@ int ff_gradient_tiles(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
     const bool direct = operand_direct(f.a, LA, sizeof(T)) && operand_direct(f.b, COLS, sizeof(T));
     dim3 grid;
-    if (int rc = tile_grid<TL, TL::BN>(f.rows, f.b.index, grid, z)) return rc;
+    if (int rc = tile_grid<TL, TL::BN>(f.rows, f.b.index, grid, z * f.parts)) return rc;
     if (!launch) return EBSP_OK;
     if (direct) LAUNCH((tr_ff_gradient_kernel<T, TL, LA, true>), grid, dim3(TL::NT), f);
     else LAUNCH((tr_ff_gradient_kernel<T, TL, LA, false>), grid, dim3(TL::NT), f);
@@ -115,22 +133,66 @@ int ff_gradient_tiles(const FfGradient& f, int z, bool launch, hipStream_t st)
 template <class T, Layout LA>
 int ff_gradient(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
-    if (tiles_of(f.rows, f.b.index, 256, 256) * z >= 192) return ff_gradient_tiles<T, Tile<T, 2, 4, 8, 4>, LA>(f, z, launch, st);
+    if (f.large) return ff_gradient_tiles<T, Tile<T, 2, 4, 8, 4>, LA>(f, z, launch, st);
     return ff_gradient_tiles<T, Tile<T, 2, 2, 4, 4>, LA>(f, z, launch, st);
+}
+
+// How a gradient of `rows` x `columns` is cut up, `z` of them in one launch, each a sum of `steps` steps of 128 bytes.
+struct Cut {
+    bool large;                                                              // tiles of 256 x 256, not 128 x 128
+    int parts;                                                               // of every sum
+};
+
+// A CU for every tile, or for every part of one.  us, large tiles in parts / small ones in parts / small ones whole: dx 2048 x 2048 x 8192 bf16 (64
+// large tiles, 256 steps) 164 / 180 / 192, 512 x 4096 x 12288 (32, 384) 115 / 141 / 247, 1024 x 4096 x 2048 (64, 64) 58 / 58 / 52, 1 x 4096 x 12288 (32
+// small, 384) 66 / 45 / 224, f32 1024 x 1024 x 2816 (64 small, 176) 189 / 112 / 361; dW 8192 x 1024 x 2048 (64, 128) 112 / 127 / 123.
+Cut gradient_cut(i64 rows, i64 columns, int z, i64 steps, int size)
+{
+    const i64 large = tiles_of(rows, columns, 256, 256) * z, small = tiles_of(rows, columns, 128, 128) * z;
+    if (large >= 192 || small == 0) return {true, 1};
+    if (large >= 32 && steps * large >= 32 * 256) return {true, (int)(256 / large)};
+    if (small >= 192 || steps < (size == 4 ? 8 : 24)) return {false, 1};
+    const i64 parts = 256 / small, most = size == 4 ? steps / 4 : steps / 8;
+    return {false, (int)(parts < most ? parts : most)};
+}
+
+Cut dx_cut(i64 M, i64 K, i64 F, int size) { return gradient_cut(M, K, 1, 2 * ((F * size + 127) / 128), size); }
+Cut dw_cut(i64 M, i64 K, i64 F, int size) { return gradient_cut(F, K, 2, (M * size + 127) / 128, size); }
+
+size_t partial_bytes(i64 rows, i64 columns, int z, const Cut& cut)
+{
+    return cut.parts > 1 ? ((size_t)cut.parts * z * rows * partial_ld(columns) * sizeof(float) + 255) / 256 * 256 : 0;
+}
+
+// The launches of one gradient.
+template <class T, Layout LA>
+int ff_gradient_and_join(const FfGradient& f, int z, bool launch, hipStream_t st)
+{
+    if (f.rows == 0) return EBSP_OK;
+    if (int rc = ff_gradient<T, LA>(f, z, launch, st)) return rc;
+    if (!launch || f.parts == 1) return EBSP_OK;
+    const i64 blocks = (f.rows * (partial_ld(f.b.index) / 4) + 255) / 256;
+    LAUNCH(tr_ff_join_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384), (unsigned)z), dim3(256), f);
+    return EBSP_OK;
 }
 
 template <class T>
 int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg, i64 ldwg, const void* wu, i64 ldwu, const float* g,
                 const float* u, i64 ldg, i64 M, i64 K, i64 F, int act, void* dx, i64 lddx, void* dwg, void* dwu, i64 lddw, void* workspace,
-                hipStream_t st)
+                size_t workspace_bytes, hipStream_t st)
 {
     const i64 ldd = padded_units(F, sizeof(T));
     T* dg = (T*)workspace;
     T* du = dg + M * ldd;
+    const size_t units = ebsp_gated_ff_workspace_bytes(M, F, sizeof(T) == 4 ? EBSP_F32 : EBSP_BF16);
+    float* partial = (float*)((char*)workspace + units);                     // dx's, then dW's
+    Cut cx = dx_cut(M, K, F, sizeof(T)), cw = dw_cut(M, K, F, sizeof(T));
+    if (workspace_bytes < units + partial_bytes(M, K, 1, cx)) cx.parts = 1;
+    if (workspace_bytes < units + partial_bytes(F, K, 2, cw)) cw.parts = 1;
     const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0},
-                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2, M};
+                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2, M, partial, cx.parts, cx.large};
     const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
-                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1, F};
+                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1, F, partial, cw.parts, cw.large};
     for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
         const i64 chunks = M * (ldd / PER_WORD4<T>);
         if (launch && chunks > 0) {
@@ -138,10 +200,10 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
             LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, g, u,
                    ldg, dg, du, ldd, M, F, act);
         }
-        if (dx && M > 0)
-            if (int rc = ff_gradient<T, ROWS>(to_x, 1, launch, st)) return rc;
-        if (dwg && F > 0)
-            if (int rc = ff_gradient<T, COLS>(to_w, 2, launch, st)) return rc;
+        if (dx)
+            if (int rc = ff_gradient_and_join<T, ROWS>(to_x, 1, launch, st)) return rc;
+        if (dwg)
+            if (int rc = ff_gradient_and_join<T, COLS>(to_w, 2, launch, st)) return rc;
     }
     return EBSP_OK;
 }
@@ -246,6 +308,7 @@ template <class T, int SPLIT>
 int merge_split(const Merge& g, hipStream_t st)
 {
     const i64 per = (SPLIT == 1 ? 256 : 64) * PER_WORD4<T>;
+    if (!launchable((g.n + per - 1) / per, SPLIT == 1 ? 256 : SPLIT * 64)) return fail(EBSP_ERR_SHAPE, "too many weights for one call");
     LAUNCH_LDS((tr_merge_kernel<T, SPLIT>), dim3((unsigned)((g.n + per - 1) / per)), dim3(SPLIT == 1 ? 256 : SPLIT * 64), g.P * sizeof(Share), g);
     return EBSP_OK;
 }
@@ -287,6 +350,15 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
     return dtype == EBSP_BF16 ? ff_forward<__bf16>(f, st) : dtype == EBSP_F16 ? ff_forward<_Float16>(f, st) : ff_forward<float>(f, st);
 }
 
+size_t ebsp_gated_ff_split_workspace_bytes(int64_t M, int64_t K, int64_t F, int32_t dtype)
+{
+    const size_t units = ebsp_gated_ff_workspace_bytes(M, F, dtype);
+    if (!units || K < 0 || K >= SIZE_MAX_DIM) return units;
+    const int size = element_size(dtype);
+    const size_t x = partial_bytes(M, K, 1, dx_cut(M, K, F, size)), w = partial_bytes(F, K, 2, dw_cut(M, K, F, size));
+    return units + (x > w ? x : w);
+}
+
 size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype)
 {
     const int size = element_size(dtype);
@@ -317,7 +389,7 @@ int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t 
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
     auto run = dtype == EBSP_BF16 ? ff_backward<__bf16> : dtype == EBSP_F16 ? ff_backward<_Float16> : ff_backward<float>;
-    return run(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldg, M, K, F, act, dx, lddx, dwg, dwu, lddw, workspace, st);
+    return run(dh, lddh, x, ldx, wg, ldwg, wu, ldwu, g, u, ldg, M, K, F, act, dx, lddx, dwg, dwu, lddw, workspace, workspace_bytes, st);
 }
 
 size_t ebsp_distill_workspace_bytes(int64_t N, int64_t V, int32_t dtype)

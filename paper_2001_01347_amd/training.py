@@ -18,7 +18,8 @@ from .zipline import ZipLineError, _check_buffer, _check_workspace
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
-EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_workspace_bytes", "ebsp_gated_ff_backward", "ebsp_distill_workspace_bytes",
+EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_workspace_bytes",
+           "ebsp_gated_ff_split_workspace_bytes", "ebsp_gated_ff_backward", "ebsp_distill_workspace_bytes",
            "ebsp_distill_forward", "ebsp_distill_backward", "ebsp_distill_loss_grad", "ebsp_merge_pushes")
 
 STATUS_RANGE = 4          # a row's index or label lies beyond the vocabulary
@@ -37,6 +38,8 @@ def load() -> ctypes.CDLL:
         lib.ebsp_gated_ff_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp]
         lib.ebsp_gated_ff_workspace_bytes.restype = sz
         lib.ebsp_gated_ff_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.ebsp_gated_ff_split_workspace_bytes.restype = sz
+        lib.ebsp_gated_ff_split_workspace_bytes.argtypes = [i64, i64, i64, i32]
         lib.ebsp_gated_ff_backward.restype = c_int
         lib.ebsp_gated_ff_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp,
                                                i64, vp, sz, vp]
@@ -143,6 +146,10 @@ def ebsp_gated_ff_workspace_bytes(M: int, F: int, dtype: torch.dtype) -> int:
     return int(load().ebsp_gated_ff_workspace_bytes(M, F, DTYPES[dtype]))
 
 
+def ebsp_gated_ff_split_workspace_bytes(M: int, K: int, F: int, dtype: torch.dtype) -> int:
+    return int(load().ebsp_gated_ff_split_workspace_bytes(M, K, F, DTYPES[dtype]))
+
+
 def ebsp_gated_ff_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, g: torch.Tensor, u: torch.Tensor,
                            act: str = "silu", dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
                            dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
@@ -160,10 +167,11 @@ def ebsp_gated_ff_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, 
     dx = _output("dx", dx, dev, dt, (M, K)) if want_dx else None
     dwg = _output("dwg", dwg, dev, dt, (F, K)) if want_dw else None
     dwu = _output("dwu", dwu, dev, dt, (F, K)) if want_dw else None
-    need = ebsp_gated_ff_workspace_bytes(M, F, dt)
     if workspace is None:
+        need = ebsp_gated_ff_split_workspace_bytes(M, K, F, dt)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    _check_workspace(workspace, dev, need)
+    else:
+        _check_workspace(workspace, dev, ebsp_gated_ff_workspace_bytes(M, F, dt))
     ptr = [None if t is None else t.data_ptr() for t in (dx, dwg, dwu)]
     _call("ebsp_gated_ff_backward", dev, dh.data_ptr(), lddh, *operands, g.data_ptr(), u.data_ptr(), ldg, M, K, F, code, act,
           ptr[0], K, ptr[1], ptr[2], K, workspace.data_ptr(), workspace.numel())
@@ -327,7 +335,11 @@ def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "si
     if not isinstance(x, torch.Tensor) or x.dim() < 1:
         raise ValueError("x must be a tensor of shape [..., K]")
     rows = _plain_rows(x.reshape(x.shape[:-1].numel(), x.shape[-1]))
-    return _GatedFF.apply(rows, wg, wu, act).reshape(*x.shape[:-1], wg.shape[0])
+    if torch.is_grad_enabled():
+        h = _GatedFF.apply(rows, wg, wu, act)
+    else:
+        h = ebsp_gated_ff_forward(rows, wg, wu, act)[0]                      # (autograd would have g and u saved)
+    return h.reshape(*x.shape[:-1], wg.shape[0])
 
 
 class _Distill(torch.autograd.Function):

@@ -262,6 +262,27 @@ def test_streams_and_graphs(tr):
             assert torch.equal(a, b)
 
 
+# Few tokens or few units (sums shared out inside a workgroup), gradients whose sums are cut (dx of few tokens, weights' gradients of many),
+# large tiles of cut sums.
+@pytest.mark.parametrize("M,K,F", [(9, 1024, 48), (16, 1000, 160), (24, 640, 2000), (64, 200, 6000), (80, 2050, 500), (129, 90, 1500), (3000, 64, 72),
+                                   (2100, 130, 200), (6000, 40, 9), (4200, 1030, 300)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cut_sums(tr, M, K, F, dtype):
+    x, wg, wu, dh = _inputs(M, K, F, dtype, seed=20)
+    ref = Reference("silu", x, wg, wu, dh)
+    h, g, u = tr.ebsp_gated_ff_forward(x, wg, wu, save=True)
+    whole = torch.empty(max(tr.ebsp_gated_ff_workspace_bytes(M, F, dtype), 256), dtype=torch.uint8, device="cuda")
+    for workspace in (None, whole):                                          # in parts, and with room for none
+        _compare((h, *tr.ebsp_gated_ff_backward(dh, x, wg, wu, g, u, workspace=workspace)), ref, ("h", "dx", "dwg", "dwu"))
+
+
+def test_cut_sums_large_tiles(tr):
+    for M, K, F in ((1300, 1300, 6200), (16400, 1032, 770)):                 # 36 large tiles of dx, 40 of dW
+        x, wg, wu, dh = _inputs(M, K, F, torch.bfloat16, seed=21)
+        ref = Reference("gelu", x, wg, wu, dh)
+        _compare(_step(tr, "gelu", x, wg, wu, dh), ref, ("h", "dx", "dwg", "dwu"))
+
+
 def test_binding_refuses(tr):
     x, wg, wu, dh = _inputs(8, 16, 24, torch.bfloat16)
     h, g, u = tr.ebsp_gated_ff_forward(x, wg, wu, save=True)

@@ -84,6 +84,18 @@ def test_gated_ff_workspace(lib):
     assert training.ebsp_gated_ff_workspace_bytes(4, 32, __import__("torch").bfloat16) == 512
 
 
+def test_gated_ff_split_workspace(lib):
+    from paper_2001_01347_amd import training
+    least, split = lib.ebsp_gated_ff_workspace_bytes, lib.ebsp_gated_ff_split_workspace_bytes
+    for M, K, F in ((1, 4096, 12288), (64, 1024, 2048), (8192, 64, 64), (8192, 4096, 12288), (8, 8, 8), (0, 8, 8), (1, 0, 512)):
+        for dtype in (BF16, F16, F32):
+            assert split(M, K, F, dtype) >= least(M, F, dtype) and split(M, K, F, dtype) % 256 == 0
+    assert split(1, 4096, 12288, BF16) > least(1, 12288, BF16)                                       # one row of dx, summed in parts
+    assert split(8192, 4096, 12288, BF16) == least(8192, 12288, BF16) and split(8, 8, 8, BF16) == least(8, 8, BF16)
+    assert split(4, 8, 32, 3) == 0 and split(-1, 8, 32, BF16) == 0
+    assert training.ebsp_gated_ff_split_workspace_bytes(8, 8, 8, __import__("torch").bfloat16) == 256
+
+
 def test_a_valid_call_without_a_gfx950_fails_loudly(lib):
     import torch
     if torch.cuda.is_available():
