@@ -11,6 +11,7 @@ typedef uint32_t u32;
 typedef int Word4 __attribute__((ext_vector_type(4), may_alias));            // 16 bytes, the unit of every wide access
 typedef Word4 LooseWord4 __attribute__((aligned(2), may_alias));             // the same at any element's address: global memory takes it
 typedef int Word2 __attribute__((ext_vector_type(2), may_alias));
+typedef Word2 LooseWord2 __attribute__((aligned(2), may_alias));
 typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));

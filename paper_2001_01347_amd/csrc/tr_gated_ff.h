@@ -64,7 +64,7 @@ struct FfForward {
     void* h;
     float *g, *u;                                                            // NULL where nothing is kept for a backward pass
     i64 ldh, ldg;
-    int act, wide_h, wide_g;
+    int act;
 };
 
 // Gate and up of the same units lie in one wave's squares, so h is formed in registers: one read of x for both products, and
@@ -96,10 +96,10 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[k][e] = activation(f.act, acc[j + k][i][e]) * acc[j + k + HALF][i][e];
-            store_pair((T*)f.h + m * f.ldh + n, h[0], h[1], have, f.wide_h, lane);
+            store_pair((T*)f.h + m * f.ldh + n, h[0], h[1], have, lane);
             if (f.g) {
-                store_pair(f.g + m * f.ldg + n, acc[j][i], acc[j + 1][i], have, f.wide_g, lane);
-                store_pair(f.u + m * f.ldg + n, acc[j + HALF][i], acc[j + 1 + HALF][i], have, f.wide_g, lane);
+                store_pair(f.g + m * f.ldg + n, acc[j][i], acc[j + 1][i], have, lane);
+                store_pair(f.u + m * f.ldg + n, acc[j + HALF][i], acc[j + 1 + HALF][i], have, lane);
             }
         }
     }
@@ -142,7 +142,6 @@ struct FfGradient {
     Operand a, b;
     void* out[2];                                                            // dWg and dWu, one for each half of the grid; or dx
     i64 ld[2];
-    int wide[2];
     int segments;                                                            // dx: 2, the sum runs over gate and up
     i64 rows;                                                                // of the result (a.index counts the padded ones too)
     float* partial;                                                          // sums in parts: [result][parts][rows][columns, padded to 4]
@@ -184,7 +183,7 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
                 if (n + (lane >> 4) * 4 < ld) *reinterpret_cast<Float4*>(p) = acc[j][i];
                 if (n + (lane >> 4) * 4 + 16 < ld) *reinterpret_cast<Float4*>(p + 16) = acc[j + 1][i];
             } else {
-                store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, f.wide[z], lane);
+                store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, lane);
             }
         }
     }
@@ -201,7 +200,7 @@ __global__ void __launch_bounds__(256) tr_ff_join_kernel(FfGradient f)
         const i64 m = at / (ld / 4), n = (at - m * (ld / 4)) * 4;
         Float4 sum = *reinterpret_cast<const Float4*>(partial + at * 4);
         for (int p = 1; p < f.parts; ++p) sum += *reinterpret_cast<const Float4*>(partial + (p * f.rows * ld + at * 4));
-        store4((T*)f.out[z] + m * f.ld[z] + n, sum, columns - n, f.wide[z]);
+        store4((T*)f.out[z] + m * f.ld[z] + n, sum, columns - n);
     }
 }
 
@@ -277,10 +276,10 @@ __global__ void __launch_bounds__(TF::NT, 4) tr_ff_few_kernel(FfForward f)
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
-        store4((T*)f.h + m * f.ldh + n, h, have, f.wide_h);
+        store4((T*)f.h + m * f.ldh + n, h, have);
         if (f.g) {
-            store4(f.g + m * f.ldg + n, g, have, f.wide_g);
-            store4(f.u + m * f.ldg + n, u, have, f.wide_g);
+            store4(f.g + m * f.ldg + n, g, have);
+            store4(f.u + m * f.ldg + n, u, have);
         }
     }
 }

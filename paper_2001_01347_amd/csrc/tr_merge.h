@@ -99,7 +99,6 @@ __device__ __forceinline__ void store_row(U* p, const float (&v)[N], i64 have)
 #pragma unroll
         for (int i = 0; i < PER; ++i) r.v[i] = from_float<U>(v[j + i]);
         if constexpr (WHOLE) {
-            typedef Word2 LooseWord2 __attribute__((aligned(2), may_alias));
             if constexpr (sizeof(U) * PER == 16) store_loose(p + j, r.four);
             else *reinterpret_cast<LooseWord2*>(p + j) = r.two;
         } else {

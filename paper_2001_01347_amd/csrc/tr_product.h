@@ -345,36 +345,32 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         }
 }
 
-// Four neighbouring results of one row, rounded once; `have` of them exist.  `wide`: the row's stride and address let four
-// be stored at once.
+// Four neighbouring results of one row, rounded once; `have` of them exist.  At any alignment: memory takes wide stores there too.
 template <class T>
-__device__ __forceinline__ void store4(T* p, Float4 v, i64 have, bool wide)
+__device__ __forceinline__ void store4(T* p, Float4 v, i64 have)
 {
-    alignas(16) T r[4];
+    union { T r[4]; Word2 two; Word4 four; } u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = from_float<T>(v[i]);
-    if (wide && have >= 4) {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<Word2*>(p) = *reinterpret_cast<Word2*>(r);
-        } else {
-            *reinterpret_cast<Word4*>(p) = *reinterpret_cast<Word4*>(r);
-        }
+    for (int i = 0; i < 4; ++i) u.r[i] = from_float<T>(v[i]);
+    if (have >= 4) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<LooseWord2*>(p) = u.two;
+        else store_loose(p, u.four);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (i < have) p[i] = r[i];
+        if (i < have) p[i] = u.r[i];
 }
 
 // Two squares side by side of 16 rows: a lane has row lane % 16, columns (lane / 16) * 4 and on of either.  `p` is the lane's
 // row at the first square's first column, of which `have` columns exist.  For 16-bit results lanes 16 apart exchange
-// halves, so that each has eight neighbouring columns of one square and a row's 64 bytes go out at once (`wide`: eight can be stored at once).
+// halves, so that each has eight neighbouring columns of one square and a row's 64 bytes go out at once.
 template <class T>
-__device__ __forceinline__ void store_pair(T* p, Float4 first, Float4 second, i64 have, bool wide, int lane)
+__device__ __forceinline__ void store_pair(T* p, Float4 first, Float4 second, i64 have, int lane)
 {
     const int g = lane >> 4;
     if constexpr (sizeof(T) == 2) {
-        if (wide && have >= 32) {
+        if (have >= 32) {
             union { T v[4]; int w[2]; } a, b;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -388,12 +384,12 @@ __device__ __forceinline__ void store_pair(T* p, Float4 first, Float4 second, i6
                 out[i] = (int)r[0];
                 out[2 + i] = (int)r[1];
             }
-            *reinterpret_cast<Word4*>(p + (g & 1) * 16 + (g >> 1) * 8) = out;
+            store_loose(p + (g & 1) * 16 + (g >> 1) * 8, out);
             return;
         }
     }
-    store4(p + g * 4, first, have - g * 4, wide);
-    store4(p + 16 + g * 4, second, have - 16 - g * 4, wide);
+    store4(p + g * 4, first, have - g * 4);
+    store4(p + 16 + g * 4, second, have - 16 - g * 4);
 }
 
 }  // namespace

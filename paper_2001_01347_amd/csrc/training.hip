@@ -39,9 +39,6 @@ int element_size(int dtype) { return dtype == EBSP_BF16 || dtype == EBSP_F16 ? 2
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-// 16 bytes of neighbouring elements can be stored at once.
-int wide_rows(const void* p, i64 ld, int size) { return aligned(p, 16) && ld % (16 / size) == 0; }
-
 i64 padded_units(i64 F, int size)
 {
     const i64 n = 16 / size;
@@ -189,10 +186,8 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
     Cut cx = dx_cut(M, K, F, sizeof(T)), cw = dw_cut(M, K, F, sizeof(T));
     if (workspace_bytes < units + partial_bytes(M, K, 1, cx)) cx.parts = 1;
     if (workspace_bytes < units + partial_bytes(F, K, 2, cw)) cw.parts = 1;
-    const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0},
-                             {wide_rows(dx, lddx, sizeof(T)), 0}, 2, M, partial, cx.parts, cx.large};
-    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw},
-                             {wide_rows(dwg, lddw, sizeof(T)), wide_rows(dwu, lddw, sizeof(T))}, 1, F, partial, cw.parts, cw.large};
+    const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0}, 2, M, partial, cx.parts, cx.large};
+    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw}, 1, F, partial, cw.parts, cw.large};
     for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
         const i64 chunks = M * (ldd / PER_WORD4<T>);
         if (launch && chunks > 0) {
@@ -344,8 +339,7 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
     if (!aligned(x, size) || !aligned(wg, size) || !aligned(wu, size) || !aligned(h, size) || !aligned(g, 4) || !aligned(u, 4))
         return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
     if (int rc = check_device()) return rc;
-    FfForward f = {{{x, x}, {ldx, ldx}, M, K}, {{wg, wu}, {ldwg, ldwu}, F, K}, h, g, u, ldh, ldg, act,
-                   wide_rows(h, ldh, size), g ? wide_rows(g, ldg, 4) && wide_rows(u, ldg, 4) : 0};
+    FfForward f = {{{x, x}, {ldx, ldx}, M, K}, {{wg, wu}, {ldwg, ldwu}, F, K}, h, g, u, ldh, ldg, act};
     hipStream_t st = (hipStream_t)stream;
     return dtype == EBSP_BF16 ? ff_forward<__bf16>(f, st) : dtype == EBSP_F16 ? ff_forward<_Float16>(f, st) : ff_forward<float>(f, st);
 }
