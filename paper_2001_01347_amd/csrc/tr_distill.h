@@ -75,8 +75,13 @@ __device__ __forceinline__ T block_reduce(T v, T* shared, F&& join)
     return v;
 }
 
+constexpr int SEEN_BITS = 15, TWICE_MAX = 32;
+
 // A row's entries in shared memory.
-struct Entries {
+struct alignas(16) Entries {
+    u32 seen[1 << (SEEN_BITS - 5)];              // a bit for every value of an index' hash
+    int twice[TWICE_MAX];                        // indices that found their bit set
+    int twice_count, label_taken;
     int index[TOP_MAX];                          // -1: padding
     float q[TOP_MAX], s[TOP_MAX];                // the teacher's logit, later its weight; the student's logit
     Sums sums[16];
@@ -248,19 +253,51 @@ __device__ __forceinline__ Word4 slope_word(const Slope& g, Word4 raw)
     return w.raw;
 }
 
+// Which indices stand in a row more than once, for write_places: all but the first that sets a hash's bit are listed, and with them
+// a few whose hash is another's.  A barrier lies between the two steps, and another before the list is used.
+template <int NT>
+__device__ __forceinline__ void clear_places(Entries& e)
+{
+    for (int w = threadIdx.x; w < (1 << (SEEN_BITS - 7)); w += NT) reinterpret_cast<Word4*>(e.seen)[w] = Word4{0, 0, 0, 0};
+    if (threadIdx.x == 0) e.twice_count = e.label_taken = 0;
+}
+
+template <int NT>
+__device__ __forceinline__ void mark_places(const Distill& d, const Row& row, Entries& e)
+{
+    for (int k = threadIdx.x; k < d.top; k += NT) {
+        const int i = e.index[k];
+        if (i < 0) continue;
+        const u32 h = ((u32)i * 2654435761u) >> (32 - SEEN_BITS), bit = 1u << (h & 31);
+        if (atomicOr(&e.seen[h >> 5], bit) & bit) {
+            const int at = atomicAdd(&e.twice_count, 1);
+            if (at < TWICE_MAX) e.twice[at] = i;
+        }
+        if (i == row.label) e.label_taken = 1;
+    }
+}
+
 // The places of the entries and of the label, whose gradients have further terms, written over what stands there.  Entries of
-// one index add up, in the order of k, and all write the same value.
+// one index add up, in the order of k, and all write the same value; an entry at the label's place writes for both.  (Looking through all entries
+// for those of the same index took 38 of 57 us for 4096 rows of 1000 with 256 entries, 156 of 176 for 512 of 8000 with 1000.)
 template <int NT, class T, Second S>
 __device__ __forceinline__ void write_places(const Distill& d, const Row& row, const Entries& e, i64 v0, i64 v1, const Slope& g)
 {
     if (g.how < 0) return;
     T* grad = (T*)d.grad + row.n * d.ldd;
+    const int listed = e.twice_count;
     for (int k = threadIdx.x; k <= d.top; k += NT) {
         const bool own = k == d.top;                                         // the label's turn
         const int i = own ? row.label : e.index[k];
         if (i < v0 || i >= v1) continue;
-        float q = 0.f;
-        for (int j = 0; j < d.top; ++j) q += e.index[j] == i ? e.q[j] : 0.f;
+        if (own && e.label_taken) continue;
+        bool others = listed > TWICE_MAX;
+        for (int j = 0; j < min(listed, TWICE_MAX); ++j) others |= e.twice[j] == i;
+        float q = own ? 0.f : e.q[k];
+        if (others && !own) {
+            q = 0.f;
+            for (int j = 0; j < d.top; ++j) q += e.index[j] == i ? e.q[j] : 0.f;
+        }
         const float s = own ? row.label_logit : e.s[k];
         float x = g.how == 2 ? slope_at<S, 2>(g, s) : g.how == 0 ? slope_at<S, 0>(g, s) : slope_at<S, 1>(g, s);
         if (g.a != 0.f) x -= g.a * q;
@@ -405,9 +442,9 @@ __device__ __forceinline__ void forget_floats(Word4 (&w)[N])
 }
 
 // Loss and statistics, and with GRAD the gradient too: one workgroup a row.  The row's first NT x HELD words stay in registers from the one load to
-// the gradient, a row of 128000 16-bit logits in half of a CU's; only what lies behind is read twice.  While one CU computes others load and
-// store; with the labels' term the vector ALU is busy half of the time, memory two thirds (4096 rows of 128000, bf16: 602 us, with two reads and
-// a running maximum 704).
+// the gradient; only what lies behind is read twice.  A workgroup does one thing at a time, so a CU needs several to keep memory busy while
+// one of them computes: rows that fill a CU's registers are cut at half (4096 rows of 128000, bf16: 487 us, 4.3 TB/s, where one workgroup held
+// the whole row 597).
 template <int NT, class T, bool GRAD, Second S>
 __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
 {
@@ -430,6 +467,7 @@ __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
     if (has_last) last = read_logits(s, whole, d.V);
     float top;
     bool bad;
+    if constexpr (GRAD) clear_places<NT>(e);
     Row row = read_entries<NT, T>(d, n, 0, d.V, e, top, bad);
     struct Found { float top, bad, m; };
     Found f = {top, bad ? 1.f : 0.f, rest.m};
@@ -445,6 +483,7 @@ __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
                          [](Found a, Found b) { return Found{larger(a.top, b.top), fmaxf(a.bad, b.bad), fmaxf(a.m, b.m)}; });
     if (threadIdx.x == 0 && d.status) d.status[n] = f.bad > 0.f ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
     row.any = has_entries(d, f.top);
+    if constexpr (GRAD) mark_places<NT>(d, row, e);
     Sums sums = joined(rest, Sums{f.m, 0.f, 0.f}, ct);                       // (f.m is the larger)
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
@@ -536,7 +575,9 @@ __global__ void __launch_bounds__(NT) tr_distill_gradient_kernel(Distill d)
     i64 v0, v1;
     part_range(d, blockIdx.x % d.splits, N, v0, v1);
     const T* s = (const T*)d.logits + n * d.ld;
+    clear_places<NT>(e);
     const Row row = read_row<NT, T>(d, n, v0, v1, e, false);
+    mark_places<NT>(d, row, e);                                              // (read_row has barriers)
     const Slope g = slope_of(d, row, d.stats[n * 3], d.stats[n * 3 + 1], d.stats[n * 3 + 2]);
     T* out = (T*)d.grad + n * d.ldd;
     __builtin_amdgcn_s_waitcnt(0);                                           // in place: the logits of the places have been read

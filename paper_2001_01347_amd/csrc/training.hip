@@ -247,11 +247,14 @@ template <class T>
 int distill_loss(Distill d, bool grad, hipStream_t st)
 {
     if (d.splits == 1) {
-        // A gradient wants the whole row in registers.  The loss alone of many rows runs better from several small workgroups a CU, whatever
-        // of a row they have to stream (600 x 128000 52 -> 35 us).
-        const bool large = d.V / PER_WORD4<T> > 2048;
-        if (grad) return large ? distill_rows<1024, T, true>(d, st) : distill_rows<256, T, true>(d, st);
-        return large && d.N <= 256 ? distill_rows<1024, T, false>(d, st) : distill_rows<256, T, false>(d, st);
+        // Workgroups that hold a row, or half of one that would fill a CU's registers.  bf16, loss and gradient, us with 1024 / 512 / 256 / 128 threads:
+        // 4096 x 128000 597 / 487 / 599 / -, 4096 x 64000 347 / 212 / 248 / -, 4096 x 32000 276 / 162 / 128 / -, 512 x 16000 - / 17 / 17 / 20,
+        // 4096 x 8000 - / 86 / 49 / 42, 4096 x 1000 - / 74 / 37 / 21; f32, 2048 x 128000 514 / 579 / 634 / -.  The loss alone streams what it does not hold:
+        // 1024 x 128000 84 / 56 / 53 / 51, 400 x 128000 36 / 25 / 26 / 41, 128 x 128000 17 / 17 / 20 / 29, 4096 x 1000 87 / 38 / 19 / 15.
+        const i64 words = (d.V + PER_WORD4<T> - 1) / PER_WORD4<T>;
+        if (words <= 1024) return grad ? distill_rows<128, T, true>(d, st) : distill_rows<128, T, false>(d, st);
+        if (grad) return words <= 4096 ? distill_rows<256, T, true>(d, st) : words <= 16384 ? distill_rows<512, T, true>(d, st) : distill_rows<1024, T, true>(d, st);
+        return words > 2048 && d.N <= 384 ? distill_rows<512, T, false>(d, st) : distill_rows<256, T, false>(d, st);
     }
     LAUNCH((tr_distill_part_kernel<256, T>), dim3((unsigned)(d.N * d.splits)), dim3(256), d);
     LAUNCH((tr_distill_join_kernel<256, T>), dim3((unsigned)d.N), dim3(256), d);

@@ -176,6 +176,23 @@ def test_entries_of_one_place_add_up(tr, N):
     check(tr, logits, index, values, labels, dloss, 2.0, 1.0, 0.5)
 
 
+@pytest.mark.parametrize("N,V,K", [(5, 40, 1000), (300, 3000, 300), (130, 20000, 64), (3, 90000, 1024)])
+def test_few_and_many_entries_of_one_place(tr, N, V, K):
+    """A few indices twice, more than a list of such has room for, all of one; labels at such places."""
+    logits, index, values, labels, dloss = make(N, V, K, torch.bfloat16, seed=12, padding=False)
+    index[1::3, 5] = index[1::3, 17]
+    index[2::3, :K // 2] = index[2::3, K - K // 2:]
+    index[0] = index[0, 3]
+    labels = torch.where(torch.arange(N, device="cuda") % 2 == 0, index[:, 5].long().clamp(min=-1), labels)
+    check(tr, logits, index, values, labels, dloss, 2.0, 0.75, 0.5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V", [(140, 1), (140, 4099), (140, 8200), (140, 33000), (520, 33001), (140, 70003), (100, 140001)])
+def test_rows_of_every_workgroup(tr, N, V, dtype):
+    check(tr, *make(N, V, min(V, 20), dtype, seed=13), 1.5, 0.75, 0.5)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N", [4, 300])
 def test_masked_places(tr, dtype, N):
