@@ -96,7 +96,11 @@ __device__ __forceinline__ Word4 fetch_chunk(const Operand& o, int which, i64 i0
 // The same tile straight from memory to shared memory, no registers between: the shared side of such a load is 16 bytes a lane in
 // lane order, so the lanes' order is permuted on the memory side.  Rows (columns) beyond the operand repeat its last ones; what comes
 // of them is not stored.  Needs whole 16-byte chunks: operand_direct() on the host.
-template <class T, Layout L, int BI, int NT, int PAIRED>
+//
+// LOOSE: the same through registers, whatever the alignment and the length; a chunk of a COLS tile that passes the end of its row takes what
+// comes behind it (nothing that comes of that is stored either).  That stays inside the operand for all rows but the last:
+// loose_steps() says how far.
+template <class T, Layout L, int BI, int NT, int PAIRED, bool LOOSE>
 struct DirectTile {
     static constexpr int P = BI * 8 / NT, N = PER_WORD4<T>;
     const char* base;
@@ -115,8 +119,8 @@ struct DirectTile {
                 const i64 last = o.index - 1 - i0;
                 off[i] = (u32)((i64)(row < last ? row : last) * o.stride(which) * (i64)sizeof(T)) + chunk * 16;
             } else {
-                const i64 last = o.index - N - i0, col = (i64)chunk * N;
-                off[i] = (u32)((i64)row * o.ld[0] * (i64)sizeof(T) + (col < last ? col : last) * (i64)sizeof(T));
+                const i64 left = o.index - i0, col = (i64)chunk * N, at = LOOSE ? (col < left ? col : 0) : (col < left - N ? col : left - N);
+                off[i] = (u32)((i64)row * o.ld[0] * (i64)sizeof(T) + at * (i64)sizeof(T));
             }
         }
         base = (const char*)o.p[0] + (L == ROWS ? i0 * o.ld[0] : i0) * (i64)sizeof(T);
@@ -124,16 +128,36 @@ struct DirectTile {
         step = L == ROWS ? 128 : (i64)(128 / sizeof(T)) * o.ld[0] * (i64)sizeof(T);
     }
 
+    __device__ __forceinline__ bool second(int seg, int wave, int i) const
+    {
+        return PAIRED > 0 ? (i * (NT / 8) + wave * 8) % (PAIRED > 0 ? PAIRED * 16 : 1) >= PAIRED * 8 : seg != 0;
+    }
+
+    __device__ __forceinline__ Word4 load(int seg, int s, int wave, int i) const
+    {
+        return load_loose((const T*)(base + s * step + (second(seg, wave, i) ? other : 0) + off[i]));
+    }
+
     // The i-th of a thread's loads of step `s` of segment `seg`, into the slot at `lds`.  (Buffer loads, not global ones: those count as
     // accesses that may go to either memory, and the compiler then waits for all reads of shared memory where it needs one.)
     __device__ __forceinline__ void bring(char* lds, int seg, int s, int wave, int i) const
     {
         typedef __attribute__((address_space(3))) void LdsAny;
-        const bool second = PAIRED > 0 ? (i * (NT / 8) + wave * 8) % (PAIRED > 0 ? PAIRED * 16 : 1) >= PAIRED * 8 : seg != 0;
-        const auto resource = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + s * step + (second ? other : 0)), 0, -1, 0x00020000);
+        const auto resource = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + s * step + (second(seg, wave, i) ? other : 0)), 0, -1, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(resource, (LdsAny*)(lds + (i * NT + wave * 64) * 16), 16, (int)off[i], 0, 0, 0);
     }
 };
+
+// Steps at a segment's beginning that a LOOSE tile may take: whole ones that do not come to the last row of COLS, whose rows hold a chunk at
+// least and whose offsets fit 31 bits.
+template <class T, Layout L>
+__device__ __forceinline__ int loose_steps(const Operand& o)
+{
+    constexpr int BK = 128 / (int)sizeof(T);
+    const i64 far = o.ld[0] > o.ld[1] ? o.ld[0] : o.ld[1];
+    if (far * (i64)sizeof(T) * 256 > 0x7fffffffll || (L == COLS && o.index < PER_WORD4<T>)) return 0;
+    return (int)((L == COLS ? o.depth - 1 : o.depth) / BK);
+}
 
 // Four rows of 16 16-bit elements each that 16 lanes read, 8 bytes a lane, come back as columns.  (Through a restrict pointer: without any
 // aliasing facts the compiler waits for every load to shared memory under way before such a read.  Which loads have to be
@@ -259,7 +283,19 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
     if constexpr (!DIRECT) {
         const int all = steps * segments, from = (int)((i64)all * part / parts), total = (int)((i64)all * (part + 1) / parts) - from;
         if (total == 0) return;
-        auto fetch_step = [&](int s) { fetch(s >= steps, s >= steps ? s - steps : s); };
+        DirectTile<T, LA, BM, NT, 0, true> da;
+        DirectTile<T, LB, BN, NT, PAIRED, true> db;
+        da.init(a, m0);
+        db.init(b, n0);
+        const int la = loose_steps<T, LA>(a), lb = loose_steps<T, LB>(b), loose = la < lb ? la : lb;
+        auto fetch_step = [&](int s) {
+            const int seg = s >= steps, k = seg ? s - steps : s;
+            if (k >= loose) return fetch(seg, k);
+#pragma unroll
+            for (int i = 0; i < PA; ++i) ra[i] = da.load(seg, k, wave, i);
+#pragma unroll
+            for (int i = 0; i < PB; ++i) rb[i] = db.load(seg, k, wave, i);
+        };
         fetch_step(from);
         put(0);
         __syncthreads();
@@ -275,8 +311,8 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
     const int whole = (int)((a.depth < b.depth ? a.depth : b.depth) / BK), all = whole * segments;
     const int from = (int)((i64)all * part / parts), total = (int)((i64)all * (part + 1) / parts) - from;
     if (total > 0) {
-        DirectTile<T, LA, BM, NT, 0> da;
-        DirectTile<T, LB, BN, NT, PAIRED> db;
+        DirectTile<T, LA, BM, NT, 0, false> da;
+        DirectTile<T, LB, BN, NT, PAIRED, false> db;
         da.init(a, m0);
         db.init(b, n0);
         constexpr int LOADS = PA + PB;
