@@ -22,6 +22,8 @@ namespace {
 
 enum Layout { ROWS, COLS };
 
+template <int N> struct Int { static constexpr int value = N; };
+
 template <class T, int WM_, int WN_, int FM_, int FN_>
 struct Tile {
     static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_;
@@ -249,20 +251,20 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
 
     const i64 depth = a.depth > b.depth ? a.depth : b.depth;
     const int steps = (int)((depth + BK - 1) / BK);
-    Word4 ra[PA], rb[PB];
-    auto fetch = [&](int seg, int s) {
+    struct Step { Word4 a[PA], b[PB]; };                                     // what a thread brings in a step, on its way through registers
+    auto fetch = [&](Step& r, int seg, int s) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) ra[i] = fetch_chunk<T, LA, BM, 0, DIRECT>(a, seg, m0, (i64)s * BK, i * NT + tid);
+        for (int i = 0; i < PA; ++i) r.a[i] = fetch_chunk<T, LA, BM, 0, DIRECT>(a, seg, m0, (i64)s * BK, i * NT + tid);
 #pragma unroll
-        for (int i = 0; i < PB; ++i) rb[i] = fetch_chunk<T, LB, BN, PAIRED, DIRECT>(b, seg, n0, (i64)s * BK, i * NT + tid);
+        for (int i = 0; i < PB; ++i) r.b[i] = fetch_chunk<T, LB, BN, PAIRED, DIRECT>(b, seg, n0, (i64)s * BK, i * NT + tid);
     };
     auto place_a = [&](int slot) { return lds + slot * TL::SLOT_A; };
     auto place_b = [&](int slot) { return lds + 3 * TL::SLOT_A + slot * TL::SLOT_B; };
-    auto put = [&](int slot) {
+    auto put = [&](const Step& r, int slot) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) *reinterpret_cast<Word4*>(place_a(slot) + (i * NT + tid) * 16) = ra[i];
+        for (int i = 0; i < PA; ++i) *reinterpret_cast<Word4*>(place_a(slot) + (i * NT + tid) * 16) = r.a[i];
 #pragma unroll
-        for (int i = 0; i < PB; ++i) *reinterpret_cast<Word4*>(place_b(slot) + (i * NT + tid) * 16) = rb[i];
+        for (int i = 0; i < PB; ++i) *reinterpret_cast<Word4*>(place_b(slot) + (i * NT + tid) * 16) = r.b[i];
     };
     auto square_a = [&](int slot, int i, int ks) { return read_square<T, LA, BM>(place_a(slot), (wm * FM + i) * 16, ks, lane); };
     auto square_b = [&](int slot, int j, int ks) { return read_square<T, LB, BN>(place_b(slot), (wn * FN + j) * 16, ks, lane); };
@@ -288,22 +290,41 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
         da.init(a, m0);
         db.init(b, n0);
         const int la = loose_steps<T, LA>(a), lb = loose_steps<T, LB>(b), loose = la < lb ? la : lb;
-        auto fetch_step = [&](int s) {
+        Step set[2];                                                         // two steps under way: one alone does not cover memory's latency
+        auto bring_loose = [&](Step& r, int s) {
             const int seg = s >= steps, k = seg ? s - steps : s;
-            if (k >= loose) return fetch(seg, k);
 #pragma unroll
-            for (int i = 0; i < PA; ++i) ra[i] = da.load(seg, k, wave, i);
+            for (int i = 0; i < PA; ++i) r.a[i] = da.load(seg, k, wave, i);
 #pragma unroll
-            for (int i = 0; i < PB; ++i) rb[i] = db.load(seg, k, wave, i);
+            for (int i = 0; i < PB; ++i) r.b[i] = db.load(seg, k, wave, i);
         };
-        fetch_step(from);
-        put(0);
-        __syncthreads();
-        for (int s = 0; s < total; ++s) {
-            if (s + 1 < total) fetch_step(from + s + 1);
-            products(s & 1);
-            if (s + 1 < total) put(~s & 1);                                  // what nothing reads any more
+        auto bring_step = [&](Step& r, int s) {
+            const int seg = s >= steps, k = seg ? s - steps : s;
+            if (k < loose) bring_loose(r, s);
+            else fetch(r, seg, k);
+        };
+        // Step s of the stretch (its data is in shared memory): the one after the next is sent for, the next put in place.
+        auto step = [&](auto odd, int s, auto&& bring) {
+            constexpr int O = decltype(odd)::value;
+            bring(set[O], s + 2);
+            products(O);
+            if (s + 1 < total) put(set[O ^ 1], O ^ 1);                       // what nothing reads any more
             __syncthreads();
+        };
+        bring_step(set[0], from);
+        if (total > 1) bring_step(set[1], from + 1);
+        put(set[0], 0);
+        __syncthreads();
+        int s = 0;
+        const int plain = (from < steps ? min(from + total, loose) : min(from + total, steps + loose)) - from;   // steps that need no checks
+        for (; s + 4 <= plain; s += 2) {
+            step(Int<0>(), s, [&](Step& r, int t) { bring_loose(r, from + t); });
+            step(Int<1>(), s + 1, [&](Step& r, int t) { bring_loose(r, from + t); });
+        }
+        for (; s < total; s += 2) {
+            auto checked = [&](Step& r, int t) { if (t < total) bring_step(r, from + t); };
+            step(Int<0>(), s, checked);
+            if (s + 1 < total) step(Int<1>(), s + 1, checked);
         }
         return;
     }
@@ -373,9 +394,10 @@ __device__ __forceinline__ void product_tile(Float4 (&acc)[TL::FN][TL::FM], char
     if (whole < steps && part == parts - 1)
 #pragma unroll 1
         for (int seg = 0; seg < segments; ++seg) {
-            fetch(seg, whole);
+            Step r;
+            fetch(r, seg, whole);
             wait_and_meet<0, 0>();                                           // everything before has arrived and been read
-            put(0);
+            put(r, 0);
             __syncthreads();
             products(0);
         }
