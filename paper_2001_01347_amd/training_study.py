@@ -1,0 +1,124 @@
+"""BSP against ElasticBSP in training: a student distilled from a teacher by workers that meet at the searched barriers.
+
+    python -m paper_2001_01347_amd.training_study [--workers 8] [--supersteps 24] [--lookahead 15]
+
+One GPU plays all workers.  In every superstep the search (``zipline.ebsp_predict_zipline_batch``) gives each worker its
+iterations until the barrier; a worker runs them on its own copy of the weights (``training.gated_ff``, a projection to the
+vocabulary, ``training.distill_loss`` against the teacher's largest logits), and the server merges the changes weighted by the
+iterations (``training.ebsp_merge_pushes``), straight from what the search left on the device.  With a lookahead of 1 every worker
+does one iteration a superstep, which is BSP.  Data and weights are synthetic and seeded; times are the
+simulated workers', not this program's.
+"""
+from __future__ import annotations
+
+import argparse
+import sys
+from typing import Dict, List
+
+WIDTH, UNITS, VOCABULARY, TOP = 128, 320, 1000, 16
+BATCH = 64
+TEMPERATURE, KL_WEIGHT, CE_WEIGHT = 2.0, 0.9, 0.1
+LOCAL_LR, SERVER_LR, MOMENTUM = 2.0, 1.0, 0.5
+
+
+def _logits(parts, x):
+    from . import training
+    wg, wu, wo = parts
+    return training.gated_ff(x, wg, wu, "silu") @ wo.t()
+
+
+class Student:
+    """The weights in one flat float32 tensor, as the server keeps and merges them; ``views`` cuts a copy of them into matrices."""
+
+    SHAPES = ((UNITS, WIDTH), (UNITS, WIDTH), (VOCABULARY, UNITS))
+
+    @classmethod
+    def size(cls) -> int:
+        return sum(r * c for r, c in cls.SHAPES)
+
+    @classmethod
+    def initial(cls, gen):
+        import torch
+        return torch.cat([torch.randn(r * c, generator=gen, device=gen.device) * c ** -0.5 for r, c in cls.SHAPES])
+
+    @classmethod
+    def views(cls, flat):
+        out, at = [], 0
+        for r, c in cls.SHAPES:
+            out.append(flat[at:at + r * c].view(r, c))
+            at += r * c
+        return out
+
+
+def _teach(teacher, x):
+    """The teacher's largest logits for a batch, with their places, and its first choice as the label."""
+    import torch
+    with torch.no_grad():
+        values, index = torch.topk(_logits(Student.views(teacher), x).float(), TOP, dim=1)
+    return index, values.to(x.dtype), index[:, 0].contiguous()
+
+
+def _loss(parts, x, index, values, labels):
+    from . import training
+    return training.distill_loss(_logits(parts, x), index, values, TEMPERATURE, KL_WEIGHT, labels, CE_WEIGHT).mean()
+
+
+def train(workers: int = 8, supersteps: int = 24, lookahead: int = 15, seed: int = 0) -> List[Dict[str, float]]:
+    """One row per superstep: the barrier's time (us), the iterations done, and the server's loss on data that no worker saw."""
+    import torch
+    from . import training, workloads, zipline
+
+    dev, dtype = torch.device("cuda"), torch.bfloat16
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    teacher = Student.initial(gen).to(dtype)
+    server, velocity = Student.initial(gen), torch.zeros(Student.size(), device=dev)
+    pulled = server.to(dtype)
+    pushes = torch.empty((workers, Student.size()), dtype=dtype, device=dev)
+    held_x = torch.randn((256, WIDTH), generator=gen, device=dev).to(dtype)
+    held = _teach(teacher, held_x)
+
+    last_end, mean = workloads.make_supersteps(2, 1, instances=[0], jitter=0.0)  # 16 workers of 80 to 120 ms
+    last_end = torch.from_numpy(last_end[:, :workers]).contiguous().to(dev)
+    interval = torch.from_numpy(mean[0][:, :workers]).contiguous().to(dev)
+
+    rows = []
+    for s in range(supersteps):
+        barrier, iters, _, status = zipline.ebsp_predict_zipline_batch(last_end, interval, lookahead)
+        if int(status.max().item()) != 0:
+            raise zipline.ZipLineError("the search flagged the cluster")
+        counts = iters[0].tolist()                                           # the host runs the workers' loops
+        for p, count in enumerate(counts):
+            weights = pulled.float()
+            for _ in range(count):
+                leaves = [w.to(dtype).requires_grad_() for w in Student.views(weights)]
+                x = torch.randn((BATCH, WIDTH), generator=gen, device=dev).to(dtype)
+                _loss(leaves, x, *_teach(teacher, x)).backward()
+                for w, leaf in zip(Student.views(weights), leaves):
+                    w -= LOCAL_LR * leaf.grad
+            pushes[p] = weights - pulled.float()
+        training.ebsp_merge_pushes(server, pushes, iters[0], lr=SERVER_LR, momentum=MOMENTUM, velocity=velocity, out=server,
+                                   velocity_out=velocity, pull=pulled)
+        last_end = barrier[:, None].expand(1, workers).contiguous()          # all resume at the barrier
+        with torch.no_grad():
+            loss = _loss(Student.views(pulled), held_x, *held)
+        rows.append({"superstep": s, "barrier": float(barrier[0].item()), "iterations": float(sum(counts)), "loss": float(loss.item())})
+    return rows
+
+
+def main() -> int:
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--workers", type=int, default=8, choices=range(1, 17), metavar="1..16")
+    ap.add_argument("--supersteps", type=int, default=24)
+    ap.add_argument("--lookahead", type=int, default=15, help="predicted iterations per worker (R)")
+    args = ap.parse_args()
+    print("| | supersteps | iterations | time (s) | loss at the start | loss at the end |")
+    print("|---|---|---|---|---|---|")
+    for name, R in (("BSP", 1), (f"ElasticBSP, R = {args.lookahead}", args.lookahead)):
+        rows = train(args.workers, args.supersteps, R)
+        print(f"| {name} | {len(rows)} | {sum(r['iterations'] for r in rows):.0f} | {rows[-1]['barrier'] / 1e6:.2f} | {rows[0]['loss']:.4f} | "
+              f"{rows[-1]['loss']:.4f} |")
+    return 0
+
+
+if __name__ == "__main__":
+    sys.exit(main())
