@@ -442,20 +442,37 @@ __device__ __forceinline__ void forget_floats(Word4 (&w)[N])
 }
 
 // Loss and statistics, and with GRAD the gradient too: one workgroup a row.  The row's first NT x HELD words stay in registers from the one load to
-// the gradient; only what lies behind is read twice.  A workgroup does one thing at a time, so a CU needs several to keep memory busy while
-// one of them computes: rows that fill a CU's registers are cut at half (4096 rows of 128000, bf16: 487 us, 4.3 TB/s, where one workgroup held
-// the whole row 597).
+// the gradient, more of a long one in shared memory; only what lies behind is read twice.  A workgroup does one thing at a time, so a CU needs several to keep memory busy while
+// one of them computes: rows that fill a CU's registers are cut at half (4096 rows of 128000, bf16: 483 us, 4.3 TB/s, where one workgroup held
+// the whole row 597; with nothing in shared memory 487, and 2048 rows of 128000 in fp32 512 where it is 483 now).
 template <int NT, class T, bool GRAD, Second S>
 __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
 {
-    constexpr int N = PER_WORD4<T>, HELD = 16;
-    constexpr u32 STEP = NT * N;
+    constexpr int N = PER_WORD4<T>, HELD = 16, KEPT = !GRAD ? 0 : NT == 512 ? 7 : NT == 1024 ? 8 : 0;
+    constexpr u32 STEP = NT * N, BEHIND = (HELD + KEPT) * STEP;
     __shared__ Entries e;
+    __shared__ Word4 kept[KEPT > 0 ? KEPT * NT : 1];
     const i64 n = blockIdx.x;
     const T* s = (const T*)d.logits + n * d.ld;
     const float ct = LOG2E / d.temperature;
     Sums rest = {-FLT_MAX, 0.f, 0.f};
-    if (HELD * STEP < d.V) rest = part_sums<NT, T, S>(d, s, HELD * STEP, d.V);
+    if (BEHIND < d.V) rest = part_sums<NT, T, S>(d, s, BEHIND, d.V);
+    float kept_m = -FLT_MAX;
+    if constexpr (KEPT > 0) {
+        if (HELD * STEP < d.V) {
+            Word4 w[KEPT];
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j) {
+                const u32 v = threadIdx.x * N + (HELD + j) * STEP;
+                w[j] = v < d.V ? read_logits(s, v, d.V) : lowest_word<T>();
+            }
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j) {
+                kept[j * NT + threadIdx.x] = w[j];
+                kept_m = largest<T>(w[j], kept_m);
+            }
+        }
+    }
     __builtin_amdgcn_sched_barrier(0);                                       // (before the registers fill)
     // A word belongs to the row as a whole, or is the part that is left, which one thread has besides.
     const u32 v0 = threadIdx.x * N, whole = (u32)(d.V / N * N), end = min(whole, HELD * STEP);
@@ -470,7 +487,7 @@ __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
     if constexpr (GRAD) clear_places<NT>(e);
     Row row = read_entries<NT, T>(d, n, 0, d.V, e, top, bad);
     struct Found { float top, bad, m; };
-    Found f = {top, bad ? 1.f : 0.f, rest.m};
+    Found f = {top, bad ? 1.f : 0.f, fmaxf(rest.m, kept_m)};
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
         if (j * STEP < end) {
@@ -492,6 +509,9 @@ __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
             __builtin_amdgcn_sched_barrier(0);
         }
     if (has_last) add_exponentials<T, S>(sums, last, f.m, ct);
+    if constexpr (KEPT > 0)
+#pragma unroll 1
+        for (int j = 0; j < KEPT && (HELD + j) * STEP < d.V; ++j) add_exponentials<T, S>(sums, kept[j * NT + threadIdx.x], f.m, ct);
     struct Totals { float q, st, s1; };
     Totals t = {weigh_entries<NT>(d, row, e, f.top), sums.st, sums.s1};
     t = block_reduce<NT>(t, reinterpret_cast<Totals*>(e.sums), [](Totals a, Totals b) { return Totals{a.q + b.q, a.st + b.st, a.s1 + b.s1}; });
@@ -511,7 +531,13 @@ __global__ void __launch_bounds__(NT) tr_distill_row_kernel(Distill d)
             __builtin_amdgcn_sched_barrier(0);
         }
         if (has_last) write_gradient(out, whole, d.V, slope_word<T, S>(g, last));
-        for (i64 v = v0 + HELD * STEP; v < d.V; v += STEP) write_gradient(out, v, d.V, slope_word<T, S>(g, read_logits(s, v, d.V)));
+        if constexpr (KEPT > 0)
+#pragma unroll 1
+            for (int j = 0; j < KEPT; ++j) {
+                const u32 v = v0 + (HELD + j) * STEP;
+                if (v < d.V) write_gradient(out, v, d.V, slope_word<T, S>(g, kept[j * NT + threadIdx.x]));
+            }
+        for (i64 v = v0 + BEHIND; v < d.V; v += STEP) write_gradient(out, v, d.V, slope_word<T, S>(g, read_logits(s, v, d.V)));
         __builtin_amdgcn_s_waitcnt(0);                                       // stores to one address arrive in this order
         __syncthreads();
         write_places<NT, T, S>(d, row, e, 0, d.V, g);
