@@ -154,14 +154,13 @@ __host__ __device__ __forceinline__ i64 partial_ld(i64 columns) { return (column
 // long sums where tokens are few, dW where the matrices are small and tokens many; the grid's second axis cuts the sums then, and
 // the parts go to memory unrounded.
 template <class T, class TL, Layout LA, bool DIRECT>
-__global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
+__device__ __forceinline__ void gradient_tile(const FfGradient& f, u32 tile, int slice, char* lds)
 {
-    __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
     constexpr int FM = TL::FM, FN = TL::FN;
     const u32 tm = (u32)((f.rows + TL::BM - 1) / TL::BM), tn = (u32)((f.b.index + TL::BN - 1) / TL::BN);
     u32 bm, bn;
-    tile_of(blockIdx.x, tm, tn, bm, bn);
-    const int parts = f.parts, z = LA == COLS ? blockIdx.y / parts : 0, part = blockIdx.y - z * parts;
+    tile_of(tile, tm, tn, bm, bn);
+    const int parts = f.parts, z = LA == COLS ? slice / parts : 0, part = slice - z * parts;
     const Operand a = {{LA == COLS ? f.a.matrix(z) : f.a.p[0], f.a.p[1]}, {f.a.ld[0], f.a.ld[1]}, f.a.index, f.a.depth};
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * TL::BN;
     Float4 acc[FN][FM];
@@ -187,6 +186,24 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
             }
         }
     }
+}
+
+template <class T, class TL, Layout LA, bool DIRECT>
+__global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
+    gradient_tile<T, TL, LA, DIRECT>(f, blockIdx.x, blockIdx.y, lds);
+}
+
+// dx and dW side by side, dx's workgroups first: either alone leaves CUs without work at its end (forward and both gradients, us, one after the
+// other / so: bf16 1021 x 1000 x 2730 91 / 85, 2048 x 256 x 1024 50 / 39, 512 x 2048 x 4096 93 / 93; f32 1024 x 1024 x 2816 367 / 357).
+template <class T, class TL, bool DIRECT>
+__global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradients_kernel(FfGradient x, FfGradient w, u32 x_tiles, u32 x_all, u32 w_tiles)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
+    const u32 id = blockIdx.x;
+    if (id < x_all) gradient_tile<T, TL, ROWS, DIRECT>(x, id % x_tiles, id / x_tiles, lds);
+    else gradient_tile<T, TL, COLS, DIRECT>(w, (id - x_all) % w_tiles, (id - x_all) / w_tiles, lds);
 }
 
 // The parts of a result, added up in their order and rounded.

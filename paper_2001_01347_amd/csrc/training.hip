@@ -115,10 +115,13 @@ int ff_forward(const FfForward& f, hipStream_t st)
     return ff_forward_tiles<T, Tile<T, 2, 2, 4, 4>>(f, st);
 }
 
+template <class T, Layout LA>
+bool gradient_direct(const FfGradient& f) { return operand_direct(f.a, LA, sizeof(T)) && operand_direct(f.b, COLS, sizeof(T)); }
+
 template <class T, class TL, Layout LA>
 int ff_gradient_tiles(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
-    const bool direct = operand_direct(f.a, LA, sizeof(T)) && operand_direct(f.b, COLS, sizeof(T));
+    const bool direct = gradient_direct<T, LA>(f);
     dim3 grid;
     if (int rc = tile_grid<TL, TL::BN>(f.rows, f.b.index, grid, z * f.parts)) return rc;
     if (!launch) return EBSP_OK;
@@ -161,16 +164,38 @@ size_t partial_bytes(i64 rows, i64 columns, int z, const Cut& cut)
     return cut.parts > 1 ? ((size_t)cut.parts * z * rows * partial_ld(columns) * sizeof(float) + 255) / 256 * 256 : 0;
 }
 
+template <class T>
+int ff_join(const FfGradient& f, int z, hipStream_t st)
+{
+    if (f.parts == 1) return EBSP_OK;
+    const i64 blocks = (f.rows * (partial_ld(f.b.index) / 4) + 255) / 256;
+    LAUNCH(tr_ff_join_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384), (unsigned)z), dim3(256), f);
+    return EBSP_OK;
+}
+
 // The launches of one gradient.
 template <class T, Layout LA>
 int ff_gradient_and_join(const FfGradient& f, int z, bool launch, hipStream_t st)
 {
     if (f.rows == 0) return EBSP_OK;
     if (int rc = ff_gradient<T, LA>(f, z, launch, st)) return rc;
-    if (!launch || f.parts == 1) return EBSP_OK;
-    const i64 blocks = (f.rows * (partial_ld(f.b.index) / 4) + 255) / 256;
-    LAUNCH(tr_ff_join_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384), (unsigned)z), dim3(256), f);
-    return EBSP_OK;
+    return launch ? ff_join<T>(f, z, st) : EBSP_OK;
+}
+
+// Both gradients in one launch, where both have small tiles.
+template <class T>
+int ff_gradients(const FfGradient& x, const FfGradient& w, bool launch, hipStream_t st)
+{
+    using TL = Tile<T, 2, 2, 4, 4>;
+    const bool direct = gradient_direct<T, ROWS>(x);
+    const i64 x_tiles = tiles_of(x.rows, x.b.index, TL::BM, TL::BN), w_tiles = tiles_of(w.rows, w.b.index, TL::BM, TL::BN);
+    const i64 x_all = x_tiles * x.parts, all = x_all + w_tiles * 2 * w.parts;
+    if (!launchable(all, TL::NT)) return fail(EBSP_ERR_SHAPE, "the result is too large for one call");
+    if (!launch) return EBSP_OK;
+    if (direct) LAUNCH((tr_ff_gradients_kernel<T, TL, true>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles);
+    else LAUNCH((tr_ff_gradients_kernel<T, TL, false>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles);
+    if (int rc = ff_join<T>(x, 1, st)) return rc;
+    return ff_join<T>(w, 2, st);
 }
 
 template <class T>
@@ -182,18 +207,24 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
     T* dg = (T*)workspace;
     T* du = dg + M * ldd;
     const size_t units = ebsp_gated_ff_workspace_bytes(M, F, sizeof(T) == 4 ? EBSP_F32 : EBSP_BF16);
-    float* partial = (float*)((char*)workspace + units);                     // dx's, then dW's
+    float* partial = (float*)((char*)workspace + units);
     Cut cx = dx_cut(M, K, F, sizeof(T)), cw = dw_cut(M, K, F, sizeof(T));
-    if (workspace_bytes < units + partial_bytes(M, K, 1, cx)) cx.parts = 1;
-    if (workspace_bytes < units + partial_bytes(F, K, 2, cw)) cw.parts = 1;
+    const size_t px = partial_bytes(M, K, 1, cx), pw = partial_bytes(F, K, 2, cw);
+    if (workspace_bytes < units + px + pw) cx.parts = cw.parts = 1;
+    float* partial_w = cx.parts > 1 ? (float*)((char*)partial + px) : partial;
     const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0}, 2, M, partial, cx.parts, cx.large};
-    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw}, 1, F, partial, cw.parts, cw.large};
+    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw}, 1, F, partial_w, cw.parts, cw.large};
+    const bool together = dx && dwg && M > 0 && F > 0 && !cx.large && !cw.large && gradient_direct<T, ROWS>(to_x) == gradient_direct<T, COLS>(to_w);
     for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
         const i64 chunks = M * (ldd / PER_WORD4<T>);
         if (launch && chunks > 0) {
             const i64 blocks = (chunks + 255) / 256;
             LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, g, u,
                    ldg, dg, du, ldd, M, F, act);
+        }
+        if (together) {
+            if (int rc = ff_gradients<T>(to_x, to_w, launch, st)) return rc;
+            continue;
         }
         if (dx)
             if (int rc = ff_gradient_and_join<T, ROWS>(to_x, 1, launch, st)) return rc;
@@ -352,8 +383,7 @@ size_t ebsp_gated_ff_split_workspace_bytes(int64_t M, int64_t K, int64_t F, int3
     const size_t units = ebsp_gated_ff_workspace_bytes(M, F, dtype);
     if (!units || K < 0 || K >= SIZE_MAX_DIM) return units;
     const int size = element_size(dtype);
-    const size_t x = partial_bytes(M, K, 1, dx_cut(M, K, F, size)), w = partial_bytes(F, K, 2, dw_cut(M, K, F, size));
-    return units + (x > w ? x : w);
+    return units + partial_bytes(M, K, 1, dx_cut(M, K, F, size)) + partial_bytes(F, K, 2, dw_cut(M, K, F, size));
 }
 
 size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype)

@@ -3,7 +3,8 @@ and what the server does at one.
 
 ``ebsp_*`` bind the C ABI 1:1 like ``zipline`` does: argument checks, ``torch.empty`` for outputs that are not given, the
 current stream of the inputs' device, no synchronisation and no fallback.  ``gated_ff`` and ``distill_loss`` are the same
-operators as part of an autograd graph.
+operators as part of an autograd graph.  (As with any torch operator, a HIP graph that captures a backward pass captures its forward
+pass too, and no eager graph of the same leaves is alive meanwhile.)
 """
 from __future__ import annotations
 
