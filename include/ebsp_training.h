@@ -59,10 +59,20 @@ extern "C" {
  *               alone is written then.
  * The others of one element type `dtype`; sums are held in 32 bits and rounded once.
  * M == 0 or F == 0 is a valid no-op, K == 0 gives zero products.
+ *
+ * ebsp_gated_ff_forward_split does the same with a workspace, 256-byte aligned:
+ * where ebsp_gated_ff_forward_workspace_bytes(M, K, F, dtype) is not 0 and the
+ * workspace is that large, long sums of few results run in several parts side by
+ * side, which is faster there.  NULL or less room: as ebsp_gated_ff_forward.
  */
 int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu, int64_t ldwu,
                           int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
                           void* h, int64_t ldh, float* g, float* u, int64_t ldg, void* stream);
+size_t ebsp_gated_ff_forward_workspace_bytes(int64_t M, int64_t K, int64_t F, int32_t dtype);
+int ebsp_gated_ff_forward_split(const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu, int64_t ldwu,
+                                int64_t M, int64_t K, int64_t F, int32_t dtype, int32_t act,
+                                void* h, int64_t ldh, float* g, float* u, int64_t ldg,
+                                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Its backward pass: from dh = dL/dh,

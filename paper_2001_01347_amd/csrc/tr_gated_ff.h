@@ -65,10 +65,14 @@ struct FfForward {
     float *g, *u;                                                            // NULL where nothing is kept for a backward pass
     i64 ldh, ldg;
     int act;
+    float* partial;                                                          // sums in parts: [parts][gate, up][tokens][units, padded to 4]
+    int parts;
 };
 
+__host__ __device__ __forceinline__ i64 partial_ld(i64 columns) { return (columns + 3) / 4 * 4; }
+
 // Gate and up of the same units lie in one wave's squares, so h is formed in registers: one read of x for both products, and
-// neither product goes to memory unless a backward pass will want it.
+// neither product goes to memory unless a backward pass will want it, or the sums are cut into the grid's second axis (few tiles, long sums).
 template <class T, class TL, bool DIRECT>
 __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
 {
@@ -79,7 +83,7 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
     tile_of(blockIdx.x, tm, tn, bm, bn);
     const i64 m0 = (i64)bm * TL::BM, n0 = (i64)bn * (TL::BN / 2);
     Float4 acc[FN][FM];
-    product_tile<T, TL, ROWS, ROWS, FN, DIRECT>(acc, lds, f.x, f.w, 1, m0, n0);
+    product_tile<T, TL, ROWS, ROWS, FN, DIRECT>(acc, lds, f.x, f.w, 1, m0, n0, blockIdx.y, f.parts);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
 #pragma unroll
@@ -91,6 +95,17 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
             const i64 n = n0 + (wn * HALF + j) * 16;
             const i64 have = f.w.index - n;
             if (have <= 0) continue;
+            if (f.parts > 1) {
+                const i64 ld = partial_ld(f.w.index), up = f.x.index * ld, at = n + (lane >> 4) * 4;
+                float* p = f.partial + (i64)blockIdx.y * 2 * up + m * ld + at;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (at + 16 * k < ld) {
+                        *reinterpret_cast<Float4*>(p + 16 * k) = acc[j + k][i];
+                        *reinterpret_cast<Float4*>(p + up + 16 * k) = acc[j + k + HALF][i];
+                    }
+                continue;
+            }
             Float4 h[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
@@ -101,6 +116,30 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
                 store_pair(f.g + m * f.ldg + n, acc[j][i], acc[j + 1][i], have, lane);
                 store_pair(f.u + m * f.ldg + n, acc[j + HALF][i], acc[j + 1 + HALF][i], have, lane);
             }
+        }
+    }
+}
+
+// The parts of gate and up, added up in their order, and what is made of them.
+template <class T>
+__global__ void __launch_bounds__(256) tr_ff_forward_join_kernel(FfForward f)
+{
+    const i64 ld = partial_ld(f.w.index), up = f.x.index * ld;
+    for (i64 at = (i64)blockIdx.x * 256 + threadIdx.x; at < up / 4; at += (i64)gridDim.x * 256) {
+        const i64 m = at / (ld / 4), n = (at - m * (ld / 4)) * 4, have = f.w.index - n;
+        const float* p = f.partial + at * 4;
+        Float4 g = *reinterpret_cast<const Float4*>(p), u = *reinterpret_cast<const Float4*>(p + up), h;
+        for (int part = 1; part < f.parts; ++part) {
+            p += 2 * up;
+            g += *reinterpret_cast<const Float4*>(p);
+            u += *reinterpret_cast<const Float4*>(p + up);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
+        store4((T*)f.h + m * f.ldh + n, h, have);
+        if (f.g) {
+            store4(f.g + m * f.ldg + n, g, have);
+            store4(f.u + m * f.ldg + n, u, have);
         }
     }
 }
@@ -147,8 +186,6 @@ struct FfGradient {
     float* partial;                                                          // sums in parts: [result][parts][rows][columns, padded to 4]
     int parts, large;                                                        // large: tiles of 256 x 256
 };
-
-__host__ __device__ __forceinline__ i64 partial_ld(i64 columns) { return (columns + 3) / 4 * 4; }
 
 // dx = dg Wg + du Wu (A in rows, two segments) and dW = dg^T x, du^T x (A in columns, a half of the grid each).  dx has few tiles and
 // long sums where tokens are few, dW where the matrices are small and tokens many; the grid's second axis cuts the sums then, and

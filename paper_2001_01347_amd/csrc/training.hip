@@ -82,9 +82,12 @@ int ff_forward_tiles(const FfForward& f, hipStream_t st)
 {
     const bool direct = operand_direct(f.x, ROWS, sizeof(T)) && operand_direct(f.w, ROWS, sizeof(T));
     dim3 grid;
-    if (int rc = tile_grid<TL, TL::BN / 2>(f.x.index, f.w.index, grid)) return rc;
+    if (int rc = tile_grid<TL, TL::BN / 2>(f.x.index, f.w.index, grid, f.parts)) return rc;
     if (direct) LAUNCH((tr_ff_forward_kernel<T, TL, true>), grid, dim3(TL::NT), f);
     else LAUNCH((tr_ff_forward_kernel<T, TL, false>), grid, dim3(TL::NT), f);
+    if (f.parts == 1) return EBSP_OK;
+    const i64 blocks = (f.x.index * (partial_ld(f.w.index) / 4) + 255) / 256;
+    LAUNCH(tr_ff_forward_join_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), f);
     return EBSP_OK;
 }
 
@@ -100,19 +103,47 @@ int ff_few(const FfForward& f, hipStream_t st)
     return EBSP_OK;
 }
 
-// Tiles want workgroups enough and long sums in each: where rows or units are few the kernel that shares a sum out among its waves is faster.
-// us, it / tiles of 128 x 64 (M x K x F): bf16 1 x 4096 x 12288 37 / 49, 16 x 4096 x 2048 13 / 32, 16 x 4096 x 12288 47 / 45, 24 x 1024 x 6144 10 / 12,
-// 64 x 4096 x 4096 28 / 42, 64 x 1024 x 6144 14 / 14, 100 x 4096 x 3000 43 / 42, 192 x 4096 x 1024 24 / 34, 256 x 2048 x 2048 25 / 20; f32
-// 64 x 4096 x 4096 62 / 250, 256 x 1024 x 2816 49 / 67, 384 x 4096 x 4096 357 / 252.  Its squares hold 64 rows, or 32 where that makes too few workgroups
-// (64 x 4096 x 1024 18, so 24).
-template <class T>
-int ff_forward(const FfForward& f, hipStream_t st)
+// How the forward pass is cut up.
+struct ForwardCut {
+    int few;                                                                 // squares of 16 tokens of the kernel for few of them, or 0: tiles
+    bool large;                                                              // tiles of 256 x 128, not 128 x 64
+    int parts;                                                               // of every sum
+};
+
+// Tiles want a CU each and long sums.  Where they would be few, either the kernel that shares a sum out among its waves runs, or the sums are cut into
+// parts (`room`: there is a workspace for them).  us, that kernel / tiles in parts / whole ones (M x K x F), bf16: 16 x 4096 x 2048 13 / 14 / 33,
+// 64 x 1024 x 4096 10 / 14 / 14, 341 x 3984 x 286 15 / 18 / 42, 341 x 3981 x 286 (rows at any alignment) 43 / 25 / 68, 64 x 4096 x 4096 28 / 21 / 43,
+// 192 x 4096 x 1024 24 / 17 / 35, 100 x 4096 x 3000 43 / 20 / 42, 657 x 3392 x 936 55 / 23 / 31, 300 x 1024 x 2000 19 / 16 / 14; fp32: 64 x 4096 x 4096
+// 61 / 72 / 248, 300 x 512 x 512 10 / 18 / 36, 256 x 1024 x 2816 48 / 44 / 67, 600 x 2048 x 1024 88 / 63 / 127, 384 x 4096 x 4096 354 / 198 / 252.  The kernel's
+// squares hold 64 tokens, or 32 where that makes too few workgroups (64 x 4096 x 1024 18, so 24).
+ForwardCut forward_cut(i64 M, i64 K, i64 F, int size, bool room)
 {
-    const i64 M = f.x.index, groups = tiles_of(M, f.w.index, 64, 16);
-    if (M <= 16) return ff_few<T, 1>(f, st);
-    if (groups <= (sizeof(T) == 4 ? 768 : 352)) return M <= 32 || groups <= 128 ? ff_few<T, 2>(f, st) : ff_few<T, 4>(f, st);
-    if (tiles_of(f.x.index, f.w.index, 256, 128) >= 192) return ff_forward_tiles<T, Tile<T, 2, 4, 8, 4>>(f, st);
-    return ff_forward_tiles<T, Tile<T, 2, 2, 4, 4>>(f, st);
+    const i64 groups = tiles_of(M, F, 64, 16), tiles = tiles_of(M, F, 128, 64), steps = (K * size + 127) / 128;
+    const bool wide = size == 4;
+    int parts = 1;
+    if (room && steps >= (wide ? 16 : 32) && tiles <= (wide ? 208 : 128)) {
+        const i64 wanted = (wide ? 768 : 256) / tiles;
+        parts = (int)(wanted < steps / 8 ? wanted : steps / 8);
+    }
+    const bool aligned_rows = K * size % 16 == 0;
+    const i64 most = wide ? (parts > 1 ? 192 : 768) : parts == 1 ? 352 : aligned_rows ? 128 : 32;
+    if (M <= 16) return {1, false, 1};
+    if (groups <= most || (wide && M <= 64)) return {M <= 32 || groups <= 128 ? 2 : 4, false, 1};
+    return {0, tiles_of(M, F, 256, 128) >= 192, parts};
+}
+
+size_t forward_partial_bytes(i64 M, i64 F, int parts) { return parts > 1 ? ((size_t)2 * parts * M * partial_ld(F) * sizeof(float) + 255) / 256 * 256 : 0; }
+
+template <class T>
+int ff_forward(FfForward& f, void* workspace, size_t workspace_bytes, hipStream_t st)
+{
+    const i64 M = f.x.index, K = f.x.depth, F = f.w.index;
+    ForwardCut cut = forward_cut(M, K, F, sizeof(T), true);
+    if (workspace_bytes < forward_partial_bytes(M, F, cut.parts)) cut = forward_cut(M, K, F, sizeof(T), false);
+    f.partial = (float*)workspace;
+    f.parts = cut.parts;
+    if (cut.few) return cut.few == 1 ? ff_few<T, 1>(f, st) : cut.few == 2 ? ff_few<T, 2>(f, st) : ff_few<T, 4>(f, st);
+    return cut.large ? ff_forward_tiles<T, Tile<T, 2, 4, 8, 4>>(f, st) : ff_forward_tiles<T, Tile<T, 2, 2, 4, 4>>(f, st);
 }
 
 template <class T, Layout LA>
@@ -363,6 +394,20 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
                           int64_t F, int32_t dtype, int32_t act, void* h, int64_t ldh, float* g, float* u, int64_t ldg,
                           void* stream)
 {
+    return ebsp_gated_ff_forward_split(x, ldx, wg, ldwg, wu, ldwu, M, K, F, dtype, act, h, ldh, g, u, ldg, nullptr, 0, stream);
+}
+
+size_t ebsp_gated_ff_forward_workspace_bytes(int64_t M, int64_t K, int64_t F, int32_t dtype)
+{
+    const int size = element_size(dtype);
+    if (!size || M < 1 || K < 1 || F < 1 || M >= SIZE_MAX_DIM || K >= SIZE_MAX_DIM || F >= SIZE_MAX_DIM) return 0;
+    return forward_partial_bytes(M, F, forward_cut(M, K, F, size, true).parts);
+}
+
+int ebsp_gated_ff_forward_split(const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu, int64_t ldwu, int64_t M, int64_t K,
+                                int64_t F, int32_t dtype, int32_t act, void* h, int64_t ldh, float* g, float* u, int64_t ldg,
+                                void* workspace, size_t workspace_bytes, void* stream)
+{
     if (int rc = check_sizes(M, K, F, dtype, act)) return rc;
     if (M == 0 || F == 0) return EBSP_OK;
     if (!h || (K > 0 && (!x || !wg || !wu))) return fail(EBSP_ERR_NULL, "x, wg, wu and h must not be NULL");
@@ -372,10 +417,13 @@ int ebsp_gated_ff_forward(const void* x, int64_t ldx, const void* wg, int64_t ld
     const int size = element_size(dtype);
     if (!aligned(x, size) || !aligned(wg, size) || !aligned(wu, size) || !aligned(h, size) || !aligned(g, 4) || !aligned(u, 4))
         return fail(EBSP_ERR_ARGUMENT, "a pointer is not aligned to its elements");
+    if (!workspace) workspace_bytes = 0;
+    if (!aligned(workspace, 256)) return fail(EBSP_ERR_WORKSPACE, "workspace is not 256-byte aligned");
     if (int rc = check_device()) return rc;
-    FfForward f = {{{x, x}, {ldx, ldx}, M, K}, {{wg, wu}, {ldwg, ldwu}, F, K}, h, g, u, ldh, ldg, act};
+    FfForward f = {{{x, x}, {ldx, ldx}, M, K}, {{wg, wu}, {ldwg, ldwu}, F, K}, h, g, u, ldh, ldg, act, nullptr, 1};
     hipStream_t st = (hipStream_t)stream;
-    return dtype == EBSP_BF16 ? ff_forward<__bf16>(f, st) : dtype == EBSP_F16 ? ff_forward<_Float16>(f, st) : ff_forward<float>(f, st);
+    auto run = dtype == EBSP_BF16 ? ff_forward<__bf16> : dtype == EBSP_F16 ? ff_forward<_Float16> : ff_forward<float>;
+    return run(f, workspace, workspace_bytes, st);
 }
 
 size_t ebsp_gated_ff_split_workspace_bytes(int64_t M, int64_t K, int64_t F, int32_t dtype)

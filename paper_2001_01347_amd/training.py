@@ -19,7 +19,7 @@ from .zipline import ZipLineError, _check_buffer, _check_workspace
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
-EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_workspace_bytes",
+EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_forward_workspace_bytes", "ebsp_gated_ff_forward_split", "ebsp_gated_ff_workspace_bytes",
            "ebsp_gated_ff_split_workspace_bytes", "ebsp_gated_ff_backward", "ebsp_distill_workspace_bytes",
            "ebsp_distill_forward", "ebsp_distill_backward", "ebsp_distill_loss_grad", "ebsp_merge_pushes")
 
@@ -37,6 +37,10 @@ def load() -> ctypes.CDLL:
         vp, i64, i32, sz, c_int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int
         lib.ebsp_gated_ff_forward.restype = c_int
         lib.ebsp_gated_ff_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp]
+        lib.ebsp_gated_ff_forward_workspace_bytes.restype = sz
+        lib.ebsp_gated_ff_forward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        lib.ebsp_gated_ff_forward_split.restype = c_int
+        lib.ebsp_gated_ff_forward_split.argtypes = lib.ebsp_gated_ff_forward.argtypes[:-1] + [vp, sz, vp]
         lib.ebsp_gated_ff_workspace_bytes.restype = sz
         lib.ebsp_gated_ff_workspace_bytes.argtypes = [i64, i64, i32]
         lib.ebsp_gated_ff_split_workspace_bytes.restype = sz
@@ -127,20 +131,33 @@ def _ff_operands(x, wg, wu):
 
 
 def ebsp_gated_ff_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu", save: bool = False,
-                          h: Optional[torch.Tensor] = None, g: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None):
+                          h: Optional[torch.Tensor] = None, g: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None):
     """``act(x wg^T) * (x wu^T)`` for x [M, K] and weights [F, K]; see the header.
 
     Returns ``(h[M, F], g, u)``; with ``save`` g and u are the products [M, F], float32, that ``ebsp_gated_ff_backward`` takes,
-    otherwise None.  Rows of the operands may lie any distance apart.  Does not synchronise.
+    otherwise None.  Rows of the operands may lie any distance apart.  A ``workspace`` smaller than
+    ``ebsp_gated_ff_forward_workspace_bytes`` keeps sums whole.  Does not synchronise.
     """
     code, M, K, F, dev, dt, operands = _ff_operands(x, wg, wu)
     act = _activation(act)
     h = _output("h", h, dev, dt, (M, F))
     if save or g is not None or u is not None:
         g, u = _output("g", g, dev, torch.float32, (M, F)), _output("u", u, dev, torch.float32, (M, F))
-    _call("ebsp_gated_ff_forward", dev, *operands, M, K, F, code, act, h.data_ptr(), F,
-          None if g is None else g.data_ptr(), None if u is None else u.data_ptr(), F)
+    if workspace is None:
+        need = M > 16 and (_lib or load()).ebsp_gated_ff_forward_workspace_bytes(M, K, F, code)     # (0 for fewer: spare the call)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    else:
+        _check_workspace(workspace, dev, 0)
+    room = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _call("ebsp_gated_ff_forward_split", dev, *operands, M, K, F, code, act, h.data_ptr(), F,
+          None if g is None else g.data_ptr(), None if u is None else u.data_ptr(), F, *room)
     return h, g, u
+
+
+def ebsp_gated_ff_forward_workspace_bytes(M: int, K: int, F: int, dtype: torch.dtype) -> int:
+    return int(load().ebsp_gated_ff_forward_workspace_bytes(M, K, F, DTYPES[dtype]))
 
 
 def ebsp_gated_ff_workspace_bytes(M: int, F: int, dtype: torch.dtype) -> int:

@@ -276,6 +276,24 @@ def test_cut_sums(tr, M, K, F, dtype):
         _compare((h, *tr.ebsp_gated_ff_backward(dh, x, wg, wu, g, u, workspace=workspace)), ref, ("h", "dx", "dwg", "dwu"))
 
 
+@pytest.mark.parametrize("M,K,F", [(40, 2100, 3000), (70, 4096, 1024), (100, 2048, 1001), (129, 2056, 515), (341, 3981, 286), (700, 2049, 70), (2000, 4096, 33),
+                                   (513, 1030, 514)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_cut_sums_forward(tr, M, K, F, dtype):
+    x, wg, wu, dh = _inputs(M, K, F, dtype, seed=22)
+    ref = Reference("gelu_tanh", x, wg, wu)
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    saved = []
+    for workspace in (None, small):                                          # in parts, and without room for them
+        h, g, u = tr.ebsp_gated_ff_forward(x, wg, wu, "gelu_tanh", save=True, workspace=workspace)
+        _compare((h,), ref, ("h",))
+        for got, w in ((g, wg), (u, wu)):
+            bound = 2 * (K + 8) * 2.0 ** -24 * (x.double().abs() @ w.double().abs().t())
+            assert bool(((got.double() - x.double() @ w.double().t()).abs() <= bound + 1e-37).all())
+        alone = tr.ebsp_gated_ff_forward(x, wg, wu, "gelu_tanh", workspace=workspace)[0]
+        assert torch.equal(alone, h)
+
+
 def test_cut_sums_large_tiles(tr):
     for M, K, F in ((1300, 1300, 6200), (16400, 1032, 770)):                 # 36 large tiles of dx, 40 of dW
         x, wg, wu, dh = _inputs(M, K, F, torch.bfloat16, seed=21)

@@ -84,6 +84,25 @@ def test_gated_ff_workspace(lib):
     assert training.ebsp_gated_ff_workspace_bytes(4, 32, __import__("torch").bfloat16) == 512
 
 
+def test_gated_ff_forward_workspace(lib):
+    from paper_2001_01347_amd import training
+    room = lib.ebsp_gated_ff_forward_workspace_bytes
+    assert room(100, 4096, 3000, BF16) >= 2 * 2 * 100 * 3000 * 4                                     # two parts at least of gate and up
+    for M, K, F in ((1, 4096, 12288), (8192, 4096, 12288), (64, 64, 64), (0, 4096, 300), (100, 0, 300), (100, 4096, 0), (-1, 8, 8), (1 << 31, 8, 8)):
+        assert room(M, K, F, BF16) == 0, (M, K, F)
+    assert room(100, 4096, 3000, 3) == 0
+    for M in (17, 33, 65, 200, 1000, 5000):
+        for K in (1, 1000, 2048, 4096, 9999):
+            for F in (1, 64, 301, 5000):
+                for dtype in (BF16, F16, F32):
+                    assert room(M, K, F, dtype) % 256 == 0
+    assert training.ebsp_gated_ff_forward_workspace_bytes(8, 8, 8, __import__("torch").bfloat16) == 0
+    split = lib.ebsp_gated_ff_forward_split
+    args = (ONE, 64, ONE, 64, ONE, 64, 4, 64, 32, BF16, 0, ONE, 32, NULL, NULL, 32)
+    assert split(*args, ctypes.c_void_p(264), 1 << 20, NULL) == -3 and _error()
+    assert split(*args[:12], 31, *args[13:], ONE, 1 << 20, NULL) == -6
+
+
 def test_gated_ff_split_workspace(lib):
     from paper_2001_01347_amd import training
     least, split = lib.ebsp_gated_ff_workspace_bytes, lib.ebsp_gated_ff_split_workspace_bytes
