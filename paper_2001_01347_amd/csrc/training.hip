@@ -103,6 +103,16 @@ int ff_few(const FfForward& f, hipStream_t st)
     return EBSP_OK;
 }
 
+// Tiles of 256 x 256 and not of 128 x 128, of which there would be so many: a large one takes 3.2 times as long as a small one (4 times in 32 bits; 2.8
+// times where the sum is long and the last round leaves CUs idle), and either fills the CUs in whole rounds.  us, large / small (M x K x F), bf16: forward 8192 x 2048 x 12288 642 / 795, 8192 x 1024 x 2048 67 / 77, 2126 x 768 x 4160
+// 48 / 39, 1169 x 2624 x 8936 117 / 128, 1877 x 1759 x 4592 168 / 136, 2812 x 64 x 3200 25 / 20; dx 8192 x 4096 x 512 78 / 98; dW 1024 x 4096 x 12288 228 / 262; fp32 forward
+// 3000 x 512 x 4096 246 / 191.
+bool large_tiles(i64 large, i64 small, i64 steps, int size)
+{
+    const i64 large_rounds = (large + 255) / 256, small_rounds = (small + 255) / 256;
+    return large >= 192 && large_rounds * (size == 4 ? 20 : steps >= 32 ? 14 : 16) <= small_rounds * 5;
+}
+
 // How the forward pass is cut up.
 struct ForwardCut {
     int few;                                                                 // squares of 16 tokens of the kernel for few of them, or 0: tiles
@@ -129,7 +139,7 @@ ForwardCut forward_cut(i64 M, i64 K, i64 F, int size, bool room)
     const i64 most = wide ? (parts > 1 ? 192 : 768) : parts == 1 ? 352 : aligned_rows ? 128 : 32;
     if (M <= 16) return {1, false, 1};
     if (groups <= most || (wide && M <= 64)) return {M <= 32 || groups <= 128 ? 2 : 4, false, 1};
-    return {0, tiles_of(M, F, 256, 128) >= 192, parts};
+    return {0, large_tiles(tiles_of(M, F, 256, 128), tiles, steps, size), parts};
 }
 
 size_t forward_partial_bytes(i64 M, i64 F, int parts) { return parts > 1 ? ((size_t)2 * parts * M * partial_ld(F) * sizeof(float) + 255) / 256 * 256 : 0; }
@@ -180,8 +190,8 @@ struct Cut {
 Cut gradient_cut(i64 rows, i64 columns, int z, i64 steps, int size)
 {
     const i64 large = tiles_of(rows, columns, 256, 256) * z, small = tiles_of(rows, columns, 128, 128) * z;
-    if (large >= 192 || small == 0) return {true, 1};
-    if (large >= 32 && steps * large >= 32 * 256) return {true, (int)(256 / large)};
+    if (large_tiles(large, small, steps, size) || small == 0) return {true, 1};
+    if (large >= 32 && large < 192 && steps * large >= 32 * 256) return {true, (int)(256 / large)};
     if (small >= 192 || steps < (size == 4 ? 8 : 24)) return {false, 1};
     const i64 parts = 256 / small, most = size == 4 ? steps / 4 : steps / 8;
     return {false, (int)(parts < most ? parts : most)};
