@@ -151,13 +151,13 @@ struct DirectTile {
 };
 
 // Steps at a segment's beginning that a LOOSE tile may take: whole ones that do not come to the last row of COLS, whose rows hold a chunk at
-// least and whose offsets fit 31 bits.
+// least and whose two matrices have the same stride, and offsets that fit 31 bits.
 template <class T, Layout L>
 __device__ __forceinline__ int loose_steps(const Operand& o)
 {
     constexpr int BK = 128 / (int)sizeof(T);
     const i64 far = o.ld[0] > o.ld[1] ? o.ld[0] : o.ld[1];
-    if (far * (i64)sizeof(T) * 256 > 0x7fffffffll || (L == COLS && o.index < PER_WORD4<T>)) return 0;
+    if (far * (i64)sizeof(T) * 256 > 0x7fffffffll || (L == COLS && (o.index < PER_WORD4<T> || o.ld[0] != o.ld[1]))) return 0;
     return (int)((L == COLS ? o.depth - 1 : o.depth) / BK);
 }
 

@@ -68,10 +68,12 @@ int tile_grid(i64 m, i64 n, dim3& grid, int z = 1)
     return EBSP_OK;
 }
 
-// Whole 16-byte chunks all along, and offsets inside a tile that fit 31 bits: what loads straight to shared memory need.
+// Whole 16-byte chunks all along, and offsets inside a tile that fit 31 bits: what loads straight to shared memory need.  The two matrices of COLS share
+// their offsets, so their strides have to be the same.
 bool operand_direct(const Operand& o, Layout l, int size)
 {
     const i64 n = 16 / size;
+    if (l == COLS && o.ld[0] != o.ld[1]) return false;
     for (int w = 0; w < 2; ++w)
         if (o.p[w] && (!aligned(o.p[w], 16) || o.ld[w] % n || o.ld[w] * size * 256 > 0x7fffffffll)) return false;
     return (l == ROWS ? o.depth : o.index) % n == 0;

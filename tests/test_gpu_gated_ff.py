@@ -147,6 +147,19 @@ def test_rows_apart(tr, M, K, F, dtype, pad):
     _compare(_step(tr, "silu", x, wg, wu, dh), ref, ("h", "dx", "dwg", "dwu"))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,F", [(5, 128, 200), (70, 256, 320), (300, 200, 136), (260, 99, 77), (800, 1032, 1304)])
+def test_weights_of_different_strides(tr, M, K, F, dtype):
+    x, wg, wu, dh = _inputs(M, K, F, dtype, seed=14)
+    wide = torch.full((F, K + 40), float("nan"), device="cuda", dtype=dtype)
+    for width in (8, 5):                                                     # rows of wu at multiples of 16 bytes and at others
+        wide[:, width:width + K] = wu
+        ref = Reference("silu", x, wg, wu, dh)
+        _compare(_step(tr, "silu", x, wg, wide[:, width:width + K], dh), ref, ("h", "dx", "dwg", "dwu"))
+        _compare(_step(tr, "silu", x, wide[:, width:width + K], wg, dh)[1:2], Reference("silu", x, wu, wg, dh), ("dx",))
+        wide.fill_(float("nan"))
+
+
 @pytest.mark.parametrize("M", [3, 40, 200])
 def test_not_finite_stays_where_it_belongs(tr, M):
     """An infinity or a NaN in one token, or in one unit's weights, reaches the results that it is part of and no other."""
