@@ -232,15 +232,15 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradient_kernel(FfGradient f)
     gradient_tile<T, TL, LA, DIRECT>(f, blockIdx.x, blockIdx.y, lds);
 }
 
-// dx and dW side by side, dx's workgroups first: either alone leaves CUs without work at its end (forward and both gradients, us, one after the
-// other / so: bf16 1021 x 1000 x 2730 91 / 85, 2048 x 256 x 1024 50 / 39, 512 x 2048 x 4096 93 / 93; f32 1024 x 1024 x 2816 367 / 357).
+// dx and dW side by side, the longer sums first: either alone leaves CUs without work at its end (forward and both gradients, us, one after the
+// other / so: bf16 1021 x 1000 x 2730 91 / 85, 2048 x 256 x 1024 50 / 39, 512 x 2048 x 4096 93 / 93; f32 1024 x 1024 x 2816 367 / 337).
 template <class T, class TL, bool DIRECT>
-__global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradients_kernel(FfGradient x, FfGradient w, u32 x_tiles, u32 x_all, u32 w_tiles)
+__global__ void __launch_bounds__(TL::NT, 2) tr_ff_gradients_kernel(FfGradient x, FfGradient w, u32 x_tiles, u32 x_all, u32 w_tiles, u32 w_first)
 {
     __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
-    const u32 id = blockIdx.x;
-    if (id < x_all) gradient_tile<T, TL, ROWS, DIRECT>(x, id % x_tiles, id / x_tiles, lds);
-    else gradient_tile<T, TL, COLS, DIRECT>(w, (id - x_all) % w_tiles, (id - x_all) / w_tiles, lds);
+    const u32 id = blockIdx.x, id_x = id - w_first, id_w = id - (w_first ? 0 : x_all);   // w_first: how many of dW come before dx's
+    if (id_x < x_all) gradient_tile<T, TL, ROWS, DIRECT>(x, id_x % x_tiles, id_x / x_tiles, lds);
+    else gradient_tile<T, TL, COLS, DIRECT>(w, id_w % w_tiles, id_w / w_tiles, lds);
 }
 
 // The parts of a result, added up in their order and rounded.

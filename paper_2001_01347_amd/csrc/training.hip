@@ -189,13 +189,14 @@ struct Cut {
 // A CU for every tile, or for every part of one.  us, large tiles in parts / small ones in parts / small ones whole: dx 2048 x 2048 x 8192 bf16 (64
 // large tiles, 256 steps) 164 / 180 / 192, 512 x 4096 x 12288 (32, 384) 115 / 141 / 247, 1024 x 4096 x 2048 (64, 64) 58 / 58 / 52, 1 x 4096 x 12288 (32
 // small, 384) 66 / 45 / 224, f32 1024 x 1024 x 2816 (64 small, 176) 189 / 112 / 361; dW 8192 x 1024 x 2048 (64, 128) 112 / 127 / 123.
+// Twice as many parts in 32 bits where sums are long: both gradients end together (1024 x 1024 x 2816 355 -> 337; with sums of 64 steps, 1024 x 1024 x 1024, 133 -> 144).
 Cut gradient_cut(i64 rows, i64 columns, int z, i64 steps, int size)
 {
     const i64 large = tiles_of(rows, columns, 256, 256) * z, small = tiles_of(rows, columns, 128, 128) * z;
     if (large_tiles(large, small, steps, size) || small == 0) return {true, 1};
     if (large >= 32 && large < 192 && steps * large >= 32 * 256) return {true, (int)(256 / large)};
     if (small >= 192 || steps < (size == 4 ? 8 : 24)) return {false, 1};
-    const i64 parts = 256 / small, most = size == 4 ? steps / 4 : steps / 8;
+    const i64 parts = (size == 4 && small >= 64 && steps >= 128 ? 512 : 256) / small, most = size == 4 ? steps / 4 : steps / 8;
     return {false, (int)(parts < most ? parts : most)};
 }
 
@@ -232,11 +233,12 @@ int ff_gradients(const FfGradient& x, const FfGradient& w, bool launch, hipStrea
     using TL = Tile<T, 2, 2, 4, 4>;
     const bool direct = gradient_direct<T, ROWS>(x);
     const i64 x_tiles = tiles_of(x.rows, x.b.index, TL::BM, TL::BN), w_tiles = tiles_of(w.rows, w.b.index, TL::BM, TL::BN);
-    const i64 x_all = x_tiles * x.parts, all = x_all + w_tiles * 2 * w.parts;
+    const i64 x_all = x_tiles * x.parts, w_all = w_tiles * 2 * w.parts, all = x_all + w_all;
+    const i64 w_first = w.b.depth / w.parts > 2 * x.b.depth / x.parts ? w_all : 0;       // whose sums are longer
     if (!launchable(all, TL::NT)) return fail(EBSP_ERR_SHAPE, "the result is too large for one call");
     if (!launch) return EBSP_OK;
-    if (direct) LAUNCH((tr_ff_gradients_kernel<T, TL, true>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles);
-    else LAUNCH((tr_ff_gradients_kernel<T, TL, false>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles);
+    if (direct) LAUNCH((tr_ff_gradients_kernel<T, TL, true>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles, (u32)w_first);
+    else LAUNCH((tr_ff_gradients_kernel<T, TL, false>), dim3((unsigned)all), dim3(TL::NT), x, w, (u32)x_tiles, (u32)x_all, (u32)w_tiles, (u32)w_first);
     if (int rc = ff_join<T>(x, 1, st)) return rc;
     return ff_join<T>(w, 2, st);
 }
