@@ -84,7 +84,9 @@ int ebsp_gated_ff_forward_split(const void* x, int64_t ldx, const void* wg, int6
  *   dx       out [M][K], rows lddx apart, or NULL: not wanted
  *   dwg, dwu out [F][K], rows lddw apart, or both NULL: not wanted
  *   workspace    at least ebsp_gated_ff_workspace_bytes(M, F, dtype) bytes,
- *                256-byte aligned (it holds dg and du, rounded to dtype).  With
+ *                256-byte aligned (it holds dg and du, rounded to dtype; in fp16
+ *                times a common power of two where their largest is above 65504
+ *                or below 2^-6).  With
  *                ebsp_gated_ff_split_workspace_bytes(M, K, F, dtype) bytes, where
  *                that is more, long sums of small results run in several parts
  *                side by side, which is faster (dx where tokens are few, the

@@ -144,37 +144,97 @@ __global__ void __launch_bounds__(256) tr_ff_forward_join_kernel(FfForward f)
     }
 }
 
-// dg = dh * u * act'(g) and du = dh * act(g), rows padded with zeros to a multiple of 16 bytes.  They are rounded to the inputs' type,
-// which is what the matrix cores multiply; the sums over them stay in 32 bits.  g and u come as the forward pass summed them: rounding
-// them too would make the gradients' error 1.8 times that of rounding the results alone, as it is 1.4 times.
+// What the pass that forms dg and du reads and writes.
 template <class T>
-__global__ void __launch_bounds__(256) tr_ff_units_kernel(const T* dh, i64 lddh, const float* g, const float* u, i64 ldg, T* dg, T* du, i64 ldd,
-                                                          i64 M, i64 F, int act)
+struct FfUnits {
+    const T* dh;
+    i64 lddh;
+    const float *g, *u;
+    i64 ldg;
+    T *dg, *du;
+    i64 ldd, M, F;
+    int act;
+    float *largest, *back;                                                   // fp16: see tr_ff_units_kernel
+};
+
+constexpr int RANGE_BLOCKS = 2048;                                           // eight workgroups a CU, all resident
+constexpr int RANGE_BYTES = RANGE_BLOCKS * 4 + 256;
+
+// dg = dh * u * act'(g) and du = dh * act(g) times `by`, rows padded with zeros to a multiple of 16 bytes; the largest finite size that the
+// thread has met, before that product.
+template <class T>
+__device__ __forceinline__ float form_units(const FfUnits<T>& f, float by)
 {
     constexpr int N = PER_WORD4<T>;
-    const i64 chunks = ldd / N, all = M * chunks;
+    float largest = 0.f;
+    const i64 chunks = f.ldd / N, all = f.M * chunks;
     for (i64 at = (i64)blockIdx.x * 256 + threadIdx.x; at < all; at += (i64)gridDim.x * 256) {
-        const i64 m = at / chunks, f = (at - m * chunks) * N;
+        const i64 m = at / chunks, c = (at - m * chunks) * N;
         Pack<T> ph, og, ou;
         Pack<float> pg[N / 4], pu[N / 4];
-        ph.raw = load_some(dh + m * lddh + f, F - f);
+        ph.raw = load_some(f.dh + m * f.lddh + c, f.F - c);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            pg[i].raw = load_some(g + m * ldg + f + 4 * i, F - f - 4 * i);
-            pu[i].raw = load_some(u + m * ldg + f + 4 * i, F - f - 4 * i);
+            pg[i].raw = load_some(f.g + m * f.ldg + c + 4 * i, f.F - c - 4 * i);
+            pu[i].raw = load_some(f.u + m * f.ldg + c + 4 * i, f.F - c - 4 * i);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, d;
-            activation_both(act, pg[i / 4].v[i % 4], a, d);
+            activation_both(f.act, pg[i / 4].v[i % 4], a, d);
             const float h = to_float(ph.v[i]);
-            const bool in = f + i < F;
-            og.v[i] = from_float<T>(in ? h * pu[i / 4].v[i % 4] * d : 0.f);
-            ou.v[i] = from_float<T>(in ? h * a : 0.f);
+            const bool in = c + i < f.F;
+            const float dg = in ? h * pu[i / 4].v[i % 4] * d : 0.f, du = in ? h * a : 0.f;
+            og.v[i] = from_float<T>(dg * by);
+            ou.v[i] = from_float<T>(du * by);
+            if constexpr (__is_same(T, _Float16)) {
+                if (fabsf(dg) <= FLT_MAX) largest = fmaxf(largest, fabsf(dg));
+                if (fabsf(du) <= FLT_MAX) largest = fmaxf(largest, fabsf(du));
+            }
         }
-        *reinterpret_cast<Word4*>(dg + m * ldd + f) = og.raw;
-        *reinterpret_cast<Word4*>(du + m * ldd + f) = ou.raw;
+        *reinterpret_cast<Word4*>(f.dg + m * f.ldd + c) = og.raw;
+        *reinterpret_cast<Word4*>(f.du + m * f.ldd + c) = ou.raw;
     }
+    return largest;
+}
+
+// A value that every thread of 256 has: the largest of theirs.
+__device__ __forceinline__ float largest_of_block(float v)
+{
+    __shared__ float of_wave[4];
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
+}
+
+// They are rounded to the inputs' type, which is what the matrix cores multiply; the sums over them stay in 32 bits.  g and u come as
+// the forward pass summed them: rounding them too would make the gradients' error 1.8 times that of rounding the results alone, as it is
+// 1.4 times.  The range of fp16 does not hold every product of an fp16 and two 32-bit numbers whose sums the results have room for: there the
+// pass also leaves every workgroup's largest size for tr_ff_rescale_kernel.
+template <class T>
+__global__ void __launch_bounds__(256) tr_ff_units_kernel(FfUnits<T> f)
+{
+    const float largest = form_units(f, 1.f);
+    if constexpr (__is_same(T, _Float16)) {
+        const float all = largest_of_block(largest);
+        if (threadIdx.x == 0) f.largest[blockIdx.x] = all;
+    }
+}
+
+// fp16: where the largest of dg and du overflows, or lies below 2^-6 (of values a hundredth of it the first are no normal numbers any more), the pass
+// runs once more, times the power of two that brings it to 2^14 .. 2^15.  `back` is that power's inverse, for the sums.  Values below 2^-28 of the largest
+// lose bits then; no value is off by more than half a step of its own or 2^-39 of the largest.  The look costs a launch and reads some KB (forward and
+// gradients, us, without / with it / with the second pass: 512 x 512 x 1024 33 / 38 / -, 1021 x 1000 x 2730 84 / 90 / 95, 8192 x 4096 x 12288 4139 / 4161 / 4411).
+__global__ void __launch_bounds__(256) tr_ff_rescale_kernel(FfUnits<_Float16> f, int blocks)
+{
+    float v = 0.f;
+    for (int i = threadIdx.x; i < blocks; i += 256) v = fmaxf(v, f.largest[i]);
+    v = largest_of_block(v);
+    int up = 0;
+    if (v > 65504.f || (v > 0.f && v < 0.015625f)) up = min(14 - ilogbf(v), 100);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *f.back = ldexpf(1.f, -up);
+    if (up != 0) form_units(f, ldexpf(1.f, up));
 }
 
 struct FfGradient {
@@ -185,7 +245,16 @@ struct FfGradient {
     i64 rows;                                                                // of the result (a.index counts the padded ones too)
     float* partial;                                                          // sums in parts: [result][parts][rows][columns, padded to 4]
     int parts, large;                                                        // large: tiles of 256 x 256
+    const float* back;                                                       // fp16: what the sums are multiplied by (see tr_ff_rescale_kernel); NULL where they are empty
 };
+
+// The sums of dg and du as they are, whatever power of two these came with.
+template <class T>
+__device__ __forceinline__ Float4 brought_back(Float4 sum, float back)
+{
+    if constexpr (__is_same(T, _Float16)) sum *= back;
+    return sum;
+}
 
 // dx = dg Wg + du Wu (A in rows, two segments) and dW = dg^T x, du^T x (A in columns, a half of the grid each).  dx has few tiles and
 // long sums where tokens are few, dW where the matrices are small and tokens many; the grid's second axis cuts the sums then, and
@@ -204,6 +273,7 @@ __device__ __forceinline__ void gradient_tile(const FfGradient& f, u32 tile, int
     product_tile<T, TL, LA, COLS, 0, DIRECT>(acc, lds, a, f.b, f.segments, m0, n0, part, parts);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN;
+    const float back = __is_same(T, _Float16) && f.back ? *f.back : 1.f;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const i64 m = m0 + (wm * FM + i) * 16 + (lane & 15);
@@ -219,7 +289,7 @@ __device__ __forceinline__ void gradient_tile(const FfGradient& f, u32 tile, int
                 if (n + (lane >> 4) * 4 < ld) *reinterpret_cast<Float4*>(p) = acc[j][i];
                 if (n + (lane >> 4) * 4 + 16 < ld) *reinterpret_cast<Float4*>(p + 16) = acc[j + 1][i];
             } else {
-                store_pair((T*)f.out[z] + m * f.ld[z] + n, acc[j][i], acc[j + 1][i], have, lane);
+                store_pair((T*)f.out[z] + m * f.ld[z] + n, brought_back<T>(acc[j][i], back), brought_back<T>(acc[j + 1][i], back), have, lane);
             }
         }
     }
@@ -250,11 +320,12 @@ __global__ void __launch_bounds__(256) tr_ff_join_kernel(FfGradient f)
     const int z = blockIdx.y;
     const i64 columns = f.b.index, ld = partial_ld(columns), all = f.rows * (ld / 4);
     const float* partial = f.partial + (i64)z * f.parts * f.rows * ld;
+    const float back = __is_same(T, _Float16) && f.back ? *f.back : 1.f;
     for (i64 at = (i64)blockIdx.x * 256 + threadIdx.x; at < all; at += (i64)gridDim.x * 256) {
         const i64 m = at / (ld / 4), n = (at - m * (ld / 4)) * 4;
         Float4 sum = *reinterpret_cast<const Float4*>(partial + at * 4);
         for (int p = 1; p < f.parts; ++p) sum += *reinterpret_cast<const Float4*>(partial + (p * f.rows * ld + at * 4));
-        store4((T*)f.out[z] + m * f.ld[z] + n, sum, columns - n);
+        store4((T*)f.out[z] + m * f.ld[z] + n, brought_back<T>(sum, back), columns - n);
     }
 }
 

@@ -251,21 +251,26 @@ int ff_backward(const void* dh, i64 lddh, const void* x, i64 ldx, const void* wg
     const i64 ldd = padded_units(F, sizeof(T));
     T* dg = (T*)workspace;
     T* du = dg + M * ldd;
-    const size_t units = ebsp_gated_ff_workspace_bytes(M, F, sizeof(T) == 4 ? EBSP_F32 : EBSP_BF16);
+    constexpr bool F16 = __is_same(T, _Float16);
+    const size_t units = ebsp_gated_ff_workspace_bytes(M, F, sizeof(T) == 4 ? EBSP_F32 : F16 ? EBSP_F16 : EBSP_BF16);
     float* partial = (float*)((char*)workspace + units);
+    float* largest = F16 && units ? (float*)((char*)workspace + units - RANGE_BYTES) : nullptr;
+    float* back = largest ? largest + RANGE_BLOCKS : nullptr;
     Cut cx = dx_cut(M, K, F, sizeof(T)), cw = dw_cut(M, K, F, sizeof(T));
     const size_t px = partial_bytes(M, K, 1, cx), pw = partial_bytes(F, K, 2, cw);
     if (workspace_bytes < units + px + pw) cx.parts = cw.parts = 1;
     float* partial_w = cx.parts > 1 ? (float*)((char*)partial + px) : partial;
-    const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0}, 2, M, partial, cx.parts, cx.large};
-    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw}, 1, F, partial_w, cw.parts, cw.large};
+    const FfGradient to_x = {{{dg, du}, {ldd, ldd}, M, ldd}, {{wg, wu}, {ldwg, ldwu}, K, F}, {dx, nullptr}, {lddx, 0}, 2, M, partial, cx.parts, cx.large, back};
+    const FfGradient to_w = {{{dg, du}, {ldd, ldd}, ldd, M}, {{x, x}, {ldx, ldx}, K, M}, {dwg, dwu}, {lddw, lddw}, 1, F, partial_w, cw.parts, cw.large, back};
     const bool together = dx && dwg && M > 0 && F > 0 && !cx.large && !cw.large && gradient_direct<T, ROWS>(to_x) == gradient_direct<T, COLS>(to_w);
     for (bool launch : {false, true}) {                                      // both grids are looked at before anything is enqueued
         const i64 chunks = M * (ldd / PER_WORD4<T>);
         if (launch && chunks > 0) {
-            const i64 blocks = (chunks + 255) / 256;
-            LAUNCH(tr_ff_units_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), (const T*)dh, lddh, g, u,
-                   ldg, dg, du, ldd, M, F, act);
+            const i64 blocks = (chunks + 255) / 256, most = F16 ? RANGE_BLOCKS : 16384;
+            const dim3 grid((unsigned)(blocks < most ? blocks : most));
+            const FfUnits<T> form = {(const T*)dh, lddh, g, u, ldg, dg, du, ldd, M, F, act, largest, back};
+            LAUNCH(tr_ff_units_kernel<T>, grid, dim3(256), form);
+            if constexpr (F16) LAUNCH(tr_ff_rescale_kernel, grid, dim3(256), form, (int)grid.x);
         }
         if (together) {
             if (int rc = ff_gradients<T>(to_x, to_w, launch, st)) return rc;
@@ -452,7 +457,8 @@ size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype)
 {
     const int size = element_size(dtype);
     if (!size || M < 0 || F < 0 || M >= SIZE_MAX_DIM || F >= SIZE_MAX_DIM) return 0;
-    return ((size_t)2 * M * padded_units(F, size) * size + 255) / 256 * 256;
+    const size_t units = ((size_t)2 * M * padded_units(F, size) * size + 255) / 256 * 256;
+    return units && dtype == EBSP_F16 ? units + RANGE_BYTES : units;
 }
 
 int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, int64_t ldwg, const void* wu,
