@@ -325,8 +325,8 @@ def ebsp_merge_pushes(weights: torch.Tensor, pushes: torch.Tensor, iters: torch.
 
 class _GatedFF(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, wg, wu, act):
-        save = any(ctx.needs_input_grad)
+    def forward(ctx, x, wg, wu, act, graph):
+        save = graph and any(ctx.needs_input_grad)                           # (those are set with gradients off, too)
         h, g, u = ebsp_gated_ff_forward(x, wg, wu, act, save=save)
         if save:
             ctx.save_for_backward(x, wg, wu, g, u)
@@ -339,7 +339,7 @@ class _GatedFF(torch.autograd.Function):
         x, wg, wu, g, u = ctx.saved_tensors
         need = ctx.needs_input_grad
         dx, dwg, dwu = ebsp_gated_ff_backward(_plain_rows(dh), x, wg, wu, g, u, ctx.act, want_dx=need[0], want_dw=need[1] or need[2])
-        return dx, dwg if need[1] else None, dwu if need[2] else None, None
+        return dx, dwg if need[1] else None, dwu if need[2] else None, None, None
 
 
 def _plain_rows(t: torch.Tensor) -> torch.Tensor:
@@ -349,14 +349,12 @@ def _plain_rows(t: torch.Tensor) -> torch.Tensor:
 
 
 def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu") -> torch.Tensor:
-    """``act(x wg^T) * (x wu^T)`` for x [..., K], with gradients for all three tensors."""
+    """``act(x wg^T) * (x wu^T)`` for x [..., K], with gradients for all three tensors.  Forward-mode tangents are refused (NotImplementedError)."""
     if not isinstance(x, torch.Tensor) or x.dim() < 1:
         raise ValueError("x must be a tensor of shape [..., K]")
     rows = _plain_rows(x.reshape(x.shape[:-1].numel(), x.shape[-1]))
-    if torch.is_grad_enabled():
-        h = _GatedFF.apply(rows, wg, wu, act)
-    else:
-        h = ebsp_gated_ff_forward(rows, wg, wu, act)[0]                      # (autograd would have g and u saved)
+    # With gradients off too: a tangent of forward mode has to be refused, not lost.
+    h = _GatedFF.apply(rows, wg, wu, act, torch.is_grad_enabled())
     return h.reshape(*x.shape[:-1], wg.shape[0])
 
 

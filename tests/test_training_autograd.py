@@ -1,0 +1,44 @@
+"""The training operators as parts of an autograd graph, on the CPU: the entry points are replaced by plain torch operations."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    from paper_2001_01347_amd import training
+    seen = []
+
+    def forward(x, wg, wu, act="silu", save=False, **_):
+        seen.append(save)
+        with torch.no_grad():
+            g, u = x @ wg.t(), x @ wu.t()
+            return torch.nn.functional.silu(g) * u, g if save else None, u if save else None
+    monkeypatch.setattr(training, "ebsp_gated_ff_forward", forward)
+    return seen
+
+
+@pytest.mark.parametrize("place", range(3))
+@pytest.mark.parametrize("mode", [torch.enable_grad, torch.no_grad])
+def test_gated_ff_does_not_lose_a_tangent(calls, mode, place):
+    """Forward mode does not depend on whether gradients are on: a tangent is refused in either case."""
+    import torch.autograd.forward_ad as forward_ad
+    from paper_2001_01347_amd import training
+    args = [torch.randn(4, 16), torch.randn(8, 16), torch.randn(8, 16)]
+    with mode(), forward_ad.dual_level():
+        args[place] = forward_ad.make_dual(args[place], torch.ones_like(args[place]))
+        with pytest.raises(NotImplementedError):
+            training.gated_ff(*args)
+
+
+def test_gated_ff_saves_the_products_for_a_backward_pass_alone(calls):
+    from paper_2001_01347_amd import training
+    x, wg, wu = torch.randn(2, 3, 16), torch.randn(8, 16), torch.randn(8, 16)
+    for needed in (False, True):
+        wg.requires_grad_(needed)
+        assert training.gated_ff(x, wg, wu).requires_grad == needed
+        with torch.no_grad():
+            assert not training.gated_ff(x, wg, wu).requires_grad
+        with torch.inference_mode():
+            assert training.gated_ff(x, wg, wu).shape == (2, 3, 8)
+    assert calls == [False, False, False, True, False, False]
