@@ -179,23 +179,23 @@ __device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1,
 // log2 of a sum, for differences from m; of a row without any finite logit it is taken as 0, so its p are 0.
 __device__ __forceinline__ float log2_sum(float s) { return s == 0.f ? 0.f : log2f(s); }
 
-// The row's loss, from its statistics.
+// The row's loss, from its statistics.  A logit's distance from the largest is not multiplied before its weight is: at a place masked with the lowest
+// value of bf16 or fp32 the loss is a number of that size, and log2(e) times it, or a sum of several, would be none.
 template <int NT, class T>
 __device__ __forceinline__ float row_loss(const Distill& d, const Row& row, Entries& e, float m, float lt, float l1)
 {
-    const float ct = LOG2E / d.temperature;
-    float sum = 0.f;
+    const float unit = LN2 * d.temperature, weight = d.kl * d.temperature;
+    float sum = 0.f;                                                         // weight * T sum_k q_k (log q_k - log p), weighted term by term
     for (int k = threadIdx.x; k < d.top; k += NT) {
         const float q = e.q[k];
         if (q == 0.f) continue;
         const float s = e.s[k];
-        const float logp = s == -INFINITY ? s : (s - m) * ct - lt;
-        sum += q * (log2f(q) - logp);
+        sum += s == -INFINITY ? weight * INFINITY : weight * q * fmaf(unit, log2f(q) + lt, -(s - m));
     }
     sum = block_reduce<NT>(sum, e.scalar, [](float a, float b) { return a + b; });
-    float loss = row.any ? d.kl * d.temperature * d.temperature * (LN2 * sum) : 0.f;
+    float loss = row.any ? sum : 0.f;
     const float s = row.label_logit;
-    if (row.label >= 0) loss -= d.ce * (s == -INFINITY ? s : LN2 * ((s - m) * LOG2E - l1));
+    if (row.label >= 0) loss -= d.ce * (s == -INFINITY ? s : (s - m) - LN2 * l1);
     return loss;
 }
 
