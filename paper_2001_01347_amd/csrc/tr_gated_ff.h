@@ -38,9 +38,10 @@ __device__ __forceinline__ void activation_both(int act, float g, float& a, floa
         d = s * (1.f + g * (1.f - s));
         break;
     }
-    case EBSP_ACT_SIGMOID: {
-        a = sigmoid(g);
-        d = a * (1.f - a);
+    case EBSP_ACT_SIGMOID: {                                                 // a (1 - a) from e^-|g|: 1 - a has no digits left for large g
+        const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e);
+        a = g < 0.f ? e * r : r;
+        d = e * r * r;
         break;
     }
     case EBSP_ACT_RELU:

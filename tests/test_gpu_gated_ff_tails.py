@@ -37,3 +37,15 @@ def test_gelu_of_negative_numbers(dtype):
     _within(h, g * cdf, rel * (g * cdf).abs(), dtype)
     _within(a, g * cdf, rel * (g * cdf).abs(), dtype)
     _within(d, cdf + g * pdf, rel * (cdf + (g * pdf).abs()), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sigmoid_of_large_numbers(dtype):
+    g = torch.arange(-128, 129, device="cuda", dtype=torch.float64) / 2      # up to 64 either way
+    g = g.to(dtype).double()
+    s, other = torch.sigmoid(g), torch.sigmoid(-g)
+    rel = 2.0 ** -19 + 2.0 ** -21 * g.abs()
+    h, d, a = _results("sigmoid", g, dtype)
+    _within(h, s, rel * s, dtype)
+    _within(a, s, rel * s, dtype)
+    _within(d, s * other, rel * s * other, dtype)
