@@ -384,6 +384,11 @@ def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch
     if not isinstance(logits, torch.Tensor) or logits.dim() < 1:
         raise ValueError("logits must be a tensor of shape [..., V]")
     lead = logits.shape[:-1]
+    for name, t in (("top_index", top_index), ("top_logit", top_logit)):     # (a reshape alone would take rows in another order)
+        if not isinstance(t, torch.Tensor) or t.dim() != logits.dim() or t.shape[:-1] != lead:
+            raise ValueError(f"{name} must be a tensor of shape [..., top], with the leading dimensions of logits")
+    if labels is not None and (not isinstance(labels, torch.Tensor) or labels.shape != lead):
+        raise ValueError("labels must be a tensor of the leading dimensions of logits")
     rows = _plain_rows(logits.reshape(lead.numel(), logits.shape[-1]))
     entries = [t.reshape(lead.numel(), t.shape[-1]).contiguous() for t in (top_index, top_logit)]
     flat = None if labels is None else labels.reshape(lead.numel()).contiguous()

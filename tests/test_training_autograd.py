@@ -42,3 +42,24 @@ def test_gated_ff_saves_the_products_for_a_backward_pass_alone(calls):
         with torch.inference_mode():
             assert training.gated_ff(x, wg, wu).shape == (2, 3, 8)
     assert calls == [False, False, False, True, False, False]
+
+
+@pytest.fixture
+def losses(monkeypatch):
+    from paper_2001_01347_amd import training
+
+    def forward(logits, top_index, top_logit, temperature, kl_weight, labels, ce_weight):
+        return logits.sum(dim=1), torch.zeros(logits.shape[0], 3), None
+    monkeypatch.setattr(training, "ebsp_distill_forward", forward)
+
+
+def test_distill_loss_takes_matching_rows_only(losses):
+    """Entries and labels whose leading dimensions are others, though as many, belong to other rows."""
+    from paper_2001_01347_amd import training
+    logits, index, values, labels = torch.randn(2, 3, 50), torch.zeros(2, 3, 4, dtype=torch.int64), torch.randn(2, 3, 4), torch.zeros(2, 3, dtype=torch.int64)
+    assert training.distill_loss(logits, index, values, 2.0, 0.5, labels, 0.5).shape == (2, 3)
+    assert training.distill_loss(logits[0, 0], index[0, 0], values[0, 0], labels=labels[0, 0], ce_weight=0.5).shape == ()
+    for bad in (dict(top_index=index.transpose(0, 1)), dict(top_logit=values.transpose(0, 1)), dict(labels=labels.t()), dict(top_index=index.reshape(6, 4)),
+                dict(labels=labels.reshape(6)), dict(top_index=None), dict(top_logit=[1.0]), dict(labels=7), dict(top_index=index[:1])):
+        with pytest.raises(ValueError):
+            training.distill_loss(**{**dict(logits=logits, top_index=index, top_logit=values, labels=labels, ce_weight=0.5), **bad})
