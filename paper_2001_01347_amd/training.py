@@ -126,8 +126,8 @@ def _ff_operands(x, wg, wu):
     M, K = _matrix("x", x)
     F, _ = _matrix("wg", wg)
     dev, dt = x.device, x.dtype
-    return code, M, K, F, dev, dt, (x.data_ptr(), _rows("x", x, dev, dt, (M, K)), wg.data_ptr(), _rows("wg", wg, dev, dt, (F, K)),
-                                    wu.data_ptr(), _rows("wu", wu, dev, dt, (F, K)))
+    ldx, ldwg, ldwu = _rows("x", x, dev, dt, (M, K)), _rows("wg", wg, dev, dt, (F, K)), _rows("wu", wu, dev, dt, (F, K))
+    return code, M, K, F, dev, dt, (x.data_ptr(), ldx, wg.data_ptr(), ldwg, wu.data_ptr(), ldwu)
 
 
 def ebsp_gated_ff_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu", save: bool = False,
