@@ -58,7 +58,8 @@ extern "C" {
  *               needs.  Both NULL where there will be no backward pass; h
  *               alone is written then.
  * The others of one element type `dtype`; sums are held in 32 bits and rounded once.
- * M == 0 or F == 0 is a valid no-op, K == 0 gives zero products.
+ * M == 0 or F == 0 is a valid no-op, K == 0 gives zero products.  M, K and F are
+ * below 2^31, M x F below 2^56.
  *
  * ebsp_gated_ff_forward_split does the same with a workspace, 256-byte aligned:
  * where ebsp_gated_ff_forward_workspace_bytes(M, K, F, dtype) is not 0 and the

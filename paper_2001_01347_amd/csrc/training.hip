@@ -32,8 +32,11 @@ using namespace ebsp_host;
         }                                                                                  \
     } while (0)
 
-// Sizes up to here keep every product of two of them, in bytes, inside 64 bits.
+// Sizes up to here keep every product of two of them, in elements, inside 64 bits.
 constexpr i64 SIZE_MAX_DIM = 1ll << 31;
+
+// Results of so many elements are refused: their bytes, several buffers of them together, stay inside 64 bits.
+constexpr i64 ELEMENTS_MAX = 1ll << 56;
 
 int element_size(int dtype) { return dtype == EBSP_BF16 || dtype == EBSP_F16 ? 2 : dtype == EBSP_F32 ? 4 : 0; }
 
@@ -51,6 +54,7 @@ int check_sizes(i64 M, i64 K, i64 F, int dtype, int act)
     if (act < EBSP_ACT_SILU || act > EBSP_ACT_SIGMOID) return fail(EBSP_ERR_ARGUMENT, "act must be one of EBSP_ACT_*");
     if (M < 0 || K < 0 || F < 0 || M >= SIZE_MAX_DIM || K >= SIZE_MAX_DIM || F >= SIZE_MAX_DIM)
         return fail(EBSP_ERR_SHAPE, "invalid shape: M, K and F must be 0 to 2^31 - 1");
+    if (M * F >= ELEMENTS_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: M x F must be below 2^56");
     return EBSP_OK;
 }
 
@@ -456,7 +460,7 @@ size_t ebsp_gated_ff_split_workspace_bytes(int64_t M, int64_t K, int64_t F, int3
 size_t ebsp_gated_ff_workspace_bytes(int64_t M, int64_t F, int32_t dtype)
 {
     const int size = element_size(dtype);
-    if (!size || M < 0 || F < 0 || M >= SIZE_MAX_DIM || F >= SIZE_MAX_DIM) return 0;
+    if (!size || M < 0 || F < 0 || M >= SIZE_MAX_DIM || F >= SIZE_MAX_DIM || M * F >= ELEMENTS_MAX) return 0;
     const size_t units = ((size_t)2 * M * padded_units(F, size) * size + 255) / 256 * 256;
     return units && dtype == EBSP_F16 ? units + RANGE_BYTES : units;
 }

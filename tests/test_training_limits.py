@@ -1,0 +1,34 @@
+"""The limits of the training operators' sizes as the headers state them, on the host."""
+import ctypes
+import os
+
+import pytest
+
+NULL = ctypes.c_void_p(0)
+ONE = ctypes.c_void_p(256)           # never dereferenced: the calls below fail validation, or find no device
+BF16, F16, F32 = 0, 1, 2
+LARGEST = (1 << 31) - 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2001_01347_amd import build, training, zipline
+    if not os.path.exists(zipline.LIB_PATH):
+        build.build()
+    return training.load()
+
+
+@pytest.mark.parametrize("dtype,size", [(BF16, 2), (F16, 2), (F32, 4)])
+def test_a_workspace_size_does_not_wrap(lib, dtype, size):
+    """What is asked for holds dg and du; sizes whose bytes pass 64 bits are refused."""
+    for M in (1, 1000, 1 << 20, 1 << 25, 1 << 28, 1 << 30, LARGEST):
+        for F in (1, 4096, 1 << 25, 1 << 28, 1 << 30, LARGEST):
+            least = lib.ebsp_gated_ff_workspace_bytes(M, F, dtype)
+            split = lib.ebsp_gated_ff_split_workspace_bytes(M, 64, F, dtype)
+            if M * F < 1 << 56:
+                assert least >= 2 * M * F * size and split >= least
+            else:
+                assert least == 0 and split == 0
+                assert lib.ebsp_gated_ff_backward(ONE, F, ONE, 64, ONE, 64, ONE, 64, ONE, ONE, F, M, 64, F, dtype, 0, ONE, 64, ONE, ONE, 64, ONE,
+                                                  1 << 40, NULL) == -2
+                assert lib.ebsp_gated_ff_forward(ONE, 64, ONE, 64, ONE, 64, M, 64, F, dtype, 0, ONE, F, NULL, NULL, F, NULL) == -2
