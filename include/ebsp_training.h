@@ -178,8 +178,8 @@ int ebsp_distill_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V,
  *                    itself; both NULL: no momentum
  *   pull         out [n] of type pull_dtype: w' rounded, what the workers fetch; or NULL
  * Sums are held in 32 bits and run in an order that P and n fix: results do not
- * vary.  P is 1 to
- * EBSP_MERGE_WORKERS_MAX, n below 2^34.  n == 0 is a valid no-op.
+ * vary.  P is 1 to EBSP_MERGE_WORKERS_MAX, n below 2^34, or at most 2^34 - 1024
+ * where the pushes are fp32.  n == 0 is a valid no-op.
  */
 int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, int32_t dtype, const int32_t* iters,
                       const float* weights, const float* velocity, float lr, float momentum, int32_t nesterov,

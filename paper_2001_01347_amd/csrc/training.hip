@@ -390,8 +390,7 @@ int run_distill(Distill& d, int dtype, bool grad, void* workspace, size_t worksp
 template <class T, int SPLIT>
 int merge_split(const Merge& g, hipStream_t st)
 {
-    const i64 per = (SPLIT == 1 ? 256 : 64) * PER_WORD4<T>;
-    if (!launchable((g.n + per - 1) / per, SPLIT == 1 ? 256 : SPLIT * 64)) return fail(EBSP_ERR_SHAPE, "too many weights for one call");
+    const i64 per = (SPLIT == 1 ? 256 : 64) * PER_WORD4<T>;                  // (launchable: n is below 2^34 or, of 4 to a thread, no more than 2^34 - 1024)
     LAUNCH_LDS((tr_merge_kernel<T, SPLIT>), dim3((unsigned)((g.n + per - 1) / per)), dim3(SPLIT == 1 ? 256 : SPLIT * 64), g.P * sizeof(Share), g);
     return EBSP_OK;
 }
@@ -550,6 +549,7 @@ int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, 
     if (!size || (pull && !element_size(pull_dtype))) return fail(EBSP_ERR_ARGUMENT, "dtype and pull_dtype must be EBSP_BF16, EBSP_F16 or EBSP_F32");
     if (P < 1 || P > EBSP_MERGE_WORKERS_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: P must be 1 to EBSP_MERGE_WORKERS_MAX");
     if (n < 0 || n >= 1ll << 34) return fail(EBSP_ERR_SHAPE, "invalid shape: n must be 0 to 2^34 - 1");
+    if (size == 4 && n > (1ll << 34) - 1024) return fail(EBSP_ERR_SHAPE, "invalid shape: n must be 0 to 2^34 - 1024 for pushes in fp32");
     if (n == 0) return EBSP_OK;
     if (!pushes || !iters || !weights || !weights_out) return fail(EBSP_ERR_NULL, "pushes, iters, weights and weights_out must not be NULL");
     if (!velocity != !velocity_out) return fail(EBSP_ERR_NULL, "velocity and velocity_out must both be given or both be NULL");

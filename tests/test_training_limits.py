@@ -32,3 +32,17 @@ def test_a_workspace_size_does_not_wrap(lib, dtype, size):
                 assert lib.ebsp_gated_ff_backward(ONE, F, ONE, 64, ONE, 64, ONE, 64, ONE, ONE, F, M, 64, F, dtype, 0, ONE, 64, ONE, ONE, 64, ONE,
                                                   1 << 40, NULL) == -2
                 assert lib.ebsp_gated_ff_forward(ONE, 64, ONE, 64, ONE, 64, M, 64, F, dtype, 0, ONE, F, NULL, NULL, F, NULL) == -2
+
+
+@pytest.mark.parametrize("dtype,most", [(BF16, (1 << 34) - 1), (F16, (1 << 34) - 1), (F32, (1 << 34) - 1024)])
+def test_a_merge_of_the_most_weights(lib, dtype, most):
+    """The largest n that the header names is taken (without a GPU: refused for that alone); one more is refused for its size."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present: the call would run")
+
+    def merge(n):
+        return lib.ebsp_merge_pushes(ONE, n, 2, n, dtype, ONE, ONE, NULL, 1.0, 0.0, 0, ONE, NULL, NULL, 0, NULL)
+    assert merge(most) == -5 and merge(most + 1) == -2
+    per = 256 * (4 if dtype == F32 else 8)                                   # weights of a workgroup; a launch counts its threads in 32 bits
+    assert (most + per - 1) // per * 256 <= 0xFFFFFFFF
