@@ -134,7 +134,8 @@ int ebsp_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t 
  *                 256-byte aligned (may be NULL when that is 0)
  * A row without entries has no first term and its gradient no p.  Logits of -inf
  * (masked places) have p = 0, and where the teacher gives such a place weight the
- * loss is +inf.  ebsp_distill_forward gives the loss, ebsp_distill_backward the
+ * loss is +inf.  A temperature is positive, log2(e) / T a finite float.
+ * ebsp_distill_forward gives the loss, ebsp_distill_backward the
  * gradient from its stats, ebsp_distill_loss_grad both in one pass where a step's
  * dloss is known beforehand (1 / N for a mean).  top_index and top_logit may be
  * NULL when top is 0.  N == 0 is a valid no-op; V is at least 1; more than some

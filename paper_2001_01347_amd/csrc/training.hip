@@ -353,6 +353,7 @@ int check_distill(const Distill& d, int dtype, int index_bytes)
     if (d.N < 0 || d.N >= SIZE_MAX_DIM || d.V < 1 || d.V >= SIZE_MAX_DIM) return fail(EBSP_ERR_SHAPE, "invalid shape: N must be 0 and V 1 to 2^31 - 1");
     if (d.top < 0 || d.top > TOP_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: top must be 0 to EBSP_DISTILL_TOP_MAX");
     if (!(d.temperature > 0.f) || d.temperature > FLT_MAX) return fail(EBSP_ERR_ARGUMENT, "temperature must be a positive number");
+    if (LOG2E / d.temperature > FLT_MAX) return fail(EBSP_ERR_ARGUMENT, "temperature is too small: its inverse is no number any more");
     if (d.N == 0) return EBSP_OK;
     if (!d.logits || (d.top > 0 && (!d.top_index || !d.top_logit))) return fail(EBSP_ERR_NULL, "logits, top_index and top_logit must not be NULL");
     if (!stride_ok(d.ld, d.V) || (d.top > 0 && !stride_ok(d.ldt, d.top))) return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");

@@ -46,3 +46,12 @@ def test_a_merge_of_the_most_weights(lib, dtype, most):
     assert merge(most) == -5 and merge(most + 1) == -2
     per = 256 * (4 if dtype == F32 else 8)                                   # weights of a workgroup; a launch counts its threads in 32 bits
     assert (most + per - 1) // per * 256 <= 0xFFFFFFFF
+
+
+def test_a_temperature_without_an_inverse(lib):
+    """Below some 4e-39 log2(e) / T is infinite, and would make a NaN of the largest logit's distance from itself."""
+    def forward(T):
+        return lib.ebsp_distill_forward(ONE, 100, 4, 100, BF16, ONE, 8, ONE, BF16, 8, 8, NULL, T, 1.0, 0.0, NULL, ONE, NULL, NULL, 0, NULL)
+    # (a temperature that is taken is refused for the missing loss)
+    assert forward(1e-39) == -6 and forward(4.2e-39) == -6 and forward(4.3e-39) == -1 and forward(1e-38) == -1
+    assert forward(1.0) == -1 and forward(3.4e38) == -1 and forward(0.0) == -6
