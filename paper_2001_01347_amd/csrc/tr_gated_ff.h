@@ -10,17 +10,38 @@ namespace {
 // (The hardware's exponential and reciprocal are good to an ulp.)
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)); }
 
-// Phi(g), by the error function's complement: 1 + erf(g / sqrt 2) has no digits left where g is well below 0.  (It takes longer: forward 2048 x 2048 x 8192
-// bf16 125 us, so 131; with gradients 1021 x 1000 x 2730 86, so 88, 8192 x 4096 x 12288 4021, so 4050.)
-__device__ __forceinline__ float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678118654752f); }
+// e^(-g^2 / 2).
+__device__ __forceinline__ float bell(float g) { return __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g); }
 
+// Phi(g), with `e` = bell(g).  0.5 (1 + erf(g / sqrt 2)) would have no digits left where g is well below 0: it is formed from Phi(-|g|).  Results of 32 bits take the
+// error function's complement; for those of 16 bits, Phi(-a) e^(a^2 / 2) = t q(t) with t = 1 / (1 + 0.3 a) and a polynomial fitted to the least largest relative
+// error over 0 <= a <= 14.5 (1.7e-7; 6e-7 as evaluated), which is shorter in an epilogue that has it 128 times.  us, with the error function / its complement / this:
+// forward 2048 x 2048 x 8192 bf16 122 / 126 / 116; with gradients 1021 x 1000 x 2730 86.8 / 88.1 / 83.8, 8192 x 64 x 12288 773 / 797 / 744.
+template <class T>
+__device__ __forceinline__ float normal_cdf(float g, float e)
+{
+    if constexpr (sizeof(T) == 4) return 0.5f * erfcf(g * -0.70710678118654752f);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3f * fabsf(g));
+    float q = 0.0354237035f;
+    q = fmaf(q, t, -0.156158328f);
+    q = fmaf(q, t, 0.204556584f);
+    q = fmaf(q, t, -0.0520338379f);
+    q = fmaf(q, t, 0.127691686f);
+    q = fmaf(q, t, 0.100175969f);
+    q = fmaf(q, t, 0.120712131f);
+    q = fmaf(q, t, 0.119632006f);
+    const float tail = q * t * e;
+    return g < 0.f ? tail : 1.f - tail;
+}
+
+template <class T>
 __device__ __forceinline__ float activation(int act, float g)
 {
     switch (act) {
     case EBSP_ACT_SILU: return g * sigmoid(g);
     case EBSP_ACT_SIGMOID: return sigmoid(g);
     case EBSP_ACT_RELU: return g < 0.f ? 0.f : g;                            // (a NaN stays one)
-    case EBSP_ACT_GELU: return g * normal_cdf(g);
+    case EBSP_ACT_GELU: return g * normal_cdf<T>(g, bell(g));
     default: {                                                               // 0.5 g (1 + tanh z) = g sigmoid(2 z)
         const float c = fminf(fmaxf(g, -16.f), 16.f);                        // tanh is 1 long before; the cube stays finite
         const float z = 0.79788456080286536f * (c + 0.044715f * c * c * c);
@@ -29,6 +50,7 @@ __device__ __forceinline__ float activation(int act, float g)
     }
 }
 
+template <class T>
 __device__ __forceinline__ void activation_both(int act, float g, float& a, float& d)
 {
     switch (act) {
@@ -49,9 +71,9 @@ __device__ __forceinline__ void activation_both(int act, float g, float& a, floa
         d = g > 0.f ? 1.f : 0.f;
         break;
     case EBSP_ACT_GELU: {
-        const float cdf = normal_cdf(g);
+        const float e = bell(g), cdf = normal_cdf<T>(g, e);
         a = g * cdf;
-        d = cdf + g * 0.39894228040143268f * __builtin_amdgcn_exp2f(-0.72134752044448170f * g * g);
+        d = cdf + g * 0.39894228040143268f * e;
         break;
     }
     default: {
@@ -115,7 +137,7 @@ __global__ void __launch_bounds__(TL::NT, 2) tr_ff_forward_kernel(FfForward f)
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[k][e] = activation(f.act, acc[j + k][i][e]) * acc[j + k + HALF][i][e];
+                for (int e = 0; e < 4; ++e) h[k][e] = activation<T>(f.act, acc[j + k][i][e]) * acc[j + k + HALF][i][e];
             store_pair((T*)f.h + m * f.ldh + n, h[0], h[1], have, lane);
             if (f.g) {
                 store_pair(f.g + m * f.ldg + n, acc[j][i], acc[j + 1][i], have, lane);
@@ -140,7 +162,7 @@ __global__ void __launch_bounds__(256) tr_ff_forward_join_kernel(FfForward f)
             u += *reinterpret_cast<const Float4*>(p + up);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
+        for (int e = 0; e < 4; ++e) h[e] = activation<T>(f.act, g[e]) * u[e];
         store4((T*)f.h + m * f.ldh + n, h, have);
         if (f.g) {
             store4(f.g + m * f.ldg + n, g, have);
@@ -186,7 +208,7 @@ __device__ __forceinline__ float form_units(const FfUnits<T>& f, float by)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, d;
-            activation_both(f.act, pg[i / 4].v[i % 4], a, d);
+            activation_both<T>(f.act, pg[i / 4].v[i % 4], a, d);
             const float h = to_float(ph.v[i]);
             const bool in = c + i < f.F;
             const float dg = in ? h * pu[i / 4].v[i % 4] * d : 0.f, du = in ? h * a : 0.f;
@@ -405,7 +427,7 @@ __global__ void __launch_bounds__(TF::NT, 4) tr_ff_few_kernel(FfForward f)
             u += part[p][FM + wave][lane];
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = activation(f.act, g[e]) * u[e];
+        for (int e = 0; e < 4; ++e) h[e] = activation<T>(f.act, g[e]) * u[e];
         store4((T*)f.h + m * f.ldh + n, h, have);
         if (f.g) {
             store4(f.g + m * f.ldg + n, g, have);

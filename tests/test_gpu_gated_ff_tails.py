@@ -49,3 +49,14 @@ def test_sigmoid_of_large_numbers(dtype):
     _within(h, s, rel * s, dtype)
     _within(a, s, rel * s, dtype)
     _within(d, s * other, rel * s * other, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_gelu_around_nought(dtype):
+    g = torch.arange(-24, 97, device="cuda", dtype=torch.float64) / 8        # -3 to 12: normal numbers in fp16 too
+    cdf, pdf = 0.5 * torch.special.erfc(-g / math.sqrt(2)), torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    rel = 2.0 ** -19 + 2.0 ** -21 * (g * g / 2)
+    h, d, a = _results("gelu", g, dtype)
+    _within(h, g * cdf, rel * (g * cdf).abs(), dtype)
+    _within(a, g * cdf, rel * (g * cdf).abs(), dtype)
+    _within(d, cdf + g * pdf, rel * (cdf + (g * pdf).abs()), dtype)
