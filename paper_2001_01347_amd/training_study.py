@@ -17,6 +17,7 @@ from typing import Dict, List
 
 WIDTH, UNITS, VOCABULARY, TOP = 128, 320, 1000, 16
 BATCH = 64
+WORKERS_MAX = 16                                                             # of the cluster that the study draws its workers from
 TEMPERATURE, KL_WEIGHT, CE_WEIGHT = 2.0, 0.9, 0.1
 LOCAL_LR, SERVER_LR, MOMENTUM = 2.0, 1.0, 0.5
 
@@ -65,6 +66,8 @@ def _loss(parts, x, index, values, labels):
 
 def train(workers: int = 8, supersteps: int = 24, lookahead: int = 15, seed: int = 0) -> List[Dict[str, float]]:
     """One row per superstep: the barrier's time (us), the iterations done, and the server's loss on data that no worker saw."""
+    if not 1 <= workers <= WORKERS_MAX or supersteps < 1 or lookahead < 1:
+        raise ValueError(f"a run has 1 to {WORKERS_MAX} workers, a superstep and a predicted iteration at least")
     import torch
     from . import training, workloads, zipline
 
@@ -107,10 +110,12 @@ def train(workers: int = 8, supersteps: int = 24, lookahead: int = 15, seed: int
 
 def main() -> int:
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--workers", type=int, default=8, choices=range(1, 17), metavar="1..16")
+    ap.add_argument("--workers", type=int, default=8, choices=range(1, WORKERS_MAX + 1), metavar=f"1..{WORKERS_MAX}")
     ap.add_argument("--supersteps", type=int, default=24)
     ap.add_argument("--lookahead", type=int, default=15, help="predicted iterations per worker (R)")
     args = ap.parse_args()
+    if args.supersteps < 1 or args.lookahead < 1:
+        ap.error("--supersteps and --lookahead must be at least 1")
     print("| | supersteps | iterations | time (s) | loss at the start | loss at the end |")
     print("|---|---|---|---|---|---|")
     for name, R in (("BSP", 1), (f"ElasticBSP, R = {args.lookahead}", args.lookahead)):
