@@ -31,7 +31,9 @@ struct ForwardCut {
 // 64 x 1024 x 4096 10 / 14 / 14, 341 x 3984 x 286 15 / 18 / 42, 341 x 3981 x 286 (rows at any alignment) 43 / 25 / 68, 64 x 4096 x 4096 28 / 21 / 43,
 // 192 x 4096 x 1024 24 / 17 / 35, 100 x 4096 x 3000 43 / 20 / 42, 657 x 3392 x 936 55 / 23 / 31, 300 x 1024 x 2000 19 / 16 / 14; fp32: 64 x 4096 x 4096
 // 61 / 72 / 248, 300 x 512 x 512 10 / 18 / 36, 256 x 1024 x 2816 48 / 44 / 67, 600 x 2048 x 1024 88 / 63 / 127, 384 x 4096 x 4096 354 / 198 / 252.  The kernel's
-// squares hold 64 tokens, or 32 where that makes too few workgroups (64 x 4096 x 1024 18, so 24).
+// squares hold 64 tokens, or 32 where that makes too few workgroups (64 x 4096 x 1024 18, so 24).  The rule knows sizes alone, as the workspace is asked for by
+// them: rows of whole 16-byte chunks that a view puts at other addresses or distances are taken for aligned, and can run as the 43 of the pair above where tiles in parts
+// would take 25.
 inline ForwardCut forward_cut(i64 M, i64 K, i64 F, int size, bool room)
 {
     const i64 groups = tiles_of(M, F, 64, 16), tiles = tiles_of(M, F, 128, 64), steps = (K * size + 127) / 128;

@@ -200,7 +200,8 @@ __device__ __forceinline__ float row_loss(const Distill& d, const Row& row, Entr
 }
 
 // p1 beside p: not wanted or of the same temperature, its square (temperature 2: an exponential takes four times as long as a product),
-// or by itself.
+// or by itself, at any other temperature.  Loss and gradient, us, at temperatures 1 / 2 / 4: 4096 rows of 128000 in bf16 472 / 479 / 501, of 32000 122 / 121 / 124,
+// 2048 of 128000 in fp32 465 / 478 / 491.
 enum Second { ONE, SQUARE, APART };
 
 __host__ __device__ __forceinline__ Second second_of(const Distill& d)

@@ -334,7 +334,8 @@ int merge_split(const Merge& g, hipStream_t st)
     return EBSP_OK;
 }
 
-// The workers are split over a workgroup's waves where the chunks alone make too few waves to keep memory busy.  bf16, us, with 1 / 4 / 16
+// The workers are split over a workgroup's waves where the chunks alone make too few waves to keep memory busy.  The rule looks at the chunks and not at the
+// workers; of the sizes here it is off at 512 x 1048593 alone, which 16 parts would do in 202.  bf16, us, with 1 / 4 / 16
 // parts: 1024 x 65539 322 / 92 / 36, 256 x 200000 (391 waves) 81 / 27 / 20, 64 x 500000 (977) 25 / 14 / 17, 1024 x 524309 (1025) 508 / 200 / 217,
 // 64 x 1 M (1954) 27 / 23 / 29, 512 x 1048593 (2049) 292 / 239 / 202, 64 x 2 M (3907) 43 / 43 / 55, 256 x 2 M (4096) 184 / 201 / 211, 16 x 2 M
 // 16 / 17 / 33.

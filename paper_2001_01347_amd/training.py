@@ -354,7 +354,10 @@ def _has_tangent(*tensors) -> bool:
 
 
 def gated_ff(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str = "silu") -> torch.Tensor:
-    """``act(x wg^T) * (x wu^T)`` for x [..., K], with gradients for all three tensors.  Forward-mode tangents are refused (NotImplementedError)."""
+    """``act(x wg^T) * (x wu^T)`` for x [..., K], with gradients for all three tensors.
+
+    All three are of one type, in and outside autocast: nothing is cast.  For the backward pass the two products are kept in float32, 8
+    bytes a token and unit.  Forward-mode tangents are refused (NotImplementedError)."""
     if not isinstance(x, torch.Tensor) or x.dim() < 1:
         raise ValueError("x must be a tensor of shape [..., K]")
     rows = _plain_rows(x.reshape(x.shape[:-1].numel(), x.shape[-1]))
