@@ -385,6 +385,11 @@ class _Distill(torch.autograd.Function):
         return grad, None, None, None, None, None, None
 
 
+def _same_rows(shape: torch.Size, lead: torch.Size) -> bool:
+    """Whether rows of these dimensions stand in the order of those of ``lead``: the same but for ones, or all as one dimension."""
+    return [n for n in shape if n != 1] in ([n for n in lead if n != 1], [n for n in (lead.numel(),) if n != 1])
+
+
 def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, temperature: float = 1.0, kl_weight: float = 1.0,
                  labels: Optional[torch.Tensor] = None, ce_weight: float = 0.0) -> torch.Tensor:
     """The distillation loss of every row [...], for logits [..., V] and teacher entries [..., top], with the logits' gradient.
@@ -395,10 +400,10 @@ def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch
         raise ValueError("logits must be a tensor of shape [..., V]")
     lead = logits.shape[:-1]
     for name, t in (("top_index", top_index), ("top_logit", top_logit)):     # (a reshape alone would take rows in another order)
-        if not isinstance(t, torch.Tensor) or t.dim() != logits.dim() or t.shape[:-1] != lead:
-            raise ValueError(f"{name} must be a tensor of shape [..., top], with the leading dimensions of logits")
-    if labels is not None and (not isinstance(labels, torch.Tensor) or labels.shape != lead):
-        raise ValueError("labels must be a tensor of the leading dimensions of logits")
+        if not isinstance(t, torch.Tensor) or t.dim() < 1 or not _same_rows(t.shape[:-1], lead):
+            raise ValueError(f"{name} must be a tensor of shape [..., top], with the leading dimensions of logits or with those as one")
+    if labels is not None and (not isinstance(labels, torch.Tensor) or not _same_rows(labels.shape, lead)):
+        raise ValueError("labels must be a tensor of the leading dimensions of logits, or of those as one")
     rows = _plain_rows(logits.reshape(lead.numel(), logits.shape[-1]))
     entries = [t.reshape(lead.numel(), t.shape[-1]).contiguous() for t in (top_index, top_logit)]
     flat = None if labels is None else labels.reshape(lead.numel()).contiguous()

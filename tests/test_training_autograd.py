@@ -58,8 +58,12 @@ def test_distill_loss_takes_matching_rows_only(losses):
     from paper_2001_01347_amd import training
     logits, index, values, labels = torch.randn(2, 3, 50), torch.zeros(2, 3, 4, dtype=torch.int64), torch.randn(2, 3, 4), torch.zeros(2, 3, dtype=torch.int64)
     assert training.distill_loss(logits, index, values, 2.0, 0.5, labels, 0.5).shape == (2, 3)
+    # the rows as one dimension, and dimensions of one, leave the order as it is
+    assert training.distill_loss(logits, index.reshape(6, 4), values, 2.0, 0.5, labels.reshape(6), 0.5).shape == (2, 3)
+    assert training.distill_loss(logits.reshape(2, 3, 1, 50), index, values.reshape(6, 4), 2.0, 0.5, labels.reshape(1, 2, 3), 0.5).shape == (2, 3, 1)
+    assert training.distill_loss(logits[:0], index[:0], values[:0], labels=labels[:0], ce_weight=0.5).shape == (0, 3)
     assert training.distill_loss(logits[0, 0], index[0, 0], values[0, 0], labels=labels[0, 0], ce_weight=0.5).shape == ()
-    for bad in (dict(top_index=index.transpose(0, 1)), dict(top_logit=values.transpose(0, 1)), dict(labels=labels.t()), dict(top_index=index.reshape(6, 4)),
-                dict(labels=labels.reshape(6)), dict(top_index=None), dict(top_logit=[1.0]), dict(labels=7), dict(top_index=index[:1])):
+    for bad in (dict(top_index=index.transpose(0, 1)), dict(top_logit=values.transpose(0, 1)), dict(labels=labels.t()),
+                dict(top_index=index.reshape(6, 4).t()), dict(top_index=None), dict(top_logit=[1.0]), dict(labels=7), dict(top_index=index[:1])):
         with pytest.raises(ValueError):
             training.distill_loss(**{**dict(logits=logits, top_index=index, top_logit=values, labels=labels, ce_weight=0.5), **bad})
