@@ -384,7 +384,7 @@ def _run_preference(state):
         loss, sums, saved, _ = training.ebsp_preference_forward(s, tokens, starts, **args)
         if case["mode"] == "loss":
             return loss, sums
-        return loss, sums, training.ebsp_preference_backward(s, tokens, starts, saved, state["dloss"], mean=case["mean"])
+        return loss, sums, training.ebsp_preference_backward(s, tokens, starts, saved, state["dloss"])
     has, at = tokens >= 0, tokens.clamp(min=0)
     e, total, z = _softmax(s, 1.0)
     logp = torch.where(has, z.gather(1, at[:, None])[:, 0] - torch.log(total[:, 0]), 0.0)
