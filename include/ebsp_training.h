@@ -186,6 +186,178 @@ int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, 
                       const float* weights, const float* velocity, float lr, float momentum, int32_t nesterov,
                       float* weights_out, float* velocity_out, void* pull, int32_t pull_dtype, void* stream);
 
+/*
+ * The residual stream around a block, and the norm in front of the next: a row x of
+ * the stream, a block's output b for it, weights w and w', a gate g, a scale a and
+ * kept elements z (see dropout, below):
+ *
+ *     h = b * (mean b^2 + eps)^-1/2      d = h * w'   (no post_weight: d = b)
+ *     y = x + a * g * z * d              n = y * (mean y^2 + eps)^-1/2 * w
+ *
+ * Without a branch y = x is not written, and n alone comes back.
+ *
+ *   x           in  [M][K] of type stream_dtype, rows ldx apart: dtype itself, or EBSP_F32
+ *   branch      in  [M][K] of type dtype, rows ldb apart, or NULL: none
+ *   weight      in  [K] of type dtype
+ *   post_weight in  [K] of type dtype, or NULL: no norm behind the block
+ *   gate        in  of type dtype: [K] where ldgate is 0, otherwise [M][K], rows
+ *                   ldgate apart; or NULL: 1
+ *   p, seed, offset, rng   dropout of the block's output, as below; p 0: none
+ *   y           out [M][K] of type stream_dtype, rows ldy apart; may be x itself (same rows)
+ *   n           out [M][K] of type dtype, rows ldn apart
+ *   stats       out [M][2] float: the two inverse roots, for the backward pass; or NULL
+ * Sums are held in 32 bits; n comes from y before y is rounded.  M == 0 or K == 0
+ * is a valid no-op, M is below 2^31, K below 2^30.
+ */
+int ebsp_residual_norm_forward(const void* x, int64_t ldx, const void* branch, int64_t ldb, int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype,
+                               const void* weight, const void* post_weight, const void* gate, int64_t ldgate, float scale, float eps, float p,
+                               uint64_t seed, uint64_t offset, const int64_t* rng, void* y, int64_t ldy, void* n, int64_t ldn, float* stats, void* stream);
+
+/*
+ * Its backward pass, from dy and dn (either may be NULL: zero) and the forward pass' y
+ * (x itself where there was no branch), stats and operands; the same p, seed, offset
+ * and rng give the same kept elements.
+ *
+ *   dx          out [M][K] of type stream_dtype, rows lddx apart; may be dy itself (same rows)
+ *   dbranch     out [M][K] of type dtype, rows lddb apart
+ *   dweight, dpost_weight   out [K] of type dtype
+ *   dgate       out of type dtype: [K] where ldgate is 0, otherwise [M][K], rows lddgate apart
+ *                   Each of the five may be NULL: not wanted.
+ *   workspace   at least ebsp_residual_norm_workspace_bytes(M, K) bytes, 256-byte
+ *               aligned; may be NULL where no gradient of [K] is wanted
+ * Columns are summed in 32 bits in an order that the sizes fix: results do not vary.
+ * M == 0 gives zero gradients of [K].
+ */
+size_t ebsp_residual_norm_workspace_bytes(int64_t M, int64_t K);
+int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* y, int64_t ldy, const void* branch, int64_t ldb,
+                                int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
+                                int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
+                                int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout: out = x / (1 - p) where an element is kept, otherwise 0 (whatever x is
+ * there).  Which are kept is computed, not stored, so the same call on a gradient is
+ * the backward pass.  p is taken to a multiple of 2^-16, and element k of row r is dropped where
+ * its 16 bits are below p * 2^16: those of number k % 8, counted from the low end of
+ * the first word, in the four words that Philox4x32 of seven rounds (Salmon et al.,
+ * 2011) makes of the counter (k / 8, r, offset's low and high word) and the key
+ * (seed's low and high word).
+ *
+ *   x      in  [M][K] of type dtype, rows ldx apart
+ *   rng    in  [2] int64 on the device: seed and offset; or NULL: the two arguments
+ *              (a replayed graph draws anew where the program moves the offset on)
+ *   out    out [M][K] of type dtype, rows ldout apart; may be x itself (same rows)
+ * M == 0 or K == 0 is a valid no-op, M is below 2^31, K below 2^30.
+ */
+int ebsp_dropout(const void* x, int64_t ldx, int64_t M, int64_t K, int32_t dtype, float p, uint64_t seed, uint64_t offset, const int64_t* rng,
+                 void* out, int64_t ldout, void* stream);
+
+/*
+ * Log-probabilities of tokens: for a row's logits s, its token t and a temperature T,
+ *
+ *     logp = log softmax(s / T)[t]     dlogp/ds[j] = ([j = t] - softmax(s / T)[j]) / T
+ *
+ *   logits  in  [N][V] of type dtype, rows ld apart
+ *   tokens  in  [N] int64; negative: none in this row, whose logits are not read then.
+ *               logp and the gradient of such a row are 0
+ *   logp    out [N] float
+ *   stats   out [N][3] float: what ebsp_token_logp_backward needs; or NULL
+ *   status  out [N] int32, or NULL: EBSP_STATUS_RANGE where a token is V or more; that
+ *               row counts as one without a token
+ *   dlogp   in  [N] float: dL/dlogp of every row
+ *   dlogits out [N][V] of type dtype, rows ldd apart: dL/ds.  May be the logits
+ *               themselves (same rows): they are overwritten then
+ *   workspace   at least ebsp_token_logp_workspace_bytes(N, V, dtype) bytes,
+ *               256-byte aligned (may be NULL when that is 0)
+ * Logits of -inf (masked places) weigh nothing; a token at such a place has logp -inf.
+ * A temperature is positive, log2(e) / T a finite float.  N == 0 is a valid no-op; V
+ * is at least 1; more than some four million rows are refused (EBSP_ERR_SHAPE).
+ */
+size_t ebsp_token_logp_workspace_bytes(int64_t N, int64_t V, int32_t dtype);
+int ebsp_token_logp(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, float temperature,
+                    float* logp, float* stats, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+int ebsp_token_logp_backward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, float temperature,
+                             const float* stats, const float* dlogp, void* dlogits, int64_t ldd, void* stream);
+
+/*
+ * Clipped policy loss with a KL term, token by token: with logp as above, old its
+ * value under the policy that drew the token, A the token's advantage and ref its
+ * value under a reference,
+ *
+ *     x = exp(logp - old)
+ *     loss = -min(x * A, min(max(x, 1 - clip_low), 1 + clip_high) * A)
+ *            + kl_weight * (exp(ref - logp) - (ref - logp) - 1)
+ *
+ * and its gradient over the logits: dL/dlogp is -x * A (0 where the clipped term is
+ * the smaller) - kl_weight * (exp(ref - logp) - 1).
+ *
+ *   old_logp, advantage  in  [N] float
+ *   ref_logp  in  [N] float, or NULL: no KL term
+ *   clip_low, clip_high  not negative; infinite: no border on that side
+ *   loss      out [N] float;  logp  out [N] float, or NULL
+ *   dloss     in  [N] float: dL/dloss of every row
+ * The others as above; a row without a token has loss 0, and its old_logp, advantage and
+ * ref_logp are not read.  ebsp_policy_forward gives the loss (its workspace:
+ * ebsp_token_logp_workspace_bytes), ebsp_policy_backward the gradient from its stats,
+ * ebsp_policy_loss_grad both in one pass where a step's dloss is known beforehand
+ * (workspace: ebsp_policy_workspace_bytes).  A masked token (logp -inf) has x = 0; with a
+ * KL term its loss is +inf and its row's gradient is not finite.
+ */
+size_t ebsp_policy_workspace_bytes(int64_t N, int64_t V, int32_t dtype);
+int ebsp_policy_forward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, float temperature,
+                        const float* old_logp, const float* advantage, const float* ref_logp, float clip_low, float clip_high, float kl_weight,
+                        float* loss, float* logp, float* stats, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+int ebsp_policy_backward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, float temperature,
+                         const float* old_logp, const float* advantage, const float* ref_logp, float clip_low, float clip_high, float kl_weight,
+                         const float* stats, const float* dloss, void* dlogits, int64_t ldd, void* stream);
+int ebsp_policy_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, float temperature,
+                          const float* old_logp, const float* advantage, const float* ref_logp, float clip_low, float clip_high, float kl_weight,
+                          const float* dloss, float* loss, float* logp, void* dlogits, int64_t ldd, int32_t* status,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Kinds of preference loss, of the margin h of a pair. */
+#define EBSP_PREFERENCE_SIGMOID 0  /* -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h) */
+#define EBSP_PREFERENCE_HINGE   1  /* max(0, 1 - beta h)                                                    */
+#define EBSP_PREFERENCE_SQUARE  2  /* (h - 1 / (2 beta))^2                                                  */
+
+/*
+ * Preference loss of pairs of answers.  The rows of all answers stand one behind the
+ * other, answer 2i the preferred of pair i, answer 2i + 1 the other; with the rows'
+ * logp as above (at temperature 1) and reference sums ref,
+ *
+ *     sum_a = the sum of logp over answer a's tokens (with `mean` divided by their number)
+ *     h_i = (sum_2i - ref_2i) - (sum_2i+1 - ref_2i+1)
+ *
+ * and the loss of pair i is a function of h_i, of the kind named.
+ *
+ *   tokens  in  [N] int64; negative: this row has none (a prompt), and is not read
+ *   starts  in  [2 pairs + 1] int64, on the device: answer a is rows starts[a] to
+ *               starts[a + 1] - 1 (none where they are equal).  Rows before the first
+ *               answer and behind the last are not read; their gradient is 0
+ *   ref     in  [2 pairs] float, or NULL: zeros
+ *   loss    out [pairs] float;  sums  out [2 pairs] float, or NULL
+ *   saved   out [N + pairs][3] float: what ebsp_preference_backward needs; or NULL
+ *   status  out [pairs] int32, or NULL: EBSP_STATUS_RANGE where a token of the pair is V
+ *               or more (it counts as none) or a start is beyond N or below the one before
+ *               (rows that do not exist are left out; the pair's results mean nothing)
+ *   dloss   in  [pairs] float: dL/dloss of every pair
+ *   workspace   ebsp_preference_workspace_bytes, 256-byte aligned; for ebsp_preference_forward
+ *               with `saved`, ebsp_token_logp_workspace_bytes are enough
+ * beta is positive; smoothing, 0 to 1, is of the sigmoid loss alone.  Sums over an
+ * answer and what follows of them are held in 64 bits, in an order that the sizes fix.
+ * ebsp_preference_loss_grad gives loss and gradient where dloss is known beforehand.
+ */
+size_t ebsp_preference_workspace_bytes(int64_t N, int64_t pairs, int64_t V, int32_t dtype);
+int ebsp_preference_forward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, const int64_t* starts,
+                            int64_t pairs, const float* ref, float beta, int32_t kind, float smoothing, int32_t mean, float* loss, float* sums,
+                            float* saved, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+int ebsp_preference_backward(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, const int64_t* starts,
+                             int64_t pairs, const float* saved, const float* dloss, void* dlogits, int64_t ldd, void* stream);
+int ebsp_preference_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int64_t* tokens, const int64_t* starts,
+                              int64_t pairs, const float* ref, float beta, int32_t kind, float smoothing, int32_t mean, const float* dloss, float* loss,
+                              float* sums, void* dlogits, int64_t ldd, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

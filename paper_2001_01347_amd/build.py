@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zipline.hip", "training.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zipline.hip", "training.hip", "tuning.hip")]
 LIB = os.path.join(HERE, "libebsp_zipline.so")
 
 HIPCC_FLAGS = [

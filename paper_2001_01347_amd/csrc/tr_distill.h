@@ -10,12 +10,11 @@
 // from the lowest finite value: logits of -inf then weigh nothing without a case of their own.
 #pragma once
 #include "ebsp_training.h"
-#include "tr_common.h"
+#include "tr_rows.h"
 
 namespace {
 
 constexpr int TOP_MAX = 1024;                    // most entries of a row: they lie in shared memory
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 
 struct Distill {
     const void* logits;
@@ -35,8 +34,6 @@ struct Distill {
     float temperature, kl, ce;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
 struct Sums {
     float m, st, s1;
 };
@@ -49,30 +46,6 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b, float ct)
     r.st = a.st * exp2_fast(da * ct) + b.st * exp2_fast(db * ct);
     r.s1 = a.s1 * exp2_fast(da * LOG2E) + b.s1 * exp2_fast(db * LOG2E);
     return r;
-}
-
-// Values that every thread of a workgroup has, over all of them, in an order that depends on nothing but NT.
-template <int NT, class T, class F>
-__device__ __forceinline__ T block_reduce(T v, T* shared, F&& join)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        T o;
-        const float* in = reinterpret_cast<const float*>(&v);
-        float* out = reinterpret_cast<float*>(&o);
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) / 4); ++i) out[i] = __shfl_xor(in[i], d);
-        v = join(v, o);
-    }
-    if constexpr (NT > WAVE) {
-        __syncthreads();                                                     // the last reduction's readers are through
-        if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = shared[0];
-#pragma unroll
-        for (int w = 1; w < NT / WAVE; ++w) v = join(v, shared[w]);
-    }
-    return v;
 }
 
 constexpr int SEEN_BITS = 15, TWICE_MAX = 32;
@@ -101,9 +74,6 @@ __device__ __forceinline__ float top_logit(const Distill& d, i64 at)
     return d.top_type == EBSP_F32 ? ((const float*)d.top_logit)[at]
          : d.top_type == EBSP_F16 ? to_float(((const _Float16*)d.top_logit)[at]) : to_float(((const __bf16*)d.top_logit)[at]);
 }
-
-// The larger of two, or the one that is no number: a NaN among a row's entries comes through, its results are not those of the others.
-__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
 
 // Entries and label of row n, checked: what does not lie in the vocabulary is left out and counted as bad.  The student's logits are
 // fetched for those from `v0` up to `v1`.  Each thread keeps to its own entries until the next barrier; `top` is the largest of them.
@@ -175,9 +145,6 @@ __device__ __forceinline__ Row read_row(const Distill& d, i64 n, i64 v0, i64 v1,
     __syncthreads();
     return row;
 }
-
-// log2 of a sum, for differences from m; of a row without any finite logit it is taken as 0, so its p are 0.
-__device__ __forceinline__ float log2_sum(float s) { return s == 0.f ? 0.f : log2f(s); }
 
 // The row's loss, from its statistics.  A logit's distance from the largest is not multiplied before its weight is: at a place masked with the lowest
 // value of bf16 or fp32 the loss is a number of that size, and log2(e) times it, or a sum of several, would be none.
@@ -307,39 +274,6 @@ __device__ __forceinline__ void write_places(const Distill& d, const Row& row, c
     }
 }
 
-template <class T>
-__device__ __forceinline__ Word4 lowest_word()
-{
-    Pack<T> w;
-#pragma unroll
-    for (int i = 0; i < PER_WORD4<T>; ++i) w.v[i] = (T)-INFINITY;
-    return w.raw;
-}
-
-// 16 bytes of a row from element v on; -inf behind its end.  The word that passes the end is read from where it fits and moved: element
-// by element its one lane would hold up the row.
-template <class T>
-__device__ __forceinline__ Word4 read_logits(const T* s, i64 v, i64 end)
-{
-    constexpr int N = PER_WORD4<T>;
-    if (v + N <= end) return load_loose(s + v);
-    Pack<T> w;
-    if (end >= N) {
-        w.raw = load_loose(s + end - N);
-        for (i64 moves = v + N - end; moves > 0; --moves) {
-#pragma unroll
-            for (int i = 0; i < N - 1; ++i) w.v[i] = w.v[i + 1];
-            w.v[N - 1] = (T)-INFINITY;
-        }
-    } else {
-        w.raw = lowest_word<T>();
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (v + i < end) w.v[i] = s[v + i];
-    }
-    return w.raw;
-}
-
 // The sums of a word's exponentials, from a maximum that stands.
 template <class T, Second S>
 __device__ __forceinline__ void add_exponentials(Sums& s, Word4 raw, float m, float ct)
@@ -355,16 +289,6 @@ __device__ __forceinline__ void add_exponentials(Sums& s, Word4 raw, float m, fl
     }
 }
 
-template <class T>
-__device__ __forceinline__ float largest(Word4 raw, float m)
-{
-    Pack<T> w;
-    w.raw = raw;
-#pragma unroll
-    for (int i = 0; i < PER_WORD4<T>; ++i) m = fmaxf(m, to_float(w.v[i]));
-    return m;
-}
-
 // A word more, whose values may pass the maximum so far.
 template <class T, Second S>
 __device__ __forceinline__ void add_word(Sums& s, Word4 raw, float ct)
@@ -376,21 +300,6 @@ __device__ __forceinline__ void add_word(Sums& s, Word4 raw, float ct)
         s.m = high;
     }
     add_exponentials<T, S>(s, raw, s.m, ct);
-}
-
-template <class T>
-__device__ __forceinline__ void write_gradient(T* g, i64 v, i64 end, Word4 raw)
-{
-    constexpr int N = PER_WORD4<T>;
-    if (v + N <= end) {
-        store_loose(g + v, raw);
-        return;
-    }
-    Pack<T> w;
-    w.raw = raw;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (v + i < end) g[v + i] = w.v[i];
 }
 
 template <int NT, class T, Second S>
@@ -432,14 +341,6 @@ __device__ __forceinline__ void write_loss(const Distill& d, i64 n, float loss, 
         d.stats[n * 3 + 1] = lt;
         d.stats[n * 3 + 2] = l1;
     }
-}
-
-// Packed words stay packed: without this the compiler keeps the floats of one use for the next, twice the registers.
-template <int N>
-__device__ __forceinline__ void forget_floats(Word4 (&w)[N])
-{
-#pragma unroll
-    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
 }
 
 // Loss and statistics, and with GRAD the gradient too: one workgroup a row.  The row's first NT x HELD words stay in registers from the one load to

@@ -1,0 +1,457 @@
+// Losses of the tokens that were taken: their log-probabilities, the clipped policy loss with a KL term, the preference loss of pairs.
+// Part of the ZipLine library (see tuning.hip); device code for gfx950.
+//
+// Per row, with logits s over a vocabulary, a token t and a temperature T:
+//     p = softmax(s / T)     logp = (s_t - m) / T - ln sum_j e^((s_j - m) / T)     d logp / d s_j = ([j = t] - p_j) / T
+// and every loss is a function of the rows' logp, so its gradient is a row's slope dL/dlogp times the last.  Policy, with old the log-probability
+// under the policy that drew t, A the advantage and ref that of a reference:
+//     x = e^(logp - old)     loss = -min(x A, clamp(x, 1 - low, 1 + high) A) + kl (e^(ref - logp) - (ref - logp) - 1)
+// Exponentials are taken to base 2.  Statistics are the row's largest logit m and log2 of the sum, apart, as in tr_distill.h; m starts from the lowest finite
+// value, so logits of -inf weigh nothing.  Rows without a token are not read.
+#pragma once
+#include "ebsp_training.h"
+#include "tr_rows.h"
+
+namespace {
+
+enum TokenLoss { TOKEN_LOGP, TOKEN_POLICY, TOKEN_PREFERENCE };
+
+struct Tokens {
+    const void* logits;
+    i64 ld, N, V;
+    const i64* tokens;
+    float temperature;
+    int kind;
+    const float *old_logp, *advantage, *ref_logp;            // policy
+    float low, high, kl;
+    const i64* starts;                                       // preference: [2 pairs + 1]
+    i64 pairs;
+    const float* outer;                                      // dL/dlogp or dL/dloss of every row, dL/dloss of every pair
+    float *loss, *logp;
+    float* stats;                                            // [N][3]: m, log2 of the sum, logp; behind them, for a preference loss, [pairs][3]
+    int* status;
+    void* grad;
+    i64 ldd;
+    float* partial;                                          // [N][splits][2]: m and the sum of a part of a row
+    int splits;
+};
+
+struct Sum {
+    float m, s;
+};
+
+__device__ __forceinline__ Sum joined(Sum a, Sum b, float ct)
+{
+    Sum r;
+    r.m = fmaxf(a.m, b.m);
+    r.s = a.s * exp2_fast((a.m - r.m) * ct) + b.s * exp2_fast((b.m - r.m) * ct);
+    return r;
+}
+
+// The sum of a word's exponentials, from a maximum that stands.
+template <class T>
+__device__ __forceinline__ void add_exponentials(Sum& s, Word4 raw, float ct)
+{
+    Pack<T> w;
+    w.raw = raw;
+#pragma unroll
+    for (int i = 0; i < PER_WORD4<T>; ++i) s.s += exp2_fast((to_float(w.v[i]) - s.m) * ct);
+}
+
+template <class T>
+__device__ __forceinline__ void add_word(Sum& s, Word4 raw, float ct)
+{
+    const float high = largest<T>(raw, s.m);
+    if (high > s.m) {
+        s.s *= exp2_fast((s.m - high) * ct);
+        s.m = high;
+    }
+    add_exponentials<T>(s, raw, ct);
+}
+
+template <int NT, class T>
+__device__ __forceinline__ Sum part_sum(const T* s, i64 v0, i64 v1, float ct)
+{
+    constexpr int N = PER_WORD4<T>, AHEAD = 4;
+    Sum sum = {-FLT_MAX, 0.f};
+    i64 v = v0 + (i64)threadIdx.x * N;
+    for (; v + (AHEAD - 1) * NT * N + N <= v1; v += AHEAD * NT * N) {
+        Word4 w[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) w[j] = load_loose(s + v + j * NT * N);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) add_word<T>(sum, w[j], ct);
+    }
+    for (; v < v1; v += NT * N) add_word<T>(sum, read_logits(s, v, v1), ct);
+    return sum;
+}
+
+// The row's token, -1 for none: negative, beyond the vocabulary, or a row outside all answers.
+__device__ __forceinline__ int token_of(const Tokens& d, i64 n, bool& bad)
+{
+    const i64 t = d.tokens[n];
+    i64 first = 0, behind = d.N;
+    if (d.kind == TOKEN_PREFERENCE) {                                        // (with a return in here the compiler has lost the token)
+        first = d.starts[0];
+        behind = d.starts[2 * d.pairs];
+    }
+    bad = t >= d.V;
+    return ((t < 0) | bad | (n < first) | (n >= behind)) ? -1 : (int)t;
+}
+
+// e^g - g - 1, to its own precision where g is small: there by its series.
+__device__ __forceinline__ float exp_above_tangent(float g)
+{
+    if (fabsf(g) > 0.25f) {
+        const float e = expm1f(g);
+        return e == INFINITY ? e : e - g;
+    }
+    float t = 1.f / 40320.f;
+    t = fmaf(t, g, 1.f / 5040.f);
+    t = fmaf(t, g, 1.f / 720.f);
+    t = fmaf(t, g, 1.f / 120.f);
+    t = fmaf(t, g, 1.f / 24.f);
+    t = fmaf(t, g, 1.f / 6.f);
+    return fmaf(t, g, 0.5f) * g * g;
+}
+
+// The policy loss of a row, and its slope over logp.  (NaN comes through: comparisons are made so that it takes the slope with the ratio in it.)
+__device__ __forceinline__ float policy_of(const Tokens& d, i64 n, float logp, float& loss)
+{
+    const float a = d.advantage[n], x = expf(logp - d.old_logp[n]);
+    const float border = a < 0.f ? 1.f - d.low : 1.f + d.high;
+    const bool held = a < 0.f ? x < border : x > border;
+    loss = -a * (held ? border : x);
+    float slope = held ? a - a : -a * x;
+    if (d.ref_logp && d.kl != 0.f) {
+        const float g = d.ref_logp[n] - logp;
+        loss = fmaf(d.kl, exp_above_tangent(g), loss);
+        slope = fmaf(-d.kl, expm1f(g), slope);
+    }
+    return slope;
+}
+
+__device__ __forceinline__ float logp_of(float token_logit, float m, float l, float temperature)
+{
+    return (token_logit - m) / temperature - LN2 * l;
+}
+
+// What a row with a token leaves behind; one thread writes.
+__device__ __forceinline__ void write_row(const Tokens& d, i64 n, float m, float l, float logp, float loss)
+{
+    if (d.logp) d.logp[n] = logp;
+    if (d.loss) d.loss[n] = loss;
+    if (d.stats) {
+        d.stats[n * 3] = m;
+        d.stats[n * 3 + 1] = l;
+        d.stats[n * 3 + 2] = logp;
+    }
+}
+
+// The answer that row n is part of: how many starts are not behind it, less one.  64 starts are looked at together; all lanes of a wave take part.
+__device__ __forceinline__ i64 answer_of(const Tokens& d, i64 n)
+{
+    i64 lo = 0, hi = 2 * d.pairs;                                            // starts[lo] <= n < starts[hi]
+    const int lane = threadIdx.x & 63;
+    while (hi - lo > 1) {
+        const i64 step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step;
+        const u32 before = (u32)__popcll(__ballot(at < hi && d.starts[at] <= n));
+        lo += before * step;
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    return lo;
+}
+
+// dL/dlogp of row n, whole: times what stands outside the loss.
+__device__ __forceinline__ float slope_of(const Tokens& d, i64 n, float logp)
+{
+    float loss;
+    if (d.kind == TOKEN_LOGP) return d.outer[n];
+    if (d.kind == TOKEN_POLICY) return policy_of(d, n, logp, loss) * d.outer[n];
+    const i64 answer = answer_of(d, n);
+    return d.stats[(d.N + answer / 2) * 3 + (answer & 1)] * d.outer[answer / 2];
+}
+
+// A row's gradient: c ([j = token] - p_j).
+struct TokenSlope {
+    float m, ct, l, c;
+};
+
+template <class T>
+__device__ __forceinline__ Word4 gradient_word(const TokenSlope& g, Word4 raw)
+{
+    Pack<T> w;
+    w.raw = raw;
+#pragma unroll
+    for (int i = 0; i < PER_WORD4<T>; ++i) w.v[i] = from_float<T>(-g.c * exp2_fast((to_float(w.v[i]) - g.m) * g.ct - g.l));
+    return w.raw;
+}
+
+template <class T>
+__device__ __forceinline__ T token_gradient(const TokenSlope& g, float s)
+{
+    return from_float<T>(fmaf(-g.c, exp2_fast((s - g.m) * g.ct - g.l), g.c));
+}
+
+template <int NT, class T>
+__device__ __forceinline__ void write_zeros(T* out, i64 v0, i64 v1)
+{
+    for (i64 v = v0 + (i64)threadIdx.x * PER_WORD4<T>; v < v1; v += NT * PER_WORD4<T>) write_gradient(out, v, v1, Word4{0, 0, 0, 0});
+}
+
+// Loss and statistics, and with GRAD the gradient too: one workgroup a row, whose first words stay in registers and, with GRAD, shared memory from the
+// one load on, as in tr_distill.h.
+template <int NT, class T, bool GRAD>
+__global__ void __launch_bounds__(NT) tr_token_row_kernel(Tokens d)
+{
+    constexpr int N = PER_WORD4<T>, HELD = 16, KEPT = !GRAD ? 0 : NT == 512 ? 7 : NT == 1024 ? 8 : 0;
+    constexpr u32 STEP = NT * N, BEHIND = (HELD + KEPT) * STEP;
+    __shared__ float scalar[16];
+    __shared__ Word4 kept[KEPT > 0 ? KEPT * NT : 1];
+    const i64 n = blockIdx.x;
+    const T* s = (const T*)d.logits + n * d.ld;
+    bool bad;
+    const int token = token_of(d, n, bad);
+    if (threadIdx.x == 0 && d.status) d.status[n] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    if (token < 0) {
+        if (threadIdx.x == 0) write_row(d, n, 0.f, 0.f, 0.f, 0.f);
+        if constexpr (GRAD) write_zeros<NT, T>((T*)d.grad + n * d.ldd, 0, d.V);
+        return;
+    }
+    const float token_logit = to_float(s[token]), ct = LOG2E / d.temperature;
+    Sum rest = {-FLT_MAX, 0.f};
+    if (BEHIND < d.V) rest = part_sum<NT, T>(s, BEHIND, d.V, ct);
+    float m = rest.m;
+    if constexpr (KEPT > 0) {
+        if (HELD * STEP < d.V) {
+            Word4 w[KEPT];
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j) {
+                const u32 v = threadIdx.x * N + (HELD + j) * STEP;
+                w[j] = v < d.V ? read_logits(s, v, d.V) : lowest_word<T>();
+            }
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j) {
+                kept[j * NT + threadIdx.x] = w[j];
+                m = largest<T>(w[j], m);
+            }
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);                                       // (before the registers fill)
+    // A word belongs to the row as a whole, or is the part that is left, which one thread has besides.
+    const u32 v0 = threadIdx.x * N, whole = (u32)(d.V / N * N), end = min(whole, HELD * STEP);
+    const bool has_last = whole < (u32)d.V && whole < HELD * STEP && whole % STEP == v0;
+    Word4 held[HELD];
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) held[j] = v0 + j * STEP < end ? load_loose(s + j * STEP + v0) : lowest_word<T>();
+    Word4 last = lowest_word<T>();
+    if (has_last) last = read_logits(s, whole, d.V);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (j * STEP < end) {
+            m = largest<T>(held[j], m);
+            __builtin_amdgcn_sched_barrier(0);                               // word by word: the registers are full
+        }
+    if (has_last) m = largest<T>(last, m);
+    forget_floats(held);
+    m = block_reduce<NT>(m, scalar, [](float a, float b) { return fmaxf(a, b); });
+    Sum sum = joined(rest, Sum{m, 0.f}, ct);                                 // (m is the larger)
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (j * STEP < end) {
+            add_exponentials<T>(sum, held[j], ct);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    if (has_last) add_exponentials<T>(sum, last, ct);
+    if constexpr (KEPT > 0)
+#pragma unroll 1
+        for (int j = 0; j < KEPT && (HELD + j) * STEP < d.V; ++j) add_exponentials<T>(sum, kept[j * NT + threadIdx.x], ct);
+    const float l = log2_sum(block_reduce<NT>(sum.s, scalar, [](float a, float b) { return a + b; }));
+    const float logp = logp_of(token_logit, m, l, d.temperature);
+    float loss = 0.f, slope = 0.f;
+    if (d.kind == TOKEN_POLICY) slope = policy_of(d, n, logp, loss);
+    if (threadIdx.x == 0) write_row(d, n, m, l, logp, loss);
+    if constexpr (GRAD) {
+        const TokenSlope g = {m, ct, l, slope * d.outer[n] / d.temperature};
+        T* out = (T*)d.grad + n * d.ldd;
+        if (g.c == 0.f) {
+            write_zeros<NT, T>(out, 0, d.V);
+            return;
+        }
+        forget_floats(held);
+        __builtin_amdgcn_s_waitcnt(0);                                       // in place: every thread has the token's logit
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            if (v0 + j * STEP < end) store_loose(out + j * STEP + v0, gradient_word<T>(g, held[j]));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (has_last) write_gradient(out, whole, d.V, gradient_word<T>(g, last));
+        if constexpr (KEPT > 0)
+#pragma unroll 1
+            for (int j = 0; j < KEPT; ++j) {
+                const u32 v = v0 + (HELD + j) * STEP;
+                if (v < d.V) write_gradient(out, v, d.V, gradient_word<T>(g, kept[j * NT + threadIdx.x]));
+            }
+        for (i64 v = v0 + BEHIND; v < d.V; v += STEP) write_gradient(out, v, d.V, gradient_word<T>(g, read_logits(s, v, d.V)));
+        __builtin_amdgcn_s_waitcnt(0);                                       // stores to one address arrive in this order
+        __syncthreads();
+        if (threadIdx.x == 0) out[token] = token_gradient<T>(g, token_logit);
+    }
+}
+
+__device__ __forceinline__ void part_range(const Tokens& d, int part, int per_word, i64& v0, i64& v1)
+{
+    const i64 words = (d.V + per_word - 1) / per_word, each = (words + d.splits - 1) / d.splits;
+    v0 = min(part * each * per_word, d.V);
+    v1 = min(v0 + each * per_word, d.V);
+}
+
+// Few rows: the sum of a part of a row by each workgroup ...
+template <int NT, class T>
+__global__ void __launch_bounds__(NT) tr_token_part_kernel(Tokens d)
+{
+    __shared__ Sum shared[16];
+    const i64 n = blockIdx.x / d.splits;
+    const float ct = LOG2E / d.temperature;
+    bool bad;
+    if (token_of(d, n, bad) < 0) return;
+    i64 v0, v1;
+    part_range(d, blockIdx.x % d.splits, PER_WORD4<T>, v0, v1);
+    Sum sum = part_sum<NT, T>((const T*)d.logits + n * d.ld, v0, v1, ct);
+    sum = block_reduce<NT>(sum, shared, [ct](Sum x, Sum y) { return joined(x, y, ct); });
+    if (threadIdx.x == 0) {
+        float* out = d.partial + (i64)blockIdx.x * 2;
+        out[0] = sum.m;
+        out[1] = sum.s;
+    }
+}
+
+// ... joined by one wave a row, in the order of the parts.
+template <class T>
+__global__ void __launch_bounds__(64) tr_token_join_kernel(Tokens d)
+{
+    const i64 n = blockIdx.x;
+    bool bad;
+    const int token = token_of(d, n, bad);
+    if (threadIdx.x == 0 && d.status) d.status[n] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    if (token < 0) {
+        if (threadIdx.x == 0) write_row(d, n, 0.f, 0.f, 0.f, 0.f);
+        return;
+    }
+    const float token_logit = to_float(((const T*)d.logits)[n * d.ld + token]), ct = LOG2E / d.temperature;
+    Sum sum = {-FLT_MAX, 0.f};
+    for (int p = threadIdx.x; p < d.splits; p += 64) {
+        const float* in = d.partial + (n * d.splits + p) * 2;
+        sum = joined(sum, Sum{in[0], in[1]}, ct);
+    }
+    sum = block_reduce<64>(sum, (Sum*)nullptr, [ct](Sum x, Sum y) { return joined(x, y, ct); });
+    const float l = log2_sum(sum.s), logp = logp_of(token_logit, sum.m, l, d.temperature);
+    float loss = 0.f;
+    if (d.kind == TOKEN_POLICY) policy_of(d, n, logp, loss);
+    if (threadIdx.x == 0) write_row(d, n, sum.m, l, logp, loss);
+}
+
+// The gradient from statistics: every row in `splits` parts.  Nothing is read of a row but the workgroup's own part, which it may overwrite.
+template <int NT, class T>
+__global__ void __launch_bounds__(NT) tr_token_gradient_kernel(Tokens d)
+{
+    constexpr int N = PER_WORD4<T>;
+    const i64 n = blockIdx.x / d.splits;
+    i64 v0, v1;
+    part_range(d, blockIdx.x % d.splits, N, v0, v1);
+    const T* s = (const T*)d.logits + n * d.ld;
+    T* out = (T*)d.grad + n * d.ldd;
+    bool bad;
+    const int token = token_of(d, n, bad);
+    const TokenSlope g = {d.stats[n * 3], LOG2E / d.temperature, d.stats[n * 3 + 1], token < 0 ? 0.f : slope_of(d, n, d.stats[n * 3 + 2]) / d.temperature};
+    if (g.c == 0.f) {
+        write_zeros<NT, T>(out, v0, v1);
+        return;
+    }
+    const bool mine = token >= v0 && token < v1 && (token - v0) / N % NT == threadIdx.x;
+    const float token_logit = mine ? to_float(s[token]) : 0.f;
+    for (i64 v = v0 + (i64)threadIdx.x * N; v < v1; v += NT * N) write_gradient(out, v, v1, gradient_word<T>(g, read_logits(s, v, v1)));
+    if (mine) out[token] = token_gradient<T>(g, token_logit);                // behind this thread's own store of that word
+}
+
+// The losses of pairs: one workgroup a pair, whose rows' logp stand in the statistics.  Sums over an answer and what follows are in 64 bits.
+struct Preference {
+    Tokens d;
+    const float* ref;                            // [2 pairs], or NULL
+    float beta, smoothing;
+    int loss_kind, mean;
+    float *loss, *sums;
+    int* status;
+};
+
+template <int NT>
+__global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
+{
+    __shared__ double shared[2][NT / WAVE][3];
+    const i64 pair = blockIdx.x;
+    double sum[2], share[2];
+    bool bad = false;
+    for (int side = 0; side < 2; ++side) {
+        const i64* at = a.d.starts + 2 * pair + side;
+        const i64 from = at[0] < 0 ? 0 : at[0] < a.d.N ? at[0] : a.d.N, to = at[1] < from ? from : at[1] < a.d.N ? at[1] : a.d.N;
+        bad |= from != at[0] || to != at[1];
+        double f[3] = {0., 0., 0.};                                          // the sum, tokens, tokens beyond the vocabulary
+        for (i64 n = from + threadIdx.x; n < to; n += NT) {
+            bool beyond;
+            if (token_of(a.d, n, beyond) >= 0) {
+                f[0] += a.d.stats[n * 3 + 2];
+                f[1] += 1.;
+            }
+            if (beyond) f[2] += 1.;
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+#pragma unroll
+            for (int x = 32; x > 0; x >>= 1) f[i] += __shfl_xor(f[i], x);
+            if (threadIdx.x % WAVE == 0) shared[side][threadIdx.x / WAVE][i] = f[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            f[i] = shared[side][0][i];
+#pragma unroll
+            for (int w = 1; w < NT / WAVE; ++w) f[i] += shared[side][w][i];
+        }
+        bad |= f[2] > 0.;
+        share[side] = a.mean && f[1] > 0. ? 1. / f[1] : 1.;
+        sum[side] = f[0] * share[side];
+    }
+    if (threadIdx.x) return;
+    const double beta = a.beta, e = a.smoothing;
+    const double h = a.ref ? (sum[0] - a.ref[2 * pair]) - (sum[1] - a.ref[2 * pair + 1]) : sum[0] - sum[1];
+    double loss, slope;
+    if (a.loss_kind == EBSP_PREFERENCE_HINGE) {
+        loss = beta * h < 1. ? 1. - beta * h : beta * h == beta * h ? 0. : h;
+        slope = beta * h >= 1. ? 0. : beta * h == beta * h ? -beta : h;
+    } else if (a.loss_kind == EBSP_PREFERENCE_SQUARE) {
+        const double gap = h - 0.5 / beta;
+        loss = gap * gap;
+        slope = 2. * gap;
+    } else {
+        const double z = beta * h, low = exp(-fabs(z));                      // sigmoid(z) is 1 / (1 + low), or low times that
+        loss = (z < 0. ? -z : z == z ? 0. : z) + log1p(low);
+        slope = -beta * (z < 0. ? 1. : low) / (1. + low);
+        if (e != 0.) {
+            loss += e * z;
+            slope += e * beta;
+        }
+    }
+    if (a.loss) a.loss[pair] = (float)loss;
+    if (a.sums) {
+        a.sums[2 * pair] = (float)sum[0];
+        a.sums[2 * pair + 1] = (float)sum[1];
+    }
+    if (a.status) a.status[pair] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    float* out = a.d.stats + (a.d.N + pair) * 3;
+    out[0] = (float)(slope * share[0]);
+    out[1] = (float)(-slope * share[1]);
+    out[2] = 0.f;
+}
+
+}  // namespace

@@ -13,7 +13,7 @@
 #include <stdio.h>
 
 #include "ebsp_training.h"
-#include "zl_host.h"
+#include "tr_host.h"
 #include "tr_cut.h"
 #include "tr_gated_ff.h"
 #include "tr_distill.h"
@@ -21,28 +21,8 @@
 
 namespace {
 
-using namespace ebsp_host;
-
-#define LAUNCH(kernel, grid, block, ...) LAUNCH_LDS(kernel, grid, block, 0, __VA_ARGS__)
-#define LAUNCH_LDS(kernel, grid, block, lds, ...)                                          \
-    do {                                                                                   \
-        hipLaunchKernelGGL(kernel, grid, block, lds, st, __VA_ARGS__);                       \
-        hipError_t e_ = hipGetLastError();                                                 \
-        if (e_ != hipSuccess) {                                                            \
-            snprintf(g_err, sizeof g_err, "%s: %s", #kernel, hipGetErrorString(e_));       \
-            return EBSP_ERR_LAUNCH;                                                        \
-        }                                                                                  \
-    } while (0)
-
-// Sizes up to here keep every product of two of them, in elements, inside 64 bits.
-constexpr i64 SIZE_MAX_DIM = 1ll << 31;
-
 // Results of so many elements are refused: their bytes, several buffers of them together, stay inside 64 bits.
 constexpr i64 ELEMENTS_MAX = 1ll << 56;
-
-int element_size(int dtype) { return dtype == EBSP_BF16 || dtype == EBSP_F16 ? 2 : dtype == EBSP_F32 ? 4 : 0; }
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 i64 padded_units(i64 F, int size)
 {
@@ -59,11 +39,6 @@ int check_sizes(i64 M, i64 K, i64 F, int dtype, int act)
     if (M * F >= ELEMENTS_MAX) return fail(EBSP_ERR_SHAPE, "invalid shape: M x F must be below 2^56");
     return EBSP_OK;
 }
-
-bool stride_ok(i64 ld, i64 length) { return ld >= length && ld < (1ll << 40); }
-
-// A launch of so many workgroups: the runtime counts a grid's threads in 32 bits.
-bool launchable(i64 blocks, int threads) { return blocks * threads <= 0xffffffffll; }
 
 template <class TL, int PER_N>
 int tile_grid(i64 m, i64 n, dim3& grid, int z = 1)
