@@ -6,13 +6,28 @@
 // and every loss is a function of the rows' logp, so its gradient is a row's slope dL/dlogp times the last.  Policy, with old the log-probability
 // under the policy that drew t, A the advantage and ref that of a reference:
 //     x = e^(logp - old)     loss = -min(x A, clamp(x, 1 - low, 1 + high) A) + kl (e^(ref - logp) - (ref - logp) - 1)
-// Exponentials are taken to base 2.  Statistics are the row's largest logit m and log2 of the sum, apart, as in tr_distill.h; m starts from the lowest finite
-// value, so logits of -inf weigh nothing.  Rows without a token are not read.
+// Exponentials are taken to base 2, of x_j = s_j c - k with c = log2(e) / T and k = m c, m the row's largest logit: one fused product and sum.  k is rounded, but it
+// is the same in the sum, in logp and in the gradient, so what it is off by falls out.  Rows whose k is no ordinary number (of the type's lowest values, say, or +-1e30 and
+// more) take x_j = (s_j - m) c, slower and as good.  Statistics are m and log2 of the sum, apart; m starts from the lowest finite value, so logits of -inf
+// weigh nothing.  Rows without a token are not read.
 #pragma once
 #include "ebsp_training.h"
 #include "tr_rows.h"
 
 namespace {
+
+// Gradients pass the caches by, and so do logits on their last read, for there is no other soon.  policy_step_4096 417 us with neither, 395 with the stores, 376 with both;
+// logp_train_1024 89, 80 and 72.  Not logits whose words cross lines: those are read twice, by neighbours (policy_separate_odd 62 and, passing by, 70).
+template <class T>
+__device__ __forceinline__ void store_stream(T* p, Word4 v)
+{
+    __builtin_nontemporal_store(v, reinterpret_cast<LooseWord4*>(p));
+}
+template <bool STREAM, class T>
+__device__ __forceinline__ Word4 load_last(const T* p)
+{
+    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const LooseWord4*>(p)) : load_loose(p);
+}
 
 enum TokenLoss { TOKEN_LOGP, TOKEN_POLICY, TOKEN_PREFERENCE };
 
@@ -34,55 +49,95 @@ struct Tokens {
     i64 ldd;
     float* partial;                                          // [N][splits][2]: m and the sum of a part of a row
     int splits;
+    int backwards;                                           // a gradient takes the last row first
 };
 
 struct Sum {
     float m, s;
 };
 
+constexpr float FAR = 1e30f;
+
+// Whether a row whose largest logit is m takes the differences first (also where m is no number), and k of the others, nowhere infinite.
+__device__ __forceinline__ bool is_far(float m, float ct) { return !(fabsf(m) * ct < FAR); }
+__device__ __forceinline__ float reference(float m, float ct) { return fmaxf(m * ct, -FAR); }
+
+__device__ __forceinline__ float apart(float a, float b, float ct) { return is_far(a, ct) || is_far(b, ct) ? (a - b) * ct : reference(a, ct) - reference(b, ct); }
+
 __device__ __forceinline__ Sum joined(Sum a, Sum b, float ct)
 {
     Sum r;
     r.m = fmaxf(a.m, b.m);
-    r.s = a.s * exp2_fast((a.m - r.m) * ct) + b.s * exp2_fast((b.m - r.m) * ct);
+    r.s = a.s * exp2_fast(apart(a.m, r.m, ct)) + b.s * exp2_fast(apart(b.m, r.m, ct));
     return r;
 }
 
-// The sum of a word's exponentials, from a maximum that stands.
-template <class T>
-__device__ __forceinline__ void add_exponentials(Sum& s, Word4 raw, float ct)
+// The sum of a word's exponentials, from k or, of a far row, m.
+template <class T, bool FROM_M>
+__device__ __forceinline__ void add_exponentials(float& sum, Word4 raw, float from, float ct)
 {
     Pack<T> w;
     w.raw = raw;
 #pragma unroll
-    for (int i = 0; i < PER_WORD4<T>; ++i) s.s += exp2_fast((to_float(w.v[i]) - s.m) * ct);
+    for (int i = 0; i < PER_WORD4<T>; ++i) sum += exp2_fast(FROM_M ? (to_float(w.v[i]) - from) * ct : fmaf(to_float(w.v[i]), ct, -from));
 }
 
-template <class T>
-__device__ __forceinline__ void add_word(Sum& s, Word4 raw, float ct)
-{
-    const float high = largest<T>(raw, s.m);
-    if (high > s.m) {
-        s.s *= exp2_fast((s.m - high) * ct);
-        s.m = high;
-    }
-    add_exponentials<T>(s, raw, ct);
-}
-
+// A row's words: those that are whole, and what is left behind them, which the thread whose turn it would be takes by itself.
 template <int NT, class T>
-__device__ __forceinline__ Sum part_sum(const T* s, i64 v0, i64 v1, float ct)
-{
-    constexpr int N = PER_WORD4<T>, AHEAD = 4;
-    Sum sum = {-FLT_MAX, 0.f};
-    i64 v = v0 + (i64)threadIdx.x * N;
-    for (; v + (AHEAD - 1) * NT * N + N <= v1; v += AHEAD * NT * N) {
-        Word4 w[AHEAD];
+struct Words {
+    static constexpr u32 N = PER_WORD4<T>;
+    u32 first, whole, end;                                   // from `first`, a multiple of N
+    __device__ __forceinline__ Words(i64 v0, i64 v1) : first((u32)v0), whole((u32)(v1 / N * N)), end((u32)v1) {}
+    __device__ __forceinline__ bool rest() const { return whole >= first && whole < end && (whole - first) / N % NT == threadIdx.x; }
+
+    // AHEAD words, NT apart, from v on; -inf for those that are not there.  Each is loaded from somewhere: no load waits for another, as it would in a branch.
+    template <bool STREAM, int AHEAD>
+    __device__ __forceinline__ void load(Word4 (&w)[AHEAD], const T* s, u32 v) const
+    {
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) w[j] = load_loose(s + v + j * NT * N);
+        for (int j = 0; j < AHEAD; ++j) w[j] = load_last<STREAM>(s + (v + j * NT * N < whole ? v + j * NT * N : first));
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) add_word<T>(sum, w[j], ct);
+        for (int j = 0; j < AHEAD; ++j)
+            if (v + j * NT * N >= whole) w[j] = lowest_word<T>();
     }
-    for (; v < v1; v += NT * N) add_word<T>(sum, read_logits(s, v, v1), ct);
+};
+
+// The sum over a part of a row, in one pass: AHEAD words at a time with the next ones under way, the sum so far times 2^(k - k') where they have a larger one.
+template <int NT, class T>
+__device__ __forceinline__ Sum part_sum(const T* s, const Words<NT, T> at, float ct)
+{
+    constexpr u32 N = PER_WORD4<T>, AHEAD = 4, TURN = AHEAD * NT * N;
+    Sum sum = {-FLT_MAX, 0.f};
+    float k = -FAR;
+    Word4 w[AHEAD], next[AHEAD], rest[1];
+    const bool has_rest = at.rest();
+    if (has_rest) rest[0] = read_logits(s, at.whole, at.end);
+    if (at.first < at.whole) {
+        at.template load<false>(w, s, at.first + threadIdx.x * N);
+        for (u32 base = at.first; base < at.whole; base += TURN) {
+            if (base + TURN < at.whole) at.template load<false>(next, s, base + TURN + threadIdx.x * N);
+#pragma unroll
+            for (u32 j = 0; j < AHEAD; ++j) sum.m = largest<T>(w[j], sum.m);
+            const float high = reference(sum.m, ct);
+            sum.s *= exp2_fast(k - high);
+            k = high;
+#pragma unroll
+            for (u32 j = 0; j < AHEAD; ++j) add_exponentials<T, false>(sum.s, w[j], k, ct);
+#pragma unroll
+            for (u32 j = 0; j < AHEAD; ++j) w[j] = next[j];
+        }
+    }
+    if (has_rest) {
+        sum.m = largest<T>(rest[0], sum.m);
+        const float high = reference(sum.m, ct);
+        sum.s *= exp2_fast(k - high);
+        add_exponentials<T, false>(sum.s, rest[0], high, ct);
+    }
+    if (is_far(sum.m, ct)) {                                                 // (sum.m is this thread's own: so is its sum)
+        sum.s = 0.f;
+        for (u32 v = at.first + threadIdx.x * N; v < at.whole; v += NT * N) add_exponentials<T, true>(sum.s, load_loose(s + v), sum.m, ct);
+        if (has_rest) add_exponentials<T, true>(sum.s, rest[0], sum.m, ct);
+    }
     return sum;
 }
 
@@ -133,7 +188,9 @@ __device__ __forceinline__ float policy_of(const Tokens& d, i64 n, float logp, f
 
 __device__ __forceinline__ float logp_of(float token_logit, float m, float l, float temperature)
 {
-    return (token_logit - m) / temperature - LN2 * l;
+    const float ct = LOG2E / temperature;
+    if (is_far(m, ct)) return (token_logit - m) / temperature - LN2 * l;
+    return LN2 * (fmaf(token_logit, ct, -reference(m, ct)) - l);
 }
 
 // What a row with a token leaves behind; one thread writes.
@@ -172,25 +229,45 @@ __device__ __forceinline__ float slope_of(const Tokens& d, i64 n, float logp)
     return d.stats[(d.N + answer / 2) * 3 + (answer & 1)] * d.outer[answer / 2];
 }
 
-// A row's gradient: c ([j = token] - p_j).
+// A row's gradient: c ([j = token] - p_j), with p_j = 2^(x_j) 2^-l.
 struct TokenSlope {
-    float m, ct, l, c;
+    float ct, from, c, scale;                                // from: k, or m of a far row; scale: -c 2^-l
+    bool far;
 };
 
-template <class T>
+__device__ __forceinline__ TokenSlope token_slope(float m, float l, float temperature, float slope)
+{
+    const float ct = LOG2E / temperature, c = slope / temperature;
+    const bool far = is_far(m, ct);
+    return TokenSlope{ct, far ? m : reference(m, ct), c, -c * exp2_fast(-l), far};
+}
+
+template <class T, bool FROM_M>
 __device__ __forceinline__ Word4 gradient_word(const TokenSlope& g, Word4 raw)
 {
     Pack<T> w;
     w.raw = raw;
 #pragma unroll
-    for (int i = 0; i < PER_WORD4<T>; ++i) w.v[i] = from_float<T>(-g.c * exp2_fast((to_float(w.v[i]) - g.m) * g.ct - g.l));
+    for (int i = 0; i < PER_WORD4<T>; ++i) {
+        const float s = to_float(w.v[i]);
+        w.v[i] = from_float<T>(g.scale * exp2_fast(FROM_M ? (s - g.from) * g.ct : fmaf(s, g.ct, -g.from)));
+    }
     return w.raw;
 }
 
 template <class T>
 __device__ __forceinline__ T token_gradient(const TokenSlope& g, float s)
 {
-    return from_float<T>(fmaf(-g.c, exp2_fast((s - g.m) * g.ct - g.l), g.c));
+    return from_float<T>(fmaf(g.scale, exp2_fast(g.far ? (s - g.from) * g.ct : fmaf(s, g.ct, -g.from)), g.c));
+}
+
+// The body of a loop over a row's words for either kind of row.
+template <bool VALUE> struct FromM { static constexpr bool value = VALUE; };
+template <class F>
+__device__ __forceinline__ void with_far(bool far, F&& f)
+{
+    if (far) f(FromM<true>());
+    else f(FromM<false>());
 }
 
 template <int NT, class T>
@@ -199,12 +276,51 @@ __device__ __forceinline__ void write_zeros(T* out, i64 v0, i64 v1)
     for (i64 v = v0 + (i64)threadIdx.x * PER_WORD4<T>; v < v1; v += NT * PER_WORD4<T>) write_gradient(out, v, v1, Word4{0, 0, 0, 0});
 }
 
-// Loss and statistics, and with GRAD the gradient too: one workgroup a row, whose first words stay in registers and, with GRAD, shared memory from the
-// one load on, as in tr_distill.h.
-template <int NT, class T, bool GRAD>
-__global__ void __launch_bounds__(NT) tr_token_row_kernel(Tokens d)
+// A row without a token: nothing of it is read.
+template <int NT, class T>
+__device__ __forceinline__ bool leave_row(const Tokens& d, i64 n, int token, bool bad, bool grad)
 {
-    constexpr int N = PER_WORD4<T>, HELD = 16, KEPT = !GRAD ? 0 : NT == 512 ? 7 : NT == 1024 ? 8 : 0;
+    if (threadIdx.x == 0 && d.status) d.status[n] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    if (token >= 0) return false;
+    if (threadIdx.x == 0) write_row(d, n, 0.f, 0.f, 0.f, 0.f);
+    if (grad) write_zeros<NT, T>((T*)d.grad + n * d.ldd, 0, d.V);
+    return true;
+}
+
+// The row's results from its statistics; its slope.
+__device__ __forceinline__ float finish_row(const Tokens& d, i64 n, float token_logit, float m, float l)
+{
+    const float logp = logp_of(token_logit, m, l, d.temperature);
+    float loss = 0.f, slope = 0.f;
+    if (d.kind == TOKEN_POLICY) slope = policy_of(d, n, logp, loss);
+    if (threadIdx.x == 0) write_row(d, n, m, l, logp, loss);
+    return slope;
+}
+
+// Loss and statistics alone: one workgroup a row, which is read once and kept nowhere.  Memory bounds it: 4096 rows of 128000 in bf16 183 us, 5.7 TB/s, 1024 of 64000 31 (of it
+// some 9 to start and to end); with 512 threads 180 and 31, with 1024 183 and 37, two words ahead where there are four 184 and 29, 400 rows of 128000 then 36 where they take 27.
+template <int NT, class T>
+__global__ void __launch_bounds__(NT) tr_token_value_kernel(Tokens d)
+{
+    __shared__ Sum shared[16];
+    const i64 n = blockIdx.x;
+    const T* s = (const T*)d.logits + n * d.ld;
+    const float ct = LOG2E / d.temperature;
+    bool bad;
+    const int token = token_of(d, n, bad);
+    if (leave_row<NT, T>(d, n, token, bad, false)) return;
+    const float token_logit = to_float(s[token]);
+    Sum sum = part_sum(s, Words<NT, T>(0, d.V), ct);
+    sum = block_reduce<NT>(sum, shared, [ct](Sum x, Sum y) { return joined(x, y, ct); });
+    finish_row(d, n, token_logit, sum.m, log2_sum(sum.s));
+}
+
+// Loss, statistics and gradient: one workgroup a row, whose first HELD words a thread stay in registers and the next KEPT in shared memory from the one load on; only what
+// lies behind is read twice.
+template <int NT, class T, int HELD, int KEPT, bool STREAM>
+__global__ void __launch_bounds__(NT) tr_token_step_kernel(Tokens d)
+{
+    constexpr int N = PER_WORD4<T>;
     constexpr u32 STEP = NT * N, BEHIND = (HELD + KEPT) * STEP;
     __shared__ float scalar[16];
     __shared__ Word4 kept[KEPT > 0 ? KEPT * NT : 1];
@@ -212,24 +328,17 @@ __global__ void __launch_bounds__(NT) tr_token_row_kernel(Tokens d)
     const T* s = (const T*)d.logits + n * d.ld;
     bool bad;
     const int token = token_of(d, n, bad);
-    if (threadIdx.x == 0 && d.status) d.status[n] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
-    if (token < 0) {
-        if (threadIdx.x == 0) write_row(d, n, 0.f, 0.f, 0.f, 0.f);
-        if constexpr (GRAD) write_zeros<NT, T>((T*)d.grad + n * d.ldd, 0, d.V);
-        return;
-    }
+    if (leave_row<NT, T>(d, n, token, bad, true)) return;
     const float token_logit = to_float(s[token]), ct = LOG2E / d.temperature;
+    const Words<NT, T> at(0, d.V);
+    const u32 v0 = threadIdx.x * N, whole = at.whole, end = min(whole, HELD * STEP);
     Sum rest = {-FLT_MAX, 0.f};
-    if (BEHIND < d.V) rest = part_sum<NT, T>(s, BEHIND, d.V, ct);
+    if (BEHIND < whole) rest = part_sum(s, Words<NT, T>(BEHIND, whole), ct);
     float m = rest.m;
     if constexpr (KEPT > 0) {
-        if (HELD * STEP < d.V) {
+        if (HELD * STEP < whole) {
             Word4 w[KEPT];
-#pragma unroll
-            for (int j = 0; j < KEPT; ++j) {
-                const u32 v = threadIdx.x * N + (HELD + j) * STEP;
-                w[j] = v < d.V ? read_logits(s, v, d.V) : lowest_word<T>();
-            }
+            at.template load<STREAM>(w, s, v0 + HELD * STEP);
 #pragma unroll
             for (int j = 0; j < KEPT; ++j) {
                 kept[j * NT + threadIdx.x] = w[j];
@@ -238,12 +347,10 @@ __global__ void __launch_bounds__(NT) tr_token_row_kernel(Tokens d)
         }
     }
     __builtin_amdgcn_sched_barrier(0);                                       // (before the registers fill)
-    // A word belongs to the row as a whole, or is the part that is left, which one thread has besides.
-    const u32 v0 = threadIdx.x * N, whole = (u32)(d.V / N * N), end = min(whole, HELD * STEP);
-    const bool has_last = whole < (u32)d.V && whole < HELD * STEP && whole % STEP == v0;
+    const bool has_last = at.rest();
     Word4 held[HELD];
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) held[j] = v0 + j * STEP < end ? load_loose(s + j * STEP + v0) : lowest_word<T>();
+    for (int j = 0; j < HELD; ++j) held[j] = v0 + j * STEP < end ? load_last<STREAM>(s + j * STEP + v0) : lowest_word<T>();
     Word4 last = lowest_word<T>();
     if (has_last) last = read_logits(s, whole, d.V);
 #pragma unroll
@@ -255,49 +362,52 @@ __global__ void __launch_bounds__(NT) tr_token_row_kernel(Tokens d)
     if (has_last) m = largest<T>(last, m);
     forget_floats(held);
     m = block_reduce<NT>(m, scalar, [](float a, float b) { return fmaxf(a, b); });
-    Sum sum = joined(rest, Sum{m, 0.f}, ct);                                 // (m is the larger)
+    float sum = joined(rest, Sum{m, 0.f}, ct).s;                             // (m is the larger)
+    const bool far = is_far(m, ct);
+    const float from = far ? m : reference(m, ct);
+    with_far(far, [&](auto kind) {
+        constexpr bool FROM_M = decltype(kind)::value;
 #pragma unroll
-    for (int j = 0; j < HELD; ++j)
-        if (j * STEP < end) {
-            add_exponentials<T>(sum, held[j], ct);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    if (has_last) add_exponentials<T>(sum, last, ct);
-    if constexpr (KEPT > 0)
+        for (int j = 0; j < HELD; ++j)
+            if (j * STEP < end) {
+                add_exponentials<T, FROM_M>(sum, held[j], from, ct);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        if (has_last) add_exponentials<T, FROM_M>(sum, last, from, ct);
+        if constexpr (KEPT > 0)
 #pragma unroll 1
-        for (int j = 0; j < KEPT && (HELD + j) * STEP < d.V; ++j) add_exponentials<T>(sum, kept[j * NT + threadIdx.x], ct);
-    const float l = log2_sum(block_reduce<NT>(sum.s, scalar, [](float a, float b) { return a + b; }));
-    const float logp = logp_of(token_logit, m, l, d.temperature);
-    float loss = 0.f, slope = 0.f;
-    if (d.kind == TOKEN_POLICY) slope = policy_of(d, n, logp, loss);
-    if (threadIdx.x == 0) write_row(d, n, m, l, logp, loss);
-    if constexpr (GRAD) {
-        const TokenSlope g = {m, ct, l, slope * d.outer[n] / d.temperature};
-        T* out = (T*)d.grad + n * d.ldd;
-        if (g.c == 0.f) {
-            write_zeros<NT, T>(out, 0, d.V);
-            return;
-        }
-        forget_floats(held);
-        __builtin_amdgcn_s_waitcnt(0);                                       // in place: every thread has the token's logit
-        __syncthreads();
+            for (int j = 0; j < KEPT && (HELD + j) * STEP < whole; ++j) add_exponentials<T, FROM_M>(sum, kept[j * NT + threadIdx.x], from, ct);
+    });
+    const float l = log2_sum(block_reduce<NT>(sum, scalar, [](float a, float b) { return a + b; }));
+    const float slope = finish_row(d, n, token_logit, m, l);
+    const TokenSlope g = token_slope(m, l, d.temperature, slope * d.outer[n]);
+    T* out = (T*)d.grad + n * d.ldd;
+    __builtin_amdgcn_s_waitcnt(0);                                           // in place: every thread has the token's logit
+    __syncthreads();
+    if (g.c == 0.f) {
+        write_zeros<NT, T>(out, 0, d.V);
+        return;
+    }
+    forget_floats(held);
+    with_far(g.far, [&](auto kind) {
+        constexpr bool FROM_M = decltype(kind)::value;
 #pragma unroll
         for (int j = 0; j < HELD; ++j) {
-            if (v0 + j * STEP < end) store_loose(out + j * STEP + v0, gradient_word<T>(g, held[j]));
+            if (v0 + j * STEP < end) store_stream(out + j * STEP + v0, gradient_word<T, FROM_M>(g, held[j]));
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (has_last) write_gradient(out, whole, d.V, gradient_word<T>(g, last));
+        if (has_last) write_gradient(out, whole, d.V, gradient_word<T, FROM_M>(g, last));
         if constexpr (KEPT > 0)
 #pragma unroll 1
             for (int j = 0; j < KEPT; ++j) {
                 const u32 v = v0 + (HELD + j) * STEP;
-                if (v < d.V) write_gradient(out, v, d.V, gradient_word<T>(g, kept[j * NT + threadIdx.x]));
+                if (v < whole) store_stream(out + v, gradient_word<T, FROM_M>(g, kept[j * NT + threadIdx.x]));
             }
-        for (i64 v = v0 + BEHIND; v < d.V; v += STEP) write_gradient(out, v, d.V, gradient_word<T>(g, read_logits(s, v, d.V)));
-        __builtin_amdgcn_s_waitcnt(0);                                       // stores to one address arrive in this order
-        __syncthreads();
-        if (threadIdx.x == 0) out[token] = token_gradient<T>(g, token_logit);
-    }
+        for (u32 v = v0 + BEHIND; v < whole; v += STEP) store_stream(out + v, gradient_word<T, FROM_M>(g, load_loose(s + v)));
+    });
+    __builtin_amdgcn_s_waitcnt(0);                                           // stores to one address arrive in this order
+    __syncthreads();
+    if (threadIdx.x == 0) out[token] = token_gradient<T>(g, token_logit);
 }
 
 __device__ __forceinline__ void part_range(const Tokens& d, int part, int per_word, i64& v0, i64& v1)
@@ -318,7 +428,7 @@ __global__ void __launch_bounds__(NT) tr_token_part_kernel(Tokens d)
     if (token_of(d, n, bad) < 0) return;
     i64 v0, v1;
     part_range(d, blockIdx.x % d.splits, PER_WORD4<T>, v0, v1);
-    Sum sum = part_sum<NT, T>((const T*)d.logits + n * d.ld, v0, v1, ct);
+    Sum sum = part_sum((const T*)d.logits + n * d.ld, Words<NT, T>(v0, v1), ct);
     sum = block_reduce<NT>(sum, shared, [ct](Sum x, Sum y) { return joined(x, y, ct); });
     if (threadIdx.x == 0) {
         float* out = d.partial + (i64)blockIdx.x * 2;
@@ -334,11 +444,7 @@ __global__ void __launch_bounds__(64) tr_token_join_kernel(Tokens d)
     const i64 n = blockIdx.x;
     bool bad;
     const int token = token_of(d, n, bad);
-    if (threadIdx.x == 0 && d.status) d.status[n] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
-    if (token < 0) {
-        if (threadIdx.x == 0) write_row(d, n, 0.f, 0.f, 0.f, 0.f);
-        return;
-    }
+    if (leave_row<64, T>(d, n, token, bad, false)) return;
     const float token_logit = to_float(((const T*)d.logits)[n * d.ld + token]), ct = LOG2E / d.temperature;
     Sum sum = {-FLT_MAX, 0.f};
     for (int p = threadIdx.x; p < d.splits; p += 64) {
@@ -346,32 +452,44 @@ __global__ void __launch_bounds__(64) tr_token_join_kernel(Tokens d)
         sum = joined(sum, Sum{in[0], in[1]}, ct);
     }
     sum = block_reduce<64>(sum, (Sum*)nullptr, [ct](Sum x, Sum y) { return joined(x, y, ct); });
-    const float l = log2_sum(sum.s), logp = logp_of(token_logit, sum.m, l, d.temperature);
-    float loss = 0.f;
-    if (d.kind == TOKEN_POLICY) policy_of(d, n, logp, loss);
-    if (threadIdx.x == 0) write_row(d, n, sum.m, l, logp, loss);
+    finish_row(d, n, token_logit, sum.m, log2_sum(sum.s));
 }
 
 // The gradient from statistics: every row in `splits` parts.  Nothing is read of a row but the workgroup's own part, which it may overwrite.
-template <int NT, class T>
+template <int NT, class T, bool STREAM>
 __global__ void __launch_bounds__(NT) tr_token_gradient_kernel(Tokens d)
 {
     constexpr int N = PER_WORD4<T>;
-    const i64 n = blockIdx.x / d.splits;
+    const i64 row = blockIdx.x / d.splits, n = d.backwards ? d.N - 1 - row : row;
     i64 v0, v1;
     part_range(d, blockIdx.x % d.splits, N, v0, v1);
     const T* s = (const T*)d.logits + n * d.ld;
     T* out = (T*)d.grad + n * d.ldd;
     bool bad;
     const int token = token_of(d, n, bad);
-    const TokenSlope g = {d.stats[n * 3], LOG2E / d.temperature, d.stats[n * 3 + 1], token < 0 ? 0.f : slope_of(d, n, d.stats[n * 3 + 2]) / d.temperature};
+    const TokenSlope g = token_slope(d.stats[n * 3], d.stats[n * 3 + 1], d.temperature, token < 0 ? 0.f : slope_of(d, n, d.stats[n * 3 + 2]));
     if (g.c == 0.f) {
         write_zeros<NT, T>(out, v0, v1);
         return;
     }
-    const bool mine = token >= v0 && token < v1 && (token - v0) / N % NT == threadIdx.x;
+    const Words<NT, T> at(v0, v1);
+    const bool mine = token >= v0 && token < v1 && (token - v0) / N % NT == threadIdx.x, has_rest = at.rest();
     const float token_logit = mine ? to_float(s[token]) : 0.f;
-    for (i64 v = v0 + (i64)threadIdx.x * N; v < v1; v += NT * N) write_gradient(out, v, v1, gradient_word<T>(g, read_logits(s, v, v1)));
+    Word4 rest = lowest_word<T>();
+    if (has_rest) rest = read_logits(s, at.whole, at.end);
+    constexpr u32 AHEAD = 4;
+    with_far(g.far, [&](auto kind) {
+        constexpr bool FROM_M = decltype(kind)::value;
+        for (u32 base = at.first; base < at.whole; base += AHEAD * NT * N) {
+            const u32 v = base + threadIdx.x * N;
+            Word4 w[AHEAD];
+            at.template load<STREAM>(w, s, v);
+#pragma unroll
+            for (u32 j = 0; j < AHEAD; ++j)
+                if (v + j * NT * N < at.whole) store_stream(out + v + j * NT * N, gradient_word<T, FROM_M>(g, w[j]));
+        }
+        if (has_rest) write_gradient(out, at.whole, at.end, gradient_word<T, FROM_M>(g, rest));
+    });
     if (mine) out[token] = token_gradient<T>(g, token_logit);                // behind this thread's own store of that word
 }
 
