@@ -45,6 +45,18 @@ __device__ __forceinline__ void store_loose(T* p, Word4 v)
     *reinterpret_cast<LooseWord4*>(p) = v;
 }
 
+// Past the caches: results that nobody reads soon, and, with STREAM, operands on their last read.
+template <class T>
+__device__ __forceinline__ void store_stream(T* p, Word4 v)
+{
+    __builtin_nontemporal_store(v, reinterpret_cast<LooseWord4*>(p));
+}
+template <bool STREAM, class T>
+__device__ __forceinline__ Word4 load_last(const T* p)
+{
+    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const LooseWord4*>(p)) : load_loose(p);
+}
+
 // Up to 16 bytes from p: `have` elements exist (any number, also none or more than fit), the others read as zero.
 template <class T>
 __device__ __forceinline__ Word4 load_some(const T* p, i64 have)

@@ -45,13 +45,66 @@ struct Raw8 {
     }
 };
 
+// Elements moved down by `by`; zeros come from above, for 8 and more all of them.
+__device__ __forceinline__ void move_down(Raw8<float>& r, int by)
+{
+#pragma unroll
+    for (int x = 1; x < 8; x *= 2) {
+        const Word4 lo = r.w[0], hi = r.w[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r.w[0][i] = by & x ? i + x < 4 ? lo[(i + x) & 3] : hi[(i + x) & 3] : lo[i];
+            r.w[1][i] = by & x ? i + x < 4 ? hi[(i + x) & 3] : 0 : hi[i];
+        }
+    }
+    if (by >= 8) r.w[0] = r.w[1] = Word4{0, 0, 0, 0};
+}
 template <class T>
-__device__ __forceinline__ Raw8<T> load8(const T* p, int have)
+__device__ __forceinline__ void move_down(Raw8<T>& r, int by)
+{
+    static_assert(sizeof(T) == 2);
+    const unsigned __int128 v = __builtin_bit_cast(unsigned __int128, r.w[0]);
+    r.w[0] = by >= 8 ? Word4{0, 0, 0, 0} : __builtin_bit_cast(Word4, v >> 16 * by);
+}
+
+// Element k of a row: 32 bits beside the row's address, which is the same for a wave that has one row.
+template <class T>
+__device__ __forceinline__ T* element(T* row, int k)
+{
+    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (u32)k * (u32)sizeof(T));
+}
+
+// The group of G threads that this one is part of, as a number that the whole wave shares where it does.
+template <int G>
+__device__ __forceinline__ int group_of()
+{
+    const int group = threadIdx.x / G;
+    return G >= WAVE ? __builtin_amdgcn_readfirstlane(group) : group;
+}
+
+// Elements k to k + 7 of a row of K; zeros behind its end.  What passes the end is read from where it fits and moved: so no load stands in a
+// branch, where it would wait for those before it.
+template <bool LAST = false, class T>
+__device__ __forceinline__ Raw8<T> load8(const T* row, int k, int K)
 {
     Raw8<T> r;
+    if (K < 8) {                                                             // (the same for all)
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = load_some(p + j * PER_WORD4<T>, (i64)have - j * PER_WORD4<T>);
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = load_some(row + k + j * PER_WORD4<T>, (i64)K - k - j * PER_WORD4<T>);
+        return r;
+    }
+    const T* p = element(row, min(k, K - 8));
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = load_last<LAST>(p + j * PER_WORD4<T>);
+    if (k > K - 8) move_down(r, k - (K - 8));
     return r;
+}
+
+template <class T>
+__device__ __forceinline__ void forget_words(Raw8<T>& r)
+{
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) asm volatile("" : "+v"(r.w[j]));
 }
 
 template <class T>
@@ -63,20 +116,53 @@ __device__ __forceinline__ Raw8<T> zero8()
     return r;
 }
 
-template <class T>
-__device__ __forceinline__ void store8(T* p, int have, const float (&v)[8])
+template <bool STREAM = false, class T>
+__device__ __forceinline__ void store8(T* row, int k, int K, const float (&v)[8])
 {
     Pack<T> w[sizeof(T) / 2];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i / PER_WORD4<T>].v[i % PER_WORD4<T>] = from_float<T>(v[i]);
-    if (have >= 8) {
+    T* p = element(row, k);
+    if (k + 8 <= K) {
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(T) / 2; ++j) store_loose(p + j * PER_WORD4<T>, w[j].raw);
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+            if (STREAM) store_stream(p + j * PER_WORD4<T>, w[j].raw);
+            else store_loose(p + j * PER_WORD4<T>, w[j].raw);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (i < have) p[i] = w[i / PER_WORD4<T>].v[i % PER_WORD4<T>];
+        if (k + i < K) p[i] = w[i / PER_WORD4<T>].v[i % PER_WORD4<T>];
+}
+
+// v and the same of the lane that CTRL names, within rows of 16 lanes; no trip through shared memory.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float plus_lane(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+
+// The sum over each G neighbouring lanes, for all of them; G up to 32.
+template <int G>
+__device__ __forceinline__ float row_sum(float v)
+{
+    if constexpr (G > 1) v = plus_lane<0xB1>(v);                             // lanes 1 0 3 2 of each four
+    if constexpr (G > 2) v = plus_lane<0x4E>(v);                             // 2 3 0 1
+    if constexpr (G > 4) v = plus_lane<0x141>(v);                            // 7 to 0 of each eight
+    if constexpr (G > 8) v = plus_lane<0x140>(v);                            // 15 to 0 of each sixteen
+    if constexpr (G > 16) v += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401f));   // the sixteen beside
+    return v;
+}
+
+__device__ __forceinline__ float from_lane(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
+// The sum over a wave, as a number that it shares.
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = row_sum<16>(v);
+    v = plus_lane<0x142, 0xa>(v);                                            // lane 15 of the row before, for rows 1 and 3
+    v = plus_lane<0x143, 0xc>(v);                                            // lane 31, for rows 2 and 3
+    return from_lane(v, 63);
 }
 
 // Sums over the G threads of a row, in an order that G fixes.  One barrier: the buffer of one call is written again in the call after the next,
@@ -85,10 +171,9 @@ template <int G, int NT, int NV>
 __device__ __forceinline__ void group_sum(float (&v)[NV], float* shared, int& turn)
 {
 #pragma unroll
-    for (int d = (G < WAVE ? G : WAVE) / 2; d > 0; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] += __shfl_xor(v[i], d);
+    for (int i = 0; i < NV; ++i) v[i] = G >= WAVE ? wave_sum(v[i]) : row_sum<G>(v[i]);
     if constexpr (G > WAVE) {
+        constexpr int W = G / WAVE;
         float* buffer = shared + turn * (NT / WAVE * NV);
         turn ^= 1;
         const int wave = threadIdx.x / WAVE;
@@ -96,13 +181,9 @@ __device__ __forceinline__ void group_sum(float (&v)[NV], float* shared, int& tu
 #pragma unroll
             for (int i = 0; i < NV; ++i) buffer[wave * NV + i] = v[i];
         __syncthreads();
-        const float* mine = buffer + wave / (G / WAVE) * (G / WAVE) * NV;
+        const float* mine = buffer + (wave / W * W + threadIdx.x % W) * NV;  // a wave of the row for each lane
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            v[i] = mine[i];
-#pragma unroll
-            for (int w = 1; w < G / WAVE; ++w) v[i] += mine[w * NV + i];
-        }
+        for (int i = 0; i < NV; ++i) v[i] = from_lane(row_sum<W>(mine[i]), 0);
     }
 }
 
@@ -119,11 +200,11 @@ struct Factor {
 };
 
 template <class T>
-__device__ __forceinline__ Factor<T> factor_of(const Norm& a, const Generator& g, i64 row, int unit, int have)
+__device__ __forceinline__ Factor<T> factor_of(const Norm& a, const Generator& g, i64 row, int unit)
 {
     Factor<T> f;
     f.gated = a.gate != nullptr;
-    f.gate = f.gated ? load8((const T*)a.gate + row * a.ldgate + unit * 8, have) : zero8<T>();
+    f.gate = f.gated ? load8((const T*)a.gate + row * a.ldgate, unit * 8, a.K) : zero8<T>();
     f.keep = 0xffu;
     f.scale = a.scale;
     if (a.random.threshold) {
@@ -149,30 +230,28 @@ __device__ __forceinline__ void stream8(const Norm& a, const Raw8<S>& x, const R
     }
 }
 
-// Forward: G threads a row, U units of eight elements each.
+// Forward: G threads a row, U units of eight elements each.  Memory bounds it: 8192 x 4096 in bf16 53 us, 5.1 TB/s.  y is stored past the caches, for the next block comes first; n is what that reads.
 template <class S, class T, int G, int U, int NT>
 __global__ void __launch_bounds__(NT) tr_norm_forward_kernel(Norm a)
 {
     __shared__ float shared[2 * NT / WAVE];
     constexpr int R = NT / G;
     const int lane = threadIdx.x % G;
-    const i64 row = (i64)blockIdx.x * R + threadIdx.x / G;
-    const bool in = row < a.M;
+    const i64 mine = (i64)blockIdx.x * R + group_of<G>(), row = min(mine, a.M - 1);
+    const bool in = mine < a.M;                                              // (others go along with the last row, for the barriers, and write nothing)
     int turn = 0;
     Generator g = {};
     if (a.random.threshold) g = generator(a.random);
     Raw8<S> x[U];
     Raw8<T> b[U], w[U], wp[U];
-    int have[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int unit = lane + u * G;
-        have[u] = in ? a.K - unit * 8 : 0;
-        x[u] = load8((const S*)a.x + row * a.ldx + unit * 8, have[u]);
+        x[u] = load8((const S*)a.x + row * a.ldx, unit * 8, a.K);
         b[u] = wp[u] = zero8<T>();
-        if (a.branch) b[u] = load8((const T*)a.branch + row * a.ldb + unit * 8, have[u]);
-        if (a.post_weight) wp[u] = load8((const T*)a.post_weight + unit * 8, have[u]);
-        w[u] = load8((const T*)a.weight + unit * 8, have[u]);
+        if (a.branch) b[u] = load8((const T*)a.branch + row * a.ldb, unit * 8, a.K);
+        if (a.post_weight) wp[u] = load8((const T*)a.post_weight, unit * 8, a.K);
+        w[u] = load8((const T*)a.weight, unit * 8, a.K);
     }
     float rb = 0.f;
     if (a.post_weight) {
@@ -189,9 +268,9 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_kernel(Norm a)
     for (int u = 0; u < U; ++u) {
         const int unit = lane + u * G;
         Factor<T> f = {};
-        if (a.branch && have[u] > 0) f = factor_of<T>(a, g, row, unit, have[u]);
+        if (a.branch) f = factor_of<T>(a, g, row, unit);
         stream8<S, T>(a, x[u], b[u], wp[u], f, rb, y[u]);
-        if (a.branch && have[u] > 0) store8((S*)a.y + row * a.ldy + unit * 8, have[u], y[u]);
+        if (a.branch && in && unit * 8 < a.K) store8<true>((S*)a.y + row * a.ldy, unit * 8, a.K, y[u]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[0] = fmaf(y[u][i], y[u][i], sum[0]);
     }
@@ -199,10 +278,10 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_kernel(Norm a)
     const float r = inverse_root(sum[0], a.K, a.eps);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (have[u] <= 0) continue;
+        if (!in || (lane + u * G) * 8 >= a.K) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[u][i] = y[u][i] * r * w[u][i];
-        store8((T*)a.n + row * a.ldn + (lane + u * G) * 8, have[u], y[u]);
+        store8((T*)a.n + row * a.ldn, (lane + u * G) * 8, a.K, y[u]);
     }
     if (in && lane == 0 && a.stats) {
         a.stats[row * 2] = r;
@@ -225,7 +304,7 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_wide_kernel(Norm a)
     if (a.post_weight) {
         float sum[1] = {0.f};
         for (int k = threadIdx.x * 8; k < a.K; k += NT * 8) {
-            const Raw8<T> b = load8(bs + k, a.K - k);
+            const Raw8<T> b = load8(bs, k, a.K);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[0] = fmaf(b[i], b[i], sum[0]);
         }
@@ -233,15 +312,14 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_wide_kernel(Norm a)
         rb = inverse_root(sum[0], a.K, a.eps);
     }
     auto at = [&](int k, float (&y)[8]) {
-        const int have = a.K - k;
         Raw8<T> b = zero8<T>(), wp = zero8<T>();
         Factor<T> f = {};
         if (a.branch) {
-            b = load8(bs + k, have);
-            f = factor_of<T>(a, g, row, k / 8, have);
+            b = load8(bs, k, a.K);
+            f = factor_of<T>(a, g, row, k / 8);
         }
-        if (a.post_weight) wp = load8((const T*)a.post_weight + k, have);
-        stream8<S, T>(a, load8(xs + k, have), b, wp, f, rb, y);
+        if (a.post_weight) wp = load8((const T*)a.post_weight, k, a.K);
+        stream8<S, T>(a, load8(xs, k, a.K), b, wp, f, rb, y);
     };
     float sum[1] = {0.f}, y[8];
     for (int k = threadIdx.x * 8; k < a.K; k += NT * 8) {
@@ -253,11 +331,11 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_wide_kernel(Norm a)
     const float r = inverse_root(sum[0], a.K, a.eps);
     for (int k = threadIdx.x * 8; k < a.K; k += NT * 8) {
         at(k, y);
-        if (a.branch) store8((S*)a.y + row * a.ldy + k, a.K - k, y);         // (after the row's last look at x, which y may replace)
-        const Raw8<T> w = load8((const T*)a.weight + k, a.K - k);
+        if (a.branch) store8((S*)a.y + row * a.ldy, k, a.K, y);         // (after the row's last look at x, which y may replace)
+        const Raw8<T> w = load8((const T*)a.weight, k, a.K);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = y[i] * r * w[i];
-        store8((T*)a.n + row * a.ldn + k, a.K - k, y);
+        store8((T*)a.n + row * a.ldn, k, a.K, y);
     }
     if (threadIdx.x == 0 && a.stats) {
         a.stats[row * 2] = r;
@@ -265,30 +343,44 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_wide_kernel(Norm a)
     }
 }
 
-// Eight elements of a row in the backward pass.
+// Eight elements of a row in the backward pass: as they lie in memory ...
 template <class S, class T>
 struct Back8 {
     Raw8<S> y, dy;
-    Raw8<T> dn, b;
-    Factor<T> f;
+    Raw8<T> dn, b, gate;
 
-    __device__ __forceinline__ void load(const Norm& a, const Generator& g, i64 row, int unit, int have)
+    // (Gates of channels are those of the row before.)
+    __device__ __forceinline__ void load(const Norm& a, i64 row, int unit, bool first)
     {
-        const i64 k = (i64)unit * 8;
-        y = load8((const S*)a.y + row * a.ldy + k, have);
-        dy = a.dy && have > 0 ? load8((const S*)a.dy + row * a.lddy + k, have) : zero8<S>();
-        dn = a.dn && have > 0 ? load8((const T*)a.dn + row * a.lddn + k, have) : zero8<T>();
-        b = zero8<T>();
-        f = {};
-        if (a.branch && have > 0) {
-            b = load8((const T*)a.branch + row * a.ldb + k, have);
-            f = factor_of<T>(a, g, row, unit, have);
-        }
+        const int k = unit * 8;
+        y = load8((const S*)a.y + row * a.ldy, k, a.K);
+        dy = a.dy ? load8((const S*)a.dy + row * a.lddy, k, a.K) : zero8<S>();
+        dn = a.dn ? load8((const T*)a.dn + row * a.lddn, k, a.K) : zero8<T>();
+        b = a.branch ? load8((const T*)a.branch + row * a.ldb, k, a.K) : zero8<T>();
+        if (first) gate = zero8<T>();
+        if (a.gate && (first || a.ldgate)) gate = load8((const T*)a.gate + row * a.ldgate, k, a.K);
+    }
+
+    // What the branch is multiplied by; computed where it is wanted.
+    __device__ __forceinline__ Factor<T> factor(const Norm& a, u32 keep) const
+    {
+        return Factor<T>{gate, keep, a.random.threshold ? a.scale * a.random.kept : a.scale, a.gate != nullptr};
+    }
+
+    // ... and not as the floats of one use kept for the next.
+    __device__ __forceinline__ void forget()
+    {
+        forget_words(y);
+        forget_words(dy);
+        forget_words(dn);
+        forget_words(b);
+        forget_words(gate);
     }
 
     // mean(dn w u), mean(q h (dy + r dn w)) and mean(q h u), not yet divided.
-    __device__ __forceinline__ void sums(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, float r, float rb, float (&sum)[3]) const
+    __device__ __forceinline__ void sums(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, float r, float rb, float (&sum)[3]) const
     {
+        const Factor<T> f = factor(a, keep);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float u = y[i] * r, dnw = dn[i] * w[i];
@@ -302,27 +394,38 @@ struct Back8 {
     }
 
     // The row's results, and what it adds to the columns' sums.
-    __device__ __forceinline__ void results(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, i64 row, int unit, int have, float r, float rb,
+    __device__ __forceinline__ void results(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, i64 row, int unit, float r, float rb,
                                             float c1, float c2, float (&dw)[8], float (&dwp)[8], float (&dg)[8]) const
     {
-        const i64 k = (i64)unit * 8;
+        const Factor<T> f = factor(a, keep);
+        const int k = unit * 8;
         float dx[8], db[8], gate[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float u = y[i] * r;
             dx[i] = fmaf(r, fmaf(-u, c1, dn[i] * w[i]), dy[i]);
-            dw[i] = dn[i] * u;
-            db[i] = dwp[i] = dg[i] = gate[i] = 0.f;
-            if (a.branch) {
-                const float dd = f[i] * dx[i], h = a.post_weight ? b[i] * rb : b[i];
-                db[i] = a.post_weight ? rb * fmaf(-h, c2, dd * wp[i]) : dd;
-                dwp[i] = dd * h;
-                dg[i] = gate[i] = f.kept(i) ? f.scale * (a.post_weight ? h * wp[i] : h) * dx[i] : 0.f;
+            dw[i] = fmaf(dn[i], u, dw[i]);
+        }
+        if (a.dx) store8<true>((S*)a.dx + row * a.lddx, k, a.K, dx);
+        if (!a.branch) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float dd = f[i] * dx[i];
+            float h = b[i], d = h;
+            db[i] = dd;
+            if (a.post_weight) {
+                h *= rb;
+                d = h * wp[i];
+                db[i] = rb * fmaf(-h, c2, dd * wp[i]);
+                dwp[i] = fmaf(dd, h, dwp[i]);
+            }
+            if (a.gate) {
+                gate[i] = f.kept(i) ? f.scale * d * dx[i] : 0.f;
+                dg[i] += gate[i];
             }
         }
-        if (a.dx) store8((S*)a.dx + row * a.lddx + k, have, dx);
-        if (a.dbranch) store8((T*)a.dbranch + row * a.lddb + k, have, db);
-        if (a.dgate) store8((T*)a.dgate + row * a.lddgate + k, have, gate);
+        if (a.dbranch) store8<true>((T*)a.dbranch + row * a.lddb, k, a.K, db);
+        if (a.dgate) store8<true>((T*)a.dgate + row * a.lddgate, k, a.K, gate);
     }
 };
 
@@ -332,80 +435,119 @@ __device__ __forceinline__ void means(const Norm& a, const float (&sum)[3], floa
     c2 = (sum[1] - c1 * r * sum[2]) / (float)a.K;
 }
 
-// Backward: each workgroup takes rows R apart over the whole grid, G threads a row, and keeps its columns' sums in registers until the end.
-template <class S, class T, int G, int U, int NT>
+// How a backward pass keeps its row: not at all (what the results need is read again, from the cache), in registers, or with the next row under way besides.
+enum Keep { REREAD, HOLD, AHEAD };
+
+// Backward: each workgroup takes rows R apart over the whole grid, G threads a row, and keeps its columns' sums in registers until the end.  Memory bounds it, and the sums' way: 8192 x 4096 in bf16
+// with both norms, a gate for each channel and dropout 89 us, 4.5 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 92, 4.4; 262144 x 64 50, 4.0; 2048 x 16384, where the row is read again, 193, 2.1).
+// Weights and rows stay as they lie in memory: as floats, which the compiler would keep over the exchange, they took 232 registers a thread, and one workgroup stood where four do.
+template <class S, class T, int G, int U, int NT, Keep KEEP>
 __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 {
-    constexpr int R = NT / G, COLUMNS = G * U * 8;
+    constexpr int R = NT / G, COLUMNS = G * U * 8, UNITS = KEEP == REREAD ? 1 : U;
     __shared__ float shared[2 * NT / WAVE * 3];
     __shared__ float columns[R > 1 ? COLUMNS : 1];
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
+    const int lane = threadIdx.x % G, group = group_of<G>();
     int turn = 0;
     Generator g = {};
     if (a.random.threshold) g = generator(a.random);
-    Raw8<T> w[U], wp[U];
+    Raw8<T> w[UNITS], wp[UNITS];
     float dw[U][8] = {}, dwp[U][8] = {}, dg[U][8] = {};
+    auto load_weights = [&](Raw8<T>& w, Raw8<T>& wp, int unit) {
+        w = load8((const T*)a.weight, unit * 8, a.K);
+        wp = a.post_weight ? load8((const T*)a.post_weight, unit * 8, a.K) : zero8<T>();
+    };
+    if constexpr (KEEP != REREAD)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int unit = lane + u * G;
-        w[u] = load8((const T*)a.weight + unit * 8, a.K - unit * 8);
-        wp[u] = zero8<T>();
-        if (a.post_weight) wp[u] = load8((const T*)a.post_weight + unit * 8, a.K - unit * 8);
-    }
-    for (i64 base = (i64)blockIdx.x * R; base < a.M; base += (i64)gridDim.x * R) {       // (the same turns for the whole workgroup: barriers)
-        const i64 row = base + group;
-        const bool in = row < a.M;
-        const float r = in ? a.stats[row * 2] : 0.f, rb = in ? a.stats[row * 2 + 1] : 0.f;
-        Back8<S, T> e[U];
+        for (int u = 0; u < U; ++u) load_weights(w[u], wp[u], lane + u * G);
+    struct Row {
+        Back8<S, T> e[UNITS];
+        float r, rb;
+    };
+    // Groups behind the last row go along with it, for the barriers, and leave nothing.
+    auto load = [&](Row& to, i64 base, bool first) {
+        const i64 row = min(base + group, a.M - 1);
+        to.r = a.stats[row * 2];
+        to.rb = a.stats[row * 2 + 1];
+        if constexpr (KEEP != REREAD)
+#pragma unroll
+            for (int u = 0; u < U; ++u) to.e[u].load(a, row, lane + u * G, first);
+    };
+    const i64 step = (i64)gridDim.x * R;
+    Row row, next;
+    if constexpr (KEEP == AHEAD) load(next, (i64)blockIdx.x * R, true);
+    for (i64 base = (i64)blockIdx.x * R; base < a.M; base += step) {         // (the same turns for the whole workgroup: barriers)
+        if constexpr (KEEP == AHEAD) {
+            row = next;
+            if (base + step < a.M) load(next, base + step, false);
+        } else load(row, base, base < step);
+        const i64 n = base + group, held = min(n, a.M - 1);
+        const bool in = n < a.M;
         float sum[3] = {0.f, 0.f, 0.f};
+        u32 keep[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = lane + u * G;
-            e[u].load(a, g, row, unit, in ? a.K - unit * 8 : 0);
+            const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            if constexpr (KEEP == REREAD) {
+                load_weights(w[0], wp[0], unit);
+                row.e[0].load(a, held, unit, true);
+            } else {
+                forget_words(w[u]);
+                forget_words(wp[u]);
+            }
+            keep[u] = a.random.threshold ? keep_bits(g, a.random.threshold, (u32)unit, (u32)n) : 0xffu;
+            row.e[at].sums(a, w[at], wp[at], keep[u], row.r, row.rb, sum);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) e[u].sums(a, w[u], wp[u], r, rb, sum);
         group_sum<G, NT>(sum, shared, turn);
         float c1, c2;
-        means(a, sum, r, c1, c2);
-        if (!in) continue;                                                   // (its last turn)
+        means(a, sum, row.r, c1, c2);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = lane + u * G, have = a.K - unit * 8;
-            if (have <= 0) continue;
-            float w8[8], p8[8], g8[8];
-            e[u].results(a, w[u], wp[u], row, unit, have, r, rb, c1, c2, w8, p8, g8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                dw[u][i] += w8[i];
-                dwp[u][i] += p8[i];
-                dg[u][i] += g8[i];
+            const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            if constexpr (KEEP == REREAD) {
+                load_weights(w[0], wp[0], unit);
+                row.e[0].load(a, held, unit, true);
+            } else {
+                row.e[u].forget();
+                forget_words(w[u]);
+                forget_words(wp[u]);
             }
+            if (in && unit * 8 < a.K) row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, c1, c2, dw[u], dwp[u], dg[u]);
         }
     }
     const int padded = (a.K + 7) / 8 * 8;
+    // The rows' groups joined: those of a wave by exchanges between its lanes, then the waves one after the other.
+    constexpr int JOINED = G < WAVE ? WAVE : G, STEPS = NT / JOINED;
+    const int turn_of = threadIdx.x / JOINED;
     auto join = [&](float (&v)[U][8], int place) {
         if (place < 0) return;
         float* out = a.partial + ((i64)blockIdx.x * a.sums + place) * padded;
-        if constexpr (R > 1) {                                               // the groups one after the other
-            for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int d = G; d < WAVE; d *= 2)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[u][i] += __shfl_xor(v[u][i], d);
+        if constexpr (STEPS > 1) {
+            for (int r = 0; r < STEPS; ++r) {
                 __syncthreads();
-                if (group != r) continue;
+                if (turn_of != r || (int)(threadIdx.x % JOINED) >= G) continue;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float& c = columns[i * (G * U) + u * G + lane];
-                        if (r == R - 1) v[u][i] += c;
+                        if (r == STEPS - 1) v[u][i] += c;
                         else c = r == 0 ? v[u][i] : c + v[u][i];
                     }
             }
-            if (group != R - 1) return;
+            if (turn_of != STEPS - 1) return;
         }
+        if ((int)(threadIdx.x % JOINED) >= G) return;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int unit = lane + u * G;
-            if (unit * 8 < a.K) store8(out + unit * 8, 8, v[u]);
+            if (unit * 8 < a.K) store8(out, unit * 8, padded, v[u]);
         }
     };
     join(dw, a.sum_w);
@@ -427,32 +569,30 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_wide_kernel(Norm a)
         float sum[3] = {0.f, 0.f, 0.f}, c1, c2;
         auto each = [&](auto&& f) {
             for (int unit = threadIdx.x; unit * 8 < a.K; unit += NT) {
-                const int have = a.K - unit * 8;
                 Back8<S, T> e;
-                e.load(a, g, row, unit, have);
-                const Raw8<T> w = load8((const T*)a.weight + unit * 8, have);
-                const Raw8<T> wp = a.post_weight ? load8((const T*)a.post_weight + unit * 8, have) : zero8<T>();
-                f(unit, have, e, w, wp);
+                e.load(a, row, unit, true);
+                const Raw8<T> w = load8((const T*)a.weight, unit * 8, a.K);
+                const Raw8<T> wp = a.post_weight ? load8((const T*)a.post_weight, unit * 8, a.K) : zero8<T>();
+                f(unit, a.random.threshold ? keep_bits(g, a.random.threshold, (u32)unit, (u32)row) : 0xffu, e, w, wp);
             }
         };
-        each([&](int, int, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) { e.sums(a, w, wp, r, rb, sum); });
+        each([&](int, u32 keep, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) { e.sums(a, w, wp, keep, r, rb, sum); });
         group_sum<NT, NT>(sum, shared, turn);
         means(a, sum, r, c1, c2);
-        each([&](int unit, int have, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) {
-            float v[3][8];
-            e.results(a, w, wp, row, unit, have, r, rb, c1, c2, v[0], v[1], v[2]);
+        each([&](int unit, u32 keep, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) {
+            float v[3][8] = {};
             const int place[3] = {a.sum_w, a.sum_post, a.sum_gate};
 #pragma unroll
-            for (int s = 0; s < 3; ++s) {
-                if (place[s] < 0) continue;
-                float* out = mine + (i64)place[s] * padded + unit * 8;       // this thread's alone
-                if (row != blockIdx.x) {
-                    const Raw8<float> before = load8(out, 8);
+            for (int s = 0; s < 3; ++s)                                      // (this thread's alone, from its row before)
+                if (place[s] >= 0 && row != blockIdx.x) {
+                    const Raw8<float> before = load8(mine + (i64)place[s] * padded, unit * 8, padded);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[s][i] += before[i];
+                    for (int i = 0; i < 8; ++i) v[s][i] = before[i];
                 }
-                store8(out, 8, v[s]);
-            }
+            e.results(a, w, wp, keep, row, unit, r, rb, c1, c2, v[0], v[1], v[2]);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+                if (place[s] >= 0) store8(mine + (i64)place[s] * padded, unit * 8, padded, v[s]);
         });
     }
 }
@@ -487,8 +627,9 @@ struct Dropout {
     Random random;
 };
 
-// Dropout: every thread takes units of eight elements, 256 apart, of its workgroup's stretch of all the rows' units.
-template <class T, int EACH>
+// Dropout: every thread takes units of eight elements, 256 apart, of its workgroup's stretch of all the rows' units.  Memory bounds it, 8192 x 12288 in bf16 73 us, 5.5 TB/s; the
+// generator's 14 products a unit are 27 us of it, beside.
+template <class T, int EACH, bool STREAM>
 __global__ void __launch_bounds__(256) tr_dropout_kernel(Dropout a)
 {
     const u32 units = ((u32)a.K + 7) / 8;
@@ -502,13 +643,12 @@ __global__ void __launch_bounds__(256) tr_dropout_kernel(Dropout a)
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
         if (row < a.M) {
-            const int have = a.K - (int)unit * 8;
-            const Raw8<T> x = load8((const T*)a.x + row * a.ldx + unit * 8, have);
+            const Raw8<T> x = load8<STREAM>((const T*)a.x + row * a.ldx, (int)unit * 8, a.K);
             const u32 keep = a.random.threshold ? keep_bits(g, a.random.threshold, unit, (u32)row) : 0xffu;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = keep >> i & 1 ? x[i] * a.random.kept : 0.f;
-            store8((T*)a.out + row * a.ldout + unit * 8, have, v);
+            store8<STREAM>((T*)a.out + row * a.ldout, (int)unit * 8, a.K, v);
         }
         row += rows;
         unit += left;

@@ -16,19 +16,6 @@
 
 namespace {
 
-// Gradients pass the caches by, and so do logits on their last read, for there is no other soon.  policy_step_4096 417 us with neither, 395 with the stores, 376 with both;
-// logp_train_1024 89, 80 and 72.  Not logits whose words cross lines: those are read twice, by neighbours (policy_separate_odd 62 and, passing by, 70).
-template <class T>
-__device__ __forceinline__ void store_stream(T* p, Word4 v)
-{
-    __builtin_nontemporal_store(v, reinterpret_cast<LooseWord4*>(p));
-}
-template <bool STREAM, class T>
-__device__ __forceinline__ Word4 load_last(const T* p)
-{
-    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const LooseWord4*>(p)) : load_loose(p);
-}
-
 enum TokenLoss { TOKEN_LOGP, TOKEN_POLICY, TOKEN_PREFERENCE };
 
 struct Tokens {

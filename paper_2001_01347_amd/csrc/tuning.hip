@@ -23,6 +23,9 @@ namespace {
 constexpr i64 WIDTH_MAX = 1ll << 30;             // a row's elements are counted in 31 bits
 constexpr int HELD_UNITS = 2048;                 // units of eight elements of the widest row that a workgroup holds
 
+// What the last-level cache (256 MB) keeps between two kernels at best.
+constexpr i64 LAST_CACHE = 200ll << 20;
+
 bool finite(float x) { return x - x == 0.f; }
 
 int check_random(float p, uint64_t seed, uint64_t offset, const int64_t* rng, Random& r)
@@ -63,28 +66,53 @@ int check_norm_operands(const Norm& a, int stream, int dtype)
     return EBSP_OK;
 }
 
-// Threads a row and units a thread, by the row's units; a thread of its own workgroup size each.
-template <class F>
+// Threads a row and units a thread, by the row's units.  A forward pass has registers to spare: two units a thread, and half the waves to exchange sums between.
+template <bool FORWARD, class F>
 int with_group(int units, F&& f)
 {
-    if (units <= 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
-    if (units <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    if (units <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    if (units <= 128) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    if (units <= 256) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    if (units <= 512) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    if (units <= 1024) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+#define GROUP(threads, each) f(std::integral_constant<int, threads>(), std::integral_constant<int, each>())
+    if (units <= 8) return GROUP(8, 1);
+    if (units <= 16) return GROUP(16, 1);
+    if (units <= 32) return GROUP(32, 1);
+    if (units <= 64) return GROUP(64, 1);
+    if constexpr (FORWARD) {
+        if (units <= 128) return GROUP(64, 2);
+        if (units <= 256) return GROUP(128, 2);
+        if (units <= 512) return GROUP(256, 2);
+        if (units <= 1024) return GROUP(512, 2);
+    } else {
+        if (units <= 128) return GROUP(128, 1);
+        if (units <= 256) return GROUP(256, 1);
+        if (units <= 512) return GROUP(512, 1);
+        if (units <= 1024) return GROUP(1024, 1);
+    }
+    return GROUP(1024, 2);
+#undef GROUP
 }
 
-int group_threads(int units) { return units <= 8 ? 8 : units <= 16 ? 16 : units <= 128 ? 64 : units <= 512 ? 256 : 1024; }
-
-// Workgroups of a backward pass, whose columns' sums are joined by a second kernel: no more than two a CU.
-int norm_blocks(i64 M, i64 K)
+int group_threads(int units)
 {
-    const int units = (int)((K + 7) / 8), g = group_threads(units), rows = g < 256 ? 256 / g : 1;
+    const int sizes[] = {8, 16, 32, 64, 128, 256, 512};
+    for (int g : sizes)
+        if (units <= g) return g;
+    return 1024;
+}
+
+// How a backward pass is launched.  Every workgroup leaves a row of columns' sums behind, so one a CU takes all rows where there are enough of them.  16-bit operands: 1024 threads with
+// the next row under way (8192 x 4096 94 us; 512 threads two a CU 97).  With a stream in fp32 there are no registers for that: 512 threads, two a CU (fp32 4096 x 4096 92 us, bf16
+// beside it 70; 1024 threads 98 and, with the next row under way in what then spills, 103).  Few rows: as many workgroups as there are CUs before anything else.
+struct NormCut {
+    int threads, blocks;
+};
+
+NormCut norm_cut(i64 M, i64 K, bool narrow)
+{
+    const int units = (int)((K + 7) / 8), g = group_threads(units), big = g == 1024 || narrow ? 1024 : 512;
+    NormCut c = {M >= 1024 / g * 1024 ? big : g < 256 ? 256 : g, 0};
+    const int rows = c.threads / g > 0 ? c.threads / g : 1, most = c.threads == 1024 ? 256 : 512;
     const i64 blocks = (M + rows - 1) / rows;
-    return (int)(blocks < 512 ? blocks : 512);
+    c.blocks = (int)(blocks < most ? blocks : most);
+    return c;
 }
 
 template <class S, class T>
@@ -95,7 +123,7 @@ int norm_forward(const Norm& a, hipStream_t st)
         LAUNCH((tr_norm_forward_wide_kernel<S, T, 1024>), dim3((unsigned)a.M), dim3(1024), a);
         return EBSP_OK;
     }
-    return with_group(units, [&](auto group, auto each) {
+    return with_group<true>(units, [&](auto group, auto each) {
         constexpr int G = decltype(group)::value, U = decltype(each)::value, NT = G < 256 ? 256 : G;
         LAUNCH((tr_norm_forward_kernel<S, T, G, U, NT>), dim3((unsigned)((a.M + NT / G - 1) / (NT / G))), dim3(NT), a);
         return (int)EBSP_OK;
@@ -111,9 +139,13 @@ int norm_backward(const Norm& a, hipStream_t st)
         if (units > HELD_UNITS)
             LAUNCH((tr_norm_backward_wide_kernel<S, T, 1024>), dim3(a.blocks), dim3(1024), a);
         else
-            rc = with_group(units, [&](auto group, auto each) {
-                constexpr int G = decltype(group)::value, U = decltype(each)::value, NT = G < 256 ? 256 : G;
-                LAUNCH((tr_norm_backward_kernel<S, T, G, U, NT>), dim3(a.blocks), dim3(NT), a);
+            rc = with_group<false>(units, [&](auto group, auto each) {
+                constexpr int G = decltype(group)::value, U = decltype(each)::value, SMALL = G < 256 ? 256 : G;
+                constexpr bool NARROW = sizeof(S) == 2;
+                constexpr int BIG = G == 1024 || NARROW ? 1024 : 512;
+                constexpr Keep KEEP = U == 2 ? REREAD : NARROW ? AHEAD : HOLD;
+                if (norm_cut(a.M, a.K, NARROW).threads == BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, BIG, KEEP>), dim3(a.blocks), dim3(BIG), a);
+                else if constexpr (SMALL < BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, SMALL, KEEP>), dim3(a.blocks), dim3(SMALL), a);
                 return (int)EBSP_OK;
             });
         if (rc) return rc;
@@ -146,7 +178,10 @@ i64 dropout_blocks(const Dropout& a) { return (a.M * ((a.K + 7) / 8) + 256 * DRO
 template <class T>
 int dropout(const Dropout& a, hipStream_t st)
 {
-    LAUNCH((tr_dropout_kernel<T, DROPOUT_EACH>), dim3((unsigned)dropout_blocks(a)), dim3(256), a);
+    // Matrices that the last-level cache does not hold beside their result go past it where no word crosses a line: 8192 x 12288 in bf16 77 us, 73 past it.
+    const dim3 blocks((unsigned)dropout_blocks(a));
+    if (a.M * a.K * (i64)sizeof(T) > LAST_CACHE / 2 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0) LAUNCH((tr_dropout_kernel<T, DROPOUT_EACH, true>), blocks, dim3(256), a);
+    else LAUNCH((tr_dropout_kernel<T, DROPOUT_EACH, false>), blocks, dim3(256), a);
     return EBSP_OK;
 }
 
@@ -158,10 +193,6 @@ int token_splits(i64 N, i64 V, int size)
     const i64 s = 512 / (N > 0 ? N : 1), most = words / 512;
     return (int)(s < most ? s : most);
 }
-
-// Logits of more bytes than this are gone from the last-level cache (256 MB) in part when their sums are through; a gradient then begins with the rows that were read last.
-// Row by row in order / from the last, us: preference_step_16 (370 MB read) 251 / 244, logp_train_1024 (123 MB) 71 / 73.5.
-constexpr i64 LAST_CACHE = 200ll << 20;
 
 // Parts for a gradient from statistics, which need no scratch: about four workgroups a CU, of no less than 512 words.
 int token_gradient_splits(i64 N, i64 V, int size)
@@ -252,6 +283,8 @@ template <class T>
 int token_gradient(Tokens d, hipStream_t st)
 {
     d.splits = token_gradient_splits(d.N, d.V, sizeof(T));
+    // Logits that the last-level cache does not hold are gone from it in part when their sums are through: the gradient then begins with the rows that were read last.  In
+    // order / from the last, us: preference_step_16 (370 MB read) 251 / 244, logp_train_1024 (123 MB) 71 / 73.5.
     d.backwards = d.N * d.V * (i64)sizeof(T) > LAST_CACHE;
     const dim3 parts((unsigned)(d.N * d.splits));
     if (whole_words(d, sizeof(T))) LAUNCH((tr_token_gradient_kernel<256, T, true>), parts, dim3(256), d);
@@ -295,7 +328,8 @@ extern "C" {
 size_t ebsp_residual_norm_workspace_bytes(int64_t M, int64_t K)
 {
     if (M < 1 || M >= SIZE_MAX_DIM || K < 1 || K >= WIDTH_MAX) return 0;
-    return (size_t)norm_blocks(M, K) * 3 * (size_t)((K + 7) / 8 * 8) * sizeof(float);
+    const int narrow = norm_cut(M, K, true).blocks, wide = norm_cut(M, K, false).blocks;
+    return (size_t)(narrow > wide ? narrow : wide) * 3 * (size_t)((K + 7) / 8 * 8) * sizeof(float);
 }
 
 int ebsp_residual_norm_forward(const void* x, int64_t ldx, const void* branch, int64_t ldb, int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype,
@@ -358,7 +392,7 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
             return fail(EBSP_ERR_WORKSPACE, "workspace too small or not 256-byte aligned (ebsp_residual_norm_workspace_bytes)");
     }
     a.partial = (float*)workspace;
-    a.blocks = M > 0 ? norm_blocks(M, K) : 0;
+    a.blocks = M > 0 ? norm_cut(M, K, stream_dtype != EBSP_F32).blocks : 0;
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
     return with_types(stream_dtype, dtype, [&](auto s, auto t) { return norm_backward<typename decltype(s)::type, typename decltype(t)::type>(a, st); });
