@@ -493,41 +493,46 @@ struct Preference {
 template <int NT>
 __global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
 {
-    __shared__ double shared[2][NT / WAVE][3];
+    constexpr int HALF = NT / 2, WAVES = HALF / WAVE;
+    struct Found { double sum; i64 count; i64 bad; };
+    __shared__ Found found[2][WAVES];
     const i64 pair = blockIdx.x;
-    double sum[2], share[2];
-    bool bad = false;
-    for (int side = 0; side < 2; ++side) {
-        const i64* at = a.d.starts + 2 * pair + side;
-        const i64 from = at[0] < 0 ? 0 : at[0] < a.d.N ? at[0] : a.d.N, to = at[1] < from ? from : at[1] < a.d.N ? at[1] : a.d.N;
-        bad |= from != at[0] || to != at[1];
-        double f[3] = {0., 0., 0.};                                          // the sum, tokens, tokens beyond the vocabulary
-        for (i64 n = from + threadIdx.x; n < to; n += NT) {
-            bool beyond;
-            if (token_of(a.d, n, beyond) >= 0) {
-                f[0] += a.d.stats[n * 3 + 2];
-                f[1] += 1.;
-            }
-            if (beyond) f[2] += 1.;
+    const int side = threadIdx.x / HALF;                                     // half of the workgroup for each answer
+    const i64* at = a.d.starts + 2 * pair + side;
+    const i64 from = at[0] < 0 ? 0 : at[0] < a.d.N ? at[0] : a.d.N, to = at[1] < from ? from : at[1] < a.d.N ? at[1] : a.d.N;
+    double part = 0.;
+    i64 tokens = 0;
+    bool bad = from != at[0] || to != at[1];
+    for (i64 n0 = from; n0 < to; n0 += HALF) {                               // (the same turns for a wave)
+        const i64 n = n0 + threadIdx.x % HALF;
+        bool past = false, has = false;
+        if (n < to) {
+            has = token_of(a.d, n, past) >= 0;
+            if (has) part += a.d.stats[n * 3 + 2];
         }
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) f[i] += __shfl_xor(f[i], x);
-            if (threadIdx.x % WAVE == 0) shared[side][threadIdx.x / WAVE][i] = f[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            f[i] = shared[side][0][i];
-#pragma unroll
-            for (int w = 1; w < NT / WAVE; ++w) f[i] += shared[side][w][i];
-        }
-        bad |= f[2] > 0.;
-        share[side] = a.mean && f[1] > 0. ? 1. / f[1] : 1.;
-        sum[side] = f[0] * share[side];
+        tokens += __popcll(__ballot(has));
+        bad |= __ballot(past) != 0;
     }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) part += __shfl_xor(part, x);
+    if (threadIdx.x % WAVE == 0) found[side][threadIdx.x % HALF / WAVE] = Found{part, tokens, bad};
+    __syncthreads();
     if (threadIdx.x) return;
+    double sum[2], share[2];
+    bad = false;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        double all = 0.;
+        i64 n = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            all += found[s][w].sum;
+            n += found[s][w].count;
+            bad |= found[s][w].bad != 0;
+        }
+        share[s] = a.mean && n > 0 ? 1. / (double)n : 1.;
+        sum[s] = all * share[s];
+    }
     const double beta = a.beta, e = a.smoothing;
     const double h = a.ref ? (sum[0] - a.ref[2 * pair]) - (sum[1] - a.ref[2 * pair + 1]) : sum[0] - sum[1];
     double loss, slope;

@@ -171,17 +171,23 @@ int with_type(int dtype, F&& f)
     return dtype == EBSP_BF16 ? f(Type<__bf16>()) : dtype == EBSP_F16 ? f(Type<_Float16>()) : f(Type<float>());
 }
 
-constexpr int DROPOUT_EACH = 4;
+// Units of eight elements that a thread takes one after the other: one where there are few.
+int dropout_each(const Dropout& a) { return a.M * ((a.K + 7) / 8) < 256 * 4096 ? 1 : 4; }
 
-i64 dropout_blocks(const Dropout& a) { return (a.M * ((a.K + 7) / 8) + 256 * DROPOUT_EACH - 1) / (256 * DROPOUT_EACH); }
+i64 dropout_blocks(const Dropout& a)
+{
+    const i64 per = 256 * dropout_each(a);
+    return (a.M * ((a.K + 7) / 8) + per - 1) / per;
+}
 
 template <class T>
 int dropout(const Dropout& a, hipStream_t st)
 {
     // Matrices that the last-level cache does not hold beside their result go past it where no word crosses a line: 8192 x 12288 in bf16 77 us, 73 past it.
     const dim3 blocks((unsigned)dropout_blocks(a));
-    if (a.M * a.K * (i64)sizeof(T) > LAST_CACHE / 2 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0) LAUNCH((tr_dropout_kernel<T, DROPOUT_EACH, true>), blocks, dim3(256), a);
-    else LAUNCH((tr_dropout_kernel<T, DROPOUT_EACH, false>), blocks, dim3(256), a);
+    if (a.M * a.K * (i64)sizeof(T) > LAST_CACHE / 2 && aligned(a.x, 16) && a.ldx * sizeof(T) % 16 == 0) LAUNCH((tr_dropout_kernel<T, 4, true>), blocks, dim3(256), a);
+    else if (dropout_each(a) == 4) LAUNCH((tr_dropout_kernel<T, 4, false>), blocks, dim3(256), a);
+    else LAUNCH((tr_dropout_kernel<T, 1, false>), blocks, dim3(256), a);
     return EBSP_OK;
 }
 

@@ -9,6 +9,7 @@ pass too, and no eager graph of the same leaves is alive meanwhile.)
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Tuple
 
 import torch
@@ -144,6 +145,19 @@ def _output(name: str, t: Optional[torch.Tensor], dev, dtype, shape) -> torch.Te
         return torch.empty(shape, dtype=dtype, device=dev)
     _check_buffer(name, t, dev, dtype, shape)
     return t
+
+
+def _output_like(name: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype) -> torch.Tensor:
+    """An output of the shape of a checked operand (a third faster to allocate where it is of its type and layout, too)."""
+    if t is None and like.dtype is dtype and like.is_contiguous():
+        return torch.empty_like(like)
+    return _output(name, t, like.device, dtype, like.shape)
+
+
+@functools.lru_cache(maxsize=256)
+def _bytes(name: str, *sizes: int) -> int:
+    """What a size function of the library says: a function of sizes alone."""
+    return int(getattr(load(), name)(*sizes))
 
 
 def _activation(act: str) -> int:
@@ -411,14 +425,14 @@ def ebsp_residual_norm_forward(x: torch.Tensor, branch: Optional[torch.Tensor], 
     dev = x.device
     ldx = _rows("x", x, dev, x.dtype, (M, K))
     dt, operands, random = _norm_operands(branch, M, K, x.dtype, weight, post_weight, gate, scale, p, rng, dev)
-    n = _output("n", n, dev, dt, (M, K))
+    n = _output_like("n", n, x, dt)
     stats = _output("stats", stats, dev, torch.float32, (M, 2))
     if branch is None:
         y, py, ldy = x, None, K
     elif y is x:
         py, ldy = x.data_ptr(), ldx
     else:
-        y = _output("y", y, dev, x.dtype, (M, K))
+        y = _output_like("y", y, x, x.dtype)
         py, ldy = y.data_ptr(), K
     _call("ebsp_residual_norm_forward", dev, x.data_ptr(), ldx, *operands, float(eps), *random, py, ldy, n.data_ptr(), K, stats.data_ptr())
     return y, n, stats
@@ -452,12 +466,12 @@ def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.T
     elif dx is not None and dx is dy:
         lddx = lddy
     else:
-        dx = _output("dx", dx, dev, stream, (M, K))
+        dx = _output_like("dx", dx, y, stream)
     outs = [dx, None, None, None, None]
-    for i, (t, shape) in enumerate(((branch, (M, K)), (weight, (K,)), (post_weight, (K,)), (gate, None if gate is None else tuple(gate.shape))), 1):
+    for i, t in enumerate((branch, weight, post_weight, gate), 1):
         if t is not None and want[i]:
-            outs[i] = torch.empty(shape, dtype=dt, device=dev)
-    need = ebsp_residual_norm_workspace_bytes(M, K) if outs[2] is not None or outs[3] is not None or outs[4] is not None else 0
+            outs[i] = _output_like("", None, t, dt)
+    need = _bytes("ebsp_residual_norm_workspace_bytes", M, K) if outs[2] is not None or outs[3] is not None or outs[4] is not None else 0
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _check_workspace(workspace, dev, need)
@@ -479,7 +493,7 @@ def ebsp_dropout(x: torch.Tensor, p: float, rng, out: Optional[torch.Tensor] = N
     random = _random(p, rng, dev)
     ldout = ldx if out is x else K
     if out is not x:
-        out = _output("out", out, dev, x.dtype, (M, K))
+        out = _output_like("out", out, x, x.dtype)
     _call("ebsp_dropout", dev, x.data_ptr(), ldx, M, K, code, *random, out.data_ptr(), ldout)
     return out
 
@@ -521,7 +535,7 @@ def ebsp_token_logp(logits: torch.Tensor, tokens: torch.Tensor, temperature: flo
     logp = _output("logp", logp, dev, torch.float32, (N,))
     stats = _output("stats", stats, dev, torch.float32, (N, 3))
     status = _output("status", status, dev, torch.int32, (N,))
-    room = _room(workspace, (_lib or load()).ebsp_token_logp_workspace_bytes(N, V, code), dev)
+    room = _room(workspace, _bytes("ebsp_token_logp_workspace_bytes", N, V, code), dev)
     _call("ebsp_token_logp", dev, *args, float(temperature), logp.data_ptr(), stats.data_ptr(), status.data_ptr(), *room)
     return logp, stats, status
 
@@ -567,7 +581,7 @@ def ebsp_policy_forward(logits: torch.Tensor, tokens: torch.Tensor, old_logp: to
     loss, logp = _output("loss", loss, dev, torch.float32, (N,)), _output("logp", logp, dev, torch.float32, (N,))
     stats = _output("stats", stats, dev, torch.float32, (N, 3))
     status = _output("status", status, dev, torch.int32, (N,))
-    room = _room(workspace, (_lib or load()).ebsp_token_logp_workspace_bytes(N, V, code), dev)
+    room = _room(workspace, _bytes("ebsp_token_logp_workspace_bytes", N, V, code), dev)
     _call("ebsp_policy_forward", dev, *args, *policy, loss.data_ptr(), logp.data_ptr(), stats.data_ptr(), status.data_ptr(), *room)
     return loss, logp, stats, status
 
@@ -599,7 +613,7 @@ def ebsp_policy_loss_grad(logits: torch.Tensor, tokens: torch.Tensor, old_logp: 
     loss, logp = _output("loss", loss, dev, torch.float32, (N,)), _output("logp", logp, dev, torch.float32, (N,))
     status = _output("status", status, dev, torch.int32, (N,))
     dlogits, ldd = _gradient_place(logits, dlogits, dev)
-    room = _room(workspace, (_lib or load()).ebsp_policy_workspace_bytes(N, V, code), dev)
+    room = _room(workspace, _bytes("ebsp_policy_workspace_bytes", N, V, code), dev)
     _call("ebsp_policy_loss_grad", dev, *args, *policy, dloss.data_ptr(), loss.data_ptr(), logp.data_ptr(), dlogits.data_ptr(), ldd, status.data_ptr(), *room)
     return loss, dlogits, logp, status
 
@@ -644,7 +658,7 @@ def ebsp_preference_forward(logits: torch.Tensor, tokens: torch.Tensor, starts: 
     loss, sums = _output("loss", loss, dev, torch.float32, (pairs,)), _output("sums", sums, dev, torch.float32, (2 * pairs,))
     saved = _output("saved", saved, dev, torch.float32, (N + pairs, 3))
     status = _output("status", status, dev, torch.int32, (pairs,))
-    room = _room(workspace, (_lib or load()).ebsp_token_logp_workspace_bytes(N, V, code), dev)
+    room = _room(workspace, _bytes("ebsp_token_logp_workspace_bytes", N, V, code), dev)
     _call("ebsp_preference_forward", dev, *args, starts.data_ptr(), pairs, *more, loss.data_ptr(), sums.data_ptr(), saved.data_ptr(), status.data_ptr(), *room)
     return loss, sums, saved, status
 
@@ -676,7 +690,7 @@ def ebsp_preference_loss_grad(logits: torch.Tensor, tokens: torch.Tensor, starts
     loss, sums = _output("loss", loss, dev, torch.float32, (pairs,)), _output("sums", sums, dev, torch.float32, (2 * pairs,))
     status = _output("status", status, dev, torch.int32, (pairs,))
     dlogits, ldd = _gradient_place(logits, dlogits, dev)
-    room = _room(workspace, (_lib or load()).ebsp_preference_workspace_bytes(N, pairs, V, code), dev)
+    room = _room(workspace, _bytes("ebsp_preference_workspace_bytes", N, pairs, V, code), dev)
     _call("ebsp_preference_loss_grad", dev, *args, starts.data_ptr(), pairs, *more, dloss.data_ptr(), loss.data_ptr(), sums.data_ptr(), dlogits.data_ptr(),
           ldd, status.data_ptr(), *room)
     return loss, dlogits, sums, status
