@@ -7,8 +7,8 @@
 // under the policy that drew t, A the advantage and ref that of a reference:
 //     x = e^(logp - old)     loss = -min(x A, clamp(x, 1 - low, 1 + high) A) + kl (e^(ref - logp) - (ref - logp) - 1)
 // Exponentials are taken to base 2, of x_j = s_j c - k with c = log2(e) / T and k = m c, m the row's largest logit: one fused product and sum.  k is rounded, but it
-// is the same in the sum, in logp and in the gradient, so what it is off by falls out.  Rows whose k is no ordinary number (of the type's lowest values, say, or +-1e30 and
-// more) take x_j = (s_j - m) c, slower and as good.  Statistics are m and log2 of the sum, apart; m starts from the lowest finite value, so logits of -inf
+// is the same in the sum, in logp and in the gradient, so what it is off by falls out.  Rows whose k is 2^20 and more, either way (of the type's lowest values, say), where
+// that would be too much, take x_j = (s_j - m) c, slower and as good.  Statistics are m and log2 of the sum, apart; m starts from the lowest finite value, so logits of -inf
 // weigh nothing.  Rows without a token are not read.
 #pragma once
 #include "ebsp_training.h"
@@ -43,13 +43,18 @@ struct Sum {
     float m, s;
 };
 
-constexpr float FAR = 1e30f;
+constexpr float FAR = 1048576.f;                             // 2^20: k is off by 2^-5 at most, and x by as much where it is largest
 
-// Whether a row whose largest logit is m takes the differences first (also where m is no number), and k of the others, nowhere infinite.
+// Whether a row whose largest logit is m takes the differences first (also where m is no number), and k of the others.
 __device__ __forceinline__ bool is_far(float m, float ct) { return !(fabsf(m) * ct < FAR); }
 __device__ __forceinline__ float reference(float m, float ct) { return fmaxf(m * ct, -FAR); }
 
-__device__ __forceinline__ float apart(float a, float b, float ct) { return is_far(a, ct) || is_far(b, ct) ? (a - b) * ct : reference(a, ct) - reference(b, ct); }
+// What a sum from a's reference is multiplied by, as a power of two, to be one from b's: k, or m c itself where that is far.
+__device__ __forceinline__ float apart(float a, float b, float ct)
+{
+    if (is_far(a, ct)) return is_far(b, ct) ? (a - b) * ct : fmaf(a, ct, -reference(b, ct));
+    return is_far(b, ct) ? fmaf(-b, ct, reference(a, ct)) : reference(a, ct) - reference(b, ct);
+}
 
 __device__ __forceinline__ Sum joined(Sum a, Sum b, float ct)
 {

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 from typing import Optional, Tuple
 
 import torch
@@ -380,10 +381,10 @@ def _random(p: float, rng, dev: torch.device):
         if p > 0:
             raise ValueError("dropout needs rng: a seed and an offset, or an int64 tensor of the two")
         return p, 0, 0, None
-    seed, offset = rng
+    seed, offset = (operator.index(v) for v in rng)                          # (a TypeError for what is no whole number)
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must be 0 to 2^64 - 1")
-    return p, int(seed), int(offset), None
+    return p, seed, offset, None
 
 
 def _gate(gate: Optional[torch.Tensor], dev, dtype, M: int, K: int):

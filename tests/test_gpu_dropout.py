@@ -116,5 +116,18 @@ def test_refusals(tr):
                 dict(out=torch.zeros((4, 8), device="cuda", dtype=torch.float16))):
         with pytest.raises(ValueError):
             tr.ebsp_dropout(**{**dict(x=x, p=0.5, rng=(1, 2)), **bad})
+    with pytest.raises(TypeError):
+        tr.ebsp_dropout(x, 0.5, (1.5, 2))
     with pytest.raises(ValueError):
         tr.dropout(torch.zeros((), device="cuda"), 0.5, (1, 2))
+
+
+@pytest.mark.parametrize("dtype,M,K", [(torch.bfloat16, 8200, 8192), (torch.float32, 4100, 8200), (torch.bfloat16, 8200, 8195), (torch.float32, 40000, 300)])
+def test_large_matrices_in_part(tr, dtype, M, K):
+    """Those that go past the caches, and those of as many that do not; some rows looked at."""
+    x = torch.randn((M, K), device="cuda", dtype=dtype)
+    got = tr.ebsp_dropout(x, 0.25, RNG)
+    for first in (0, M // 2, M - 3):
+        keep = torch.from_numpy(philox.keep(3, K, 0.25, *RNG, first_row=first)).cuda()
+        assert torch.equal(got[first:first + 3] != 0, keep & (x[first:first + 3] != 0))
+        assert torch.equal(got[first:first + 3], torch.where(keep, (x[first:first + 3].float() * philox.kept_factor(0.25)).to(dtype), 0.0))

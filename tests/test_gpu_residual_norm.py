@@ -153,8 +153,8 @@ def test_all_parts_at_every_width(tr, M, K, stream, dtype):
 @pytest.mark.parametrize("gate", ["none", "channel", "token"])
 @pytest.mark.parametrize("branch,post,p", [(False, False, 0.0), (True, False, 0.0), (True, True, 0.0), (True, False, 0.5), (True, True, 0.3), (True, True, 1.0)])
 def test_combinations(tr, branch, post, gate, p, stream, dtype):
-    if not branch and gate != "none":
-        pytest.skip("a gate needs a branch")
+    if not branch:
+        gate = "none"                                                        # (it needs a branch)
     for M, K, pad in ((19, 300, 3), (3, 20000, 1)):
         a, dy, dn = make(M, K, stream, dtype, branch, post, gate, p, seed=1, pad=pad)
         y, n, stats = check_forward(tr, a)
@@ -168,6 +168,15 @@ def test_many_rows(tr, M, K):
     first = check_backward(tr, a, dy, dn, y, stats)
     again = tr.ebsp_residual_norm_backward(dy, dn, y, stats, a["branch"], a["weight"], a["post_weight"], a["gate"], a["scale"], a["p"], a["rng"])
     assert all(torch.equal(s, t) for s, t in zip(first, again))
+
+
+@pytest.mark.parametrize("stream,dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float16), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("M,K", [(131073, 50), (65541, 120), (32769, 255), (16385, 500), (8193, 1000), (4099, 2041), (2051, 4090), (600, 8190)])
+def test_rows_enough_for_whole_cus(tr, M, K, stream, dtype):
+    """A backward pass in its larger workgroups, for every number of threads a row."""
+    a, dy, dn = make(M, K, stream, dtype, post=True, gate="channel", seed=10)
+    y, n, stats = check_forward(tr, a)
+    check_backward(tr, a, dy, dn, y, stats)
 
 
 def test_either_gradient_may_be_missing(tr):

@@ -242,6 +242,33 @@ def test_masked_places(tr, N, V, dtype):
     assert bool(torch.isfinite(logp[4:]).all())
 
 
+@pytest.mark.parametrize("N,V", [(3, 900), (3, 50000), (200, 900), (97, 50000)])
+@pytest.mark.parametrize("T", [1e-30, 1e-6, 0.003, 1.0, 300.0, 1e30])
+def test_large_logits_and_far_temperatures(tr, N, V, T):
+    """Rows whose exponents are of any size: some of their sums are taken from differences, some of their threads' sums are and others are not."""
+    logits, tokens, gen = make(N, V, torch.float32, seed=12, spread=1.0)
+    logits[0] += 30000.0
+    logits[1] = -logits[1].abs() * 1e25                                      # most places weigh nothing
+    logits[2, ::7] *= 1e4 * min(T, 1.0)                                      # around the border between the two ways, for T of 0.003 and 1
+    ref = Reference(logits, tokens, T)
+    logp, stats, _ = tr.ebsp_token_logp(logits, tokens, T)
+    ok = ref.logp.abs() < 1e38                                               # a smaller one is -inf in 32 bits
+    # c = log2(e) / T is off by 2^-24 of itself, and so is every exponent; the sum's weights move by as much
+    more = U * ((ref.p * (logits.double() / T - (logits.double() / T).amax(dim=1, keepdim=True)).abs().nan_to_num(0, 0, 0)).sum(dim=1) + ref.logp.abs()) * 2
+    close(logp[ok], ref.logp[ok], (ref.elogp + more)[ok] + 1e-37, "logp")
+    assert not bool(torch.isnan(logp).any())
+    slope = torch.full((N,), min(T, 1.0), device="cuda")                     # (a gradient is a slope over T)
+    grad = tr.ebsp_token_logp_backward(logits, tokens, stats, slope, T)
+    want, tol = ref.gradient(slope.double(), slope.double() * 4 * U)
+    z = ((logits.double() / T) - (logits.double() / T).amax(dim=1, keepdim=True)).abs()
+    tol = tol + (slope.double() / T)[:, None].abs() * ref.p * (z * 2 + more[:, None] / U) * U
+    assert bool(torch.isfinite(grad).all())
+    close(grad, want, tol, "gradient")
+    old, advantage = torch.where(ok, ref.logp, 0.0).float(), torch.ones(N, device="cuda")
+    loss, both, again, _ = tr.ebsp_policy_loss_grad(logits, tokens, old, advantage, slope, T, 0.9, 9.0)
+    assert torch.equal(again, logp) or bool(((again - logp).abs()[ok] <= 2 * (ref.elogp + more)[ok]).all())
+
+
 def preference(sums, other, beta, kind, smoothing):
     m = sums if other is None else sums - other
     h = m[0::2] - m[1::2]
