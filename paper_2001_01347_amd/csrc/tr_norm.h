@@ -439,7 +439,7 @@ __device__ __forceinline__ void means(const Norm& a, const float (&sum)[3], floa
 enum Keep { REREAD, HOLD, AHEAD };
 
 // Backward: each workgroup takes rows R apart over the whole grid, G threads a row, and keeps its columns' sums in registers until the end.  Memory bounds it, and the sums' way: 8192 x 4096 in bf16
-// with both norms, a gate for each channel and dropout 89 us, 4.5 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 92, 4.4; 262144 x 64 50, 4.0; 2048 x 16384, where the row is read again, 193, 2.1).
+// with both norms, a gate for each channel and dropout 89 us, 4.5 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 92, 4.4; 262144 x 64 50, 4.0; 2048 x 16384 172, 2.3, with all three sums in registers, most of them spilled, 193).
 // Weights and rows stay as they lie in memory: as floats, which the compiler would keep over the exchange, they took 232 registers a thread, and one workgroup stood where four do.
 template <class S, class T, int G, int U, int NT, Keep KEEP>
 __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
@@ -452,7 +452,20 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
     Generator g = {};
     if (a.random.threshold) g = generator(a.random);
     Raw8<T> w[UNITS], wp[UNITS];
-    float dw[U][8] = {}, dwp[U][8] = {}, dg[U][8] = {};
+    // Two units a thread have no registers for all three sums: two of them stand in shared memory, each thread's own.
+    constexpr bool SHARE = U > 1;
+    __shared__ float more[SHARE ? 2 * U * 8 : 1][SHARE ? NT : 1];
+    float dw[U][8] = {}, dwp[SHARE ? 1 : U][8] = {}, dg[SHARE ? 1 : U][8] = {};
+    if constexpr (SHARE)
+        for (int i = 0; i < 2 * U * 8; ++i) more[i][threadIdx.x] = 0.f;
+    auto fetch = [&](float (&v)[8], int which, int u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = more[SHARE ? (which * U + u) * 8 + i : 0][SHARE ? threadIdx.x : 0];
+    };
+    auto leave = [&](const float (&v)[8], int which, int u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) more[SHARE ? (which * U + u) * 8 + i : 0][SHARE ? threadIdx.x : 0] = v[i];
+    };
     auto load_weights = [&](Raw8<T>& w, Raw8<T>& wp, int unit) {
         w = load8((const T*)a.weight, unit * 8, a.K);
         wp = a.post_weight ? load8((const T*)a.post_weight, unit * 8, a.K) : zero8<T>();
@@ -488,6 +501,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            if constexpr (SHARE) __builtin_amdgcn_sched_barrier(0);          // a unit after the other: no registers for both
             if constexpr (KEEP == REREAD) {
                 load_weights(w[0], wp[0], unit);
                 row.e[0].load(a, held, unit, true);
@@ -504,6 +518,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            if constexpr (SHARE) __builtin_amdgcn_sched_barrier(0);          // a unit after the other: no registers for both
             if constexpr (KEEP == REREAD) {
                 load_weights(w[0], wp[0], unit);
                 row.e[0].load(a, held, unit, true);
@@ -512,7 +527,17 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
                 forget_words(w[u]);
                 forget_words(wp[u]);
             }
-            if (in && unit * 8 < a.K) row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, c1, c2, dw[u], dwp[u], dg[u]);
+            if (!in || unit * 8 >= a.K) continue;
+            const int of = SHARE ? 0 : u;
+            if constexpr (SHARE) {
+                fetch(dwp[0], 0, u);
+                fetch(dg[0], 1, u);
+            }
+            row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, c1, c2, dw[u], dwp[of], dg[of]);
+            if constexpr (SHARE) {
+                leave(dwp[0], 0, u);
+                leave(dg[0], 1, u);
+            }
         }
     }
     const int padded = (a.K + 7) / 8 * 8;
@@ -551,8 +576,16 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
         }
     };
     join(dw, a.sum_w);
-    join(dwp, a.sum_post);
-    join(dg, a.sum_gate);
+    if constexpr (SHARE) {
+        for (int which = 0; which < 2; ++which) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) fetch(dw[u], which, u);
+            join(dw, which == 0 ? a.sum_post : a.sum_gate);
+        }
+    } else {
+        join(dwp, a.sum_post);
+        join(dg, a.sum_gate);
+    }
 }
 
 template <class S, class T, int NT>

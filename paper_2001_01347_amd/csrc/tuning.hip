@@ -100,7 +100,8 @@ int group_threads(int units)
 
 // How a backward pass is launched.  Every workgroup leaves a row of columns' sums behind, so one a CU takes all rows where there are enough of them.  16-bit operands: 1024 threads with
 // the next row under way (8192 x 4096 94 us; 512 threads two a CU 97).  With a stream in fp32 there are no registers for that: 512 threads, two a CU (fp32 4096 x 4096 92 us, bf16
-// beside it 70; 1024 threads 98 and, with the next row under way in what then spills, 103).  Few rows: as many workgroups as there are CUs before anything else.
+// beside it 70; 1024 threads 98 and, with the next row under way in what then spills, 103).  Rows above 8192 have two units a thread: held in 16 bits (3000 x 10000 171 us; read
+// again 225; 2048 x 16384 172 and 167), read again where the stream is fp32 (1024 x 16384 170; held 260).  Few rows: as many workgroups as there are CUs before anything else.
 struct NormCut {
     int threads, blocks;
 };
@@ -143,7 +144,7 @@ int norm_backward(const Norm& a, hipStream_t st)
                 constexpr int G = decltype(group)::value, U = decltype(each)::value, SMALL = G < 256 ? 256 : G;
                 constexpr bool NARROW = sizeof(S) == 2;
                 constexpr int BIG = G == 1024 || NARROW ? 1024 : 512;
-                constexpr Keep KEEP = U == 2 ? REREAD : NARROW ? AHEAD : HOLD;
+                constexpr Keep KEEP = NARROW ? U == 2 ? HOLD : AHEAD : U == 2 ? REREAD : HOLD;
                 if (norm_cut(a.M, a.K, NARROW).threads == BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, BIG, KEEP>), dim3(a.blocks), dim3(BIG), a);
                 else if constexpr (SMALL < BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, SMALL, KEEP>), dim3(a.blocks), dim3(SMALL), a);
                 return (int)EBSP_OK;
