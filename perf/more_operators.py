@@ -377,7 +377,8 @@ def _run_preference(state):
     case, s, tokens, starts, ref = (state[k] for k in ("case", "logits", "tokens", "starts", "ref"))
     if own:
         from paper_2001_01347_amd import training
-        args = dict(ref=ref, beta=case["beta"], kind=case["kind"], smoothing=case["smoothing"], mean=case["mean"])
+        smoothing = case["smoothing"] if case["kind"] == "sigmoid" else 0.0      # the other losses have none
+        args = dict(ref=ref, beta=case["beta"], kind=case["kind"], smoothing=smoothing, mean=case["mean"])
         if case["mode"] == "step":
             loss, grad, sums, _ = training.ebsp_preference_loss_grad(s, tokens, starts, state["dloss"], **args)
             return loss, sums, grad
