@@ -5,9 +5,10 @@
 //   tr_cut.h       how the feed-forward block is cut up (host only)
 //   tr_product.h   tiles of matrix products on the matrix cores
 //   tr_gated_ff.h  the gated feed-forward block and its backward pass
+//   tr_rows.h      rows of logits
 //   tr_distill.h   the distillation loss and its gradient
 //   tr_merge.h     the merge of the workers' pushes
-// This file: the host side (checks, launches, the C entry points).
+// This file: the host side (checks, launches, the C entry points); tuning.hip has the rest of that header, tr_host.h what both share.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdio.h>
