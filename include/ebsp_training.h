@@ -207,7 +207,9 @@ int ebsp_merge_pushes(const void* pushes, int64_t stride, int32_t P, int64_t n, 
  *   n           out [M][K] of type dtype, rows ldn apart
  *   stats       out [M][2] float: the two inverse roots, for the backward pass; or NULL
  * Sums are held in 32 bits; n comes from y before y is rounded.  M == 0 or K == 0
- * is a valid no-op, M is below 2^31, K below 2^30.
+ * is a valid no-op, M is below 2^31, K below 2^30; more rows than a launch has
+ * threads for (some four million of K above 4096, 500 million of K up to 64) are
+ * refused (EBSP_ERR_SHAPE).
  */
 int ebsp_residual_norm_forward(const void* x, int64_t ldx, const void* branch, int64_t ldb, int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype,
                                const void* weight, const void* post_weight, const void* gate, int64_t ldgate, float scale, float eps, float p,
@@ -248,7 +250,8 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
  *   rng    in  [2] int64 on the device: seed and offset; or NULL: the two arguments
  *              (a replayed graph draws anew where the program moves the offset on)
  *   out    out [M][K] of type dtype, rows ldout apart; may be x itself (same rows)
- * M == 0 or K == 0 is a valid no-op, M is below 2^31, K below 2^30.
+ * M == 0 or K == 0 is a valid no-op, M is below 2^31, K below 2^30; more elements than
+ * some 137 * 10^9 are refused (EBSP_ERR_SHAPE).
  */
 int ebsp_dropout(const void* x, int64_t ldx, int64_t M, int64_t K, int32_t dtype, float p, uint64_t seed, uint64_t offset, const int64_t* rng,
                  void* out, int64_t ldout, void* stream);

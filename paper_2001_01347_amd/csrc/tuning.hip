@@ -274,13 +274,16 @@ int token_values(const Tokens& d, hipStream_t st)
 // Rows that begin at multiples of 16 bytes: no word of theirs crosses a line.
 bool whole_words(const Tokens& d, int size) { return aligned(d.logits, 16) && d.ld * size % 16 == 0; }
 
+// Workgroups of a step by the row's words.  bf16, us with 128 / 256 / 512 threads, 16 words held (512 also: 8): 4096 x 8000 32 / 33 / 46 (38), 4096 x 16000 - / 56 / 64 (57), 4096 x 32000 - / 109 / 104
+// (103), 4096 x 64000 - / 213 / 190 (202), and with 22 + 9 words a thread 188.
 template <class T, bool STREAM>
 int token_steps(const Tokens& d, hipStream_t st)
 {
     const i64 words = (d.V + PER_WORD4<T> - 1) / PER_WORD4<T>;
     const dim3 rows((unsigned)d.N);
     if (words <= 1024) LAUNCH((tr_token_step_kernel<128, T, 16, 0, STREAM>), rows, dim3(128), d);
-    else if (words <= 4096) LAUNCH((tr_token_step_kernel<256, T, 16, 0, STREAM>), rows, dim3(256), d);
+    else if (words <= 2560) LAUNCH((tr_token_step_kernel<256, T, 16, 0, STREAM>), rows, dim3(256), d);
+    else if (words <= 4096) LAUNCH((tr_token_step_kernel<512, T, 8, 0, STREAM>), rows, dim3(512), d);
     else if (words <= 16384) LAUNCH((tr_token_step_kernel<512, T, 22, 9, STREAM>), rows, dim3(512), d);
     else LAUNCH((tr_token_step_kernel<1024, T, 16, 8, STREAM>), rows, dim3(1024), d);
     return EBSP_OK;

@@ -141,6 +141,15 @@ def _matrix(name: str, t: torch.Tensor) -> Tuple[int, int]:
     return tuple(t.shape)
 
 
+def _operand(name: str, t: torch.Tensor) -> Tuple[int, int, int, int]:
+    """Check a matrix operand that says what the others are: its type's number, its shape and the distance between its rows."""
+    code = _dtype(name, t)
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor with two dimensions")
+    M, K = t.shape
+    return code, M, K, K if t.is_contiguous() else _rows(name, t, t.device, t.dtype, (M, K))
+
+
 def _output(name: str, t: Optional[torch.Tensor], dev, dtype, shape) -> torch.Tensor:
     if t is None:
         return torch.empty(shape, dtype=dtype, device=dev)
@@ -421,10 +430,8 @@ def ebsp_residual_norm_forward(x: torch.Tensor, branch: Optional[torch.Tensor], 
     ``x`` is of the others' type or float32.  ``gate`` is [K] or [M, K]; ``rng`` a seed and an offset, or an int64 tensor of the two.  Returns
     ``(y[M, K], n[M, K], stats[M, 2])``; without a branch y is x.  ``y`` may be ``x``.  Does not synchronise.
     """
-    _dtype("x", x)
-    M, K = _matrix("x", x)
+    _, M, K, ldx = _operand("x", x)
     dev = x.device
-    ldx = _rows("x", x, dev, x.dtype, (M, K))
     dt, operands, random = _norm_operands(branch, M, K, x.dtype, weight, post_weight, gate, scale, p, rng, dev)
     n = _output_like("n", n, x, dt)
     stats = _output("stats", stats, dev, torch.float32, (M, 2))
@@ -453,10 +460,8 @@ def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.T
     Returns ``(dx[M, K], dbranch[M, K], dweight[K], dpost_weight[K], dgate)``, None in the place of what there is not or ``want`` leaves out.
     ``dx`` may be ``dy``.  Does not synchronise.
     """
-    _dtype("y", y)
-    M, K = _matrix("y", y)
+    _, M, K, ldy = _operand("y", y)
     dev, stream = y.device, y.dtype
-    ldy = _rows("y", y, dev, stream, (M, K))
     dt, operands, random = _norm_operands(branch, M, K, stream, weight, post_weight, gate, scale, p, rng, dev)
     lddy = K if dy is None else _rows("dy", dy, dev, stream, (M, K))
     lddn = K if dn is None else _rows("dn", dn, dev, dt, (M, K))
@@ -487,10 +492,8 @@ def ebsp_dropout(x: torch.Tensor, p: float, rng, out: Optional[torch.Tensor] = N
 
     ``rng`` is a seed and an offset, or an int64 tensor of the two.  ``out`` may be ``x``.  Does not synchronise.
     """
-    code = _dtype("x", x)
-    M, K = _matrix("x", x)
+    code, M, K, ldx = _operand("x", x)
     dev = x.device
-    ldx = _rows("x", x, dev, x.dtype, (M, K))
     random = _random(p, rng, dev)
     ldout = ldx if out is x else K
     if out is not x:
@@ -500,12 +503,10 @@ def ebsp_dropout(x: torch.Tensor, p: float, rng, out: Optional[torch.Tensor] = N
 
 
 def _token_operands(logits, tokens, temperature):
-    code = _dtype("logits", logits)
-    N, V = _matrix("logits", logits)
+    code, N, V, ld = _operand("logits", logits)
     dev = logits.device
     if V < 1:
         raise ValueError("the vocabulary must not be empty")
-    ld = _rows("logits", logits, dev, logits.dtype, (N, V))
     _check_buffer("tokens", tokens, dev, torch.int64, (N,))
     if not 0 < float(temperature) < float("inf"):
         raise ValueError("temperature must be a positive number")
