@@ -482,7 +482,10 @@ __global__ void __launch_bounds__(NT) tr_token_gradient_kernel(Tokens d)
         }
         if (has_rest) write_gradient(out, at.whole, at.end, gradient_word<T, FROM_M>(g, rest));
     });
-    if (mine) out[token] = token_gradient<T>(g, token_logit);                // behind this thread's own store of that word
+    if (mine) {
+        __builtin_amdgcn_s_waitcnt(0);                                       // behind this thread's own store of that word
+        out[token] = token_gradient<T>(g, token_logit);
+    }
 }
 
 // The losses of pairs: one workgroup a pair, whose rows' logp stand in the statistics.  Sums over an answer and what follows are in 64 bits.

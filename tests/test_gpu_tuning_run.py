@@ -165,3 +165,32 @@ def test_two_graphs_and_two_streams(tr):
         assert all(torch.equal(a, b) for i in range(2) for a, b in zip(outs[i], want[i]))
         tr.ebsp_policy_loss_grad(*cases[0])
         torch.cuda.synchronize()
+
+
+def test_preference_loss_in_a_graph_with_new_inputs(tr):
+    """A captured call, replayed on other logits, tokens, starts and weights in the same places."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    n, v = 40, 5000
+    logits, tokens = torch.zeros((n, v), device="cuda", dtype=torch.bfloat16), torch.zeros(n, dtype=torch.int64, device="cuda")
+    starts, weight = torch.zeros(5, dtype=torch.int64, device="cuda"), torch.zeros(2, device="cuda")
+
+    def call():
+        loss, sums, saved, status = tr.ebsp_preference_forward(logits, tokens, starts, beta=0.2)
+        both = tr.ebsp_preference_loss_grad(logits, tokens, starts, weight, beta=0.2)
+        return [loss, sums, status, tr.ebsp_preference_backward(logits, tokens, starts, saved, weight), *both]
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for at in ([0, 10, 20, 30, 40], [5, 5, 17, 30, 31], [0, 40, 40, 40, 40], [0, 10, 5, 30, 41]):
+        logits.copy_(torch.randn((n, v), generator=gen, device="cuda"))
+        tokens.copy_(torch.randint(-5, v, (n,), generator=gen, device="cuda"))
+        starts.copy_(torch.tensor(at, device="cuda"))
+        weight.copy_(torch.randn(2, generator=gen, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, call()):
+            assert torch.equal(a, b), at
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[4]) and torch.equal(out[3], out[5])   # one call and two
