@@ -260,13 +260,15 @@ int check_token_workspace(size_t need, const void* workspace, size_t bytes)
     return EBSP_OK;
 }
 
+// Workgroups of the losses alone, by the row's words.  us with 64 / 128 / 256 / 512 threads: 4096 x 1000 in bf16 5.9 / 8.5 / 14 / 28, 4096 x 4000 10.7 / 9.9 / 15 / 29, 300 x 8000 6.0 / 5.3 / 4.8 / 6.7,
+// 300 x 32000 17 / 11 / 8.5 / 10, 1 x 32000 11.6 / 7.3 / 5.7 / 5.8, 128 x 10007 in fp32 7.0 / 5.7 / 5.2 / 5.8.
 template <class T>
 int token_values(const Tokens& d, hipStream_t st)
 {
     const i64 words = (d.V + PER_WORD4<T> - 1) / PER_WORD4<T>;
     const dim3 rows((unsigned)d.N);
-    if (words <= 1024) LAUNCH((tr_token_value_kernel<128, T>), rows, dim3(128), d);
-    else if (words > 2048 && d.N <= 384) LAUNCH((tr_token_value_kernel<512, T>), rows, dim3(512), d);
+    if (words <= 256) LAUNCH((tr_token_value_kernel<64, T>), rows, dim3(64), d);
+    else if (words <= 1024) LAUNCH((tr_token_value_kernel<128, T>), rows, dim3(128), d);
     else LAUNCH((tr_token_value_kernel<256, T>), rows, dim3(256), d);
     return EBSP_OK;
 }
@@ -274,14 +276,18 @@ int token_values(const Tokens& d, hipStream_t st)
 // Rows that begin at multiples of 16 bytes: no word of theirs crosses a line.
 bool whole_words(const Tokens& d, int size) { return aligned(d.logits, 16) && d.ld * size % 16 == 0; }
 
-// Workgroups of a step by the row's words.  bf16, us with 128 / 256 / 512 threads, 16 words held (512 also: 8): 4096 x 8000 32 / 33 / 46 (38), 4096 x 16000 - / 56 / 64 (57), 4096 x 32000 - / 109 / 104
-// (103), 4096 x 64000 - / 213 / 190 (202), and with 22 + 9 words a thread 188.
+// Workgroups of a step by the row's words.  Many rows, bf16, us with 64 threads and 8 words each / 64 and 16 / 128 and 16 / 256 and 16 / 512 and 16 (and 8): 4096 x 1000 6.9 / 7.6 / 10.8 / - / -, 4096 x 4000
+// 12.3 / 12.4 / 16 / - / -, 4096 x 8000 28 / 22 / 27 / 33 / 46 (38), 4096 x 16000 - / - / - / 56 / 64 (57), 4096 x 32000 - / - / - / 109 / 104 (103), 4096 x 64000 - / - / - / 213 / 190 (202), and with 22 + 9
+// words a thread 188.  Few rows of up to 2048 words want more waves: with 256 threads and 8 words, against 64 and 16: 300 x 8000 5.8 / 7.9, 300 x 16000 7.7 / 14.6, 1 x 8000 4.4 / 6.8.
 template <class T, bool STREAM>
 int token_steps(const Tokens& d, hipStream_t st)
 {
     const i64 words = (d.V + PER_WORD4<T> - 1) / PER_WORD4<T>;
     const dim3 rows((unsigned)d.N);
-    if (words <= 1024) LAUNCH((tr_token_step_kernel<128, T, 16, 0, STREAM>), rows, dim3(128), d);
+    const bool many = d.N > 1024;
+    if (words <= (many ? 512 : 256)) LAUNCH((tr_token_step_kernel<64, T, 8, 0, STREAM>), rows, dim3(64), d);
+    else if (many && words <= 1024) LAUNCH((tr_token_step_kernel<64, T, 16, 0, STREAM>), rows, dim3(64), d);
+    else if (!many && words <= 2048) LAUNCH((tr_token_step_kernel<256, T, 8, 0, STREAM>), rows, dim3(256), d);
     else if (words <= 2560) LAUNCH((tr_token_step_kernel<256, T, 16, 0, STREAM>), rows, dim3(256), d);
     else if (words <= 4096) LAUNCH((tr_token_step_kernel<512, T, 8, 0, STREAM>), rows, dim3(512), d);
     else if (words <= 16384) LAUNCH((tr_token_step_kernel<512, T, 22, 9, STREAM>), rows, dim3(512), d);

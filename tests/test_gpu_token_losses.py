@@ -16,7 +16,8 @@ TYPES = [torch.bfloat16, torch.float16, torch.float32]
 LOG2E = 1.4426950408889634
 STEP = 2.0 ** -22
 U = 2.0 ** -24
-SIZES = [(1, 1), (1, 7), (2, 9), (5, 100), (300, 257), (3, 1001), (128, 4099), (1, 32000), (3, 40000), (97, 40001), (130, 70003), (7, 131072), (100, 131080), (2, 260007)]
+SIZES = [(1, 1), (1, 7), (2, 9), (5, 100), (300, 257), (3, 1001), (128, 4099), (1, 32000), (3, 40000), (97, 40001), (130, 70003), (7, 131072), (100, 131080), (2, 260007),
+         (1030, 33), (1029, 500), (1030, 2000), (1026, 4095), (1025, 8190), (1027, 18000), (400, 8190), (200, 16001)]
 
 
 @pytest.fixture(scope="module")

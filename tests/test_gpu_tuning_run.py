@@ -194,3 +194,29 @@ def test_preference_loss_in_a_graph_with_new_inputs(tr):
             assert torch.equal(a, b), at
         torch.cuda.synchronize()
         assert torch.equal(out[0], out[4]) and torch.equal(out[3], out[5])   # one call and two
+
+
+def test_without_gradients_and_forward_mode(tr):
+    """No graph where gradients are off, by either way; tangents are refused by the losses too; one tensor in two places; a stream that is changed under a graph."""
+    import torch.autograd.forward_ad as forward_ad
+    x, w = torch.randn((4, 64), device="cuda", requires_grad=True), torch.ones(64, device="cuda", requires_grad=True)
+    tokens, f, starts = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda"), torch.tensor([0, 2, 4], device="cuda")
+    calls = [lambda v: tr.token_logp(v, tokens), lambda v: tr.policy_loss(v, tokens, f, f), lambda v: tr.preference_loss(v, tokens, starts)]
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            outs = [*tr.residual_norm(x, x, w), tr.residual_norm(x, None, w)[1], tr.dropout(x, 0.5, (1, 2)), *(c(x) for c in calls)]
+            assert not any(t.requires_grad for t in outs)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x.detach(), torch.ones_like(x))
+        for c in calls:
+            with pytest.raises(NotImplementedError):
+                c(dual)
+    one, two = x.detach().clone().requires_grad_(), x.detach().clone().requires_grad_()
+    for a, b in ((x, x), (one, two)):
+        y, n = tr.residual_norm(a, b, w)
+        (y.sum() + n.square().sum()).backward()
+    assert torch.allclose(x.grad, one.grad + two.grad, rtol=1e-6, atol=1e-6)
+    y, n = tr.residual_norm(x, x, w)
+    y.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        n.sum().backward()
