@@ -201,10 +201,11 @@ int token_splits(i64 N, i64 V, int size)
     return (int)(s < most ? s : most);
 }
 
-// Parts for a gradient from statistics, which need no scratch: about four workgroups a CU, of no less than 512 words.
+// Parts for a gradient from statistics, which need no scratch: about eight workgroups a CU, of no less than 512 words.  us with four / eight: 300 x 32000 in bf16 11.1 / 9.8, 1000 x 16000 15.6 / 13.6,
+// 509 x 50021 in fp32 47 / 44; of no less than 256 words 9.7, 13.6 and 44, but 300 x 8000 5.3 where it takes 4.4.
 int token_gradient_splits(i64 N, i64 V, int size)
 {
-    const i64 most = (V * size + 15) / 16 / 512, s = 1024 / (N > 0 ? N : 1) < most ? 1024 / (N > 0 ? N : 1) : most;
+    const i64 most = (V * size + 15) / 16 / 512, each = 2048 / (N > 0 ? N : 1), s = each < most ? each : most;
     return (int)(s < 1 ? 1 : s);
 }
 
@@ -303,8 +304,16 @@ int token_gradient(Tokens d, hipStream_t st)
     // order / from the last, us: preference_step_16 (370 MB read) 251 / 244, logp_train_1024 (123 MB) 71 / 73.5.
     d.backwards = d.N * d.V * (i64)sizeof(T) > LAST_CACHE;
     const dim3 parts((unsigned)(d.N * d.splits));
-    if (whole_words(d, sizeof(T))) LAUNCH((tr_token_gradient_kernel<256, T, true>), parts, dim3(256), d);
-    else LAUNCH((tr_token_gradient_kernel<256, T, false>), parts, dim3(256), d);
+    const i64 words = (d.V + PER_WORD4<T> - 1) / PER_WORD4<T>;
+    const bool stream = whole_words(d, sizeof(T));
+    // A wave a row where the rows are short.  us with 64 / 128 / 256 threads: 4096 x 1000 in bf16 6.8 / 7.4 / 9.8, 4096 x 2000 8.6 / 8.8 / 10.6, 4096 x 4000 15.4 / 14.6 / 14.2, 300 x 8000 6.5 / 5.3 / 4.3.
+    if (words <= 256) {
+        if (stream) LAUNCH((tr_token_gradient_kernel<64, T, true>), parts, dim3(64), d);
+        else LAUNCH((tr_token_gradient_kernel<64, T, false>), parts, dim3(64), d);
+    } else {
+        if (stream) LAUNCH((tr_token_gradient_kernel<256, T, true>), parts, dim3(256), d);
+        else LAUNCH((tr_token_gradient_kernel<256, T, false>), parts, dim3(256), d);
+    }
     return EBSP_OK;
 }
 
