@@ -45,7 +45,16 @@ struct Raw8 {
     }
 };
 
-// Elements moved down by `by`; zeros come from above, for 8 and more all of them.
+template <class T>
+__device__ __forceinline__ Raw8<T> zero8()
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = Word4{0, 0, 0, 0};
+    return r;
+}
+
+// Elements moved down by `by`, 1 to 7; zeros come from above.
 __device__ __forceinline__ void move_down(Raw8<float>& r, int by)
 {
 #pragma unroll
@@ -57,14 +66,12 @@ __device__ __forceinline__ void move_down(Raw8<float>& r, int by)
             r.w[1][i] = by & x ? i + x < 4 ? hi[(i + x) & 3] : 0 : hi[i];
         }
     }
-    if (by >= 8) r.w[0] = r.w[1] = Word4{0, 0, 0, 0};
 }
 template <class T>
 __device__ __forceinline__ void move_down(Raw8<T>& r, int by)
 {
     static_assert(sizeof(T) == 2);
-    const unsigned __int128 v = __builtin_bit_cast(unsigned __int128, r.w[0]);
-    r.w[0] = by >= 8 ? Word4{0, 0, 0, 0} : __builtin_bit_cast(Word4, v >> 16 * by);
+    r.w[0] = __builtin_bit_cast(Word4, __builtin_bit_cast(unsigned __int128, r.w[0]) >> 16 * by);
 }
 
 // Element k of a row: 32 bits beside the row's address, which is the same for a wave that has one row.
@@ -96,7 +103,8 @@ __device__ __forceinline__ Raw8<T> load8(const T* row, int k, int K)
     const T* p = element(row, min(k, K - 8));
 #pragma unroll
     for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = load_last<LAST>(p + j * PER_WORD4<T>);
-    if (k > K - 8) move_down(r, k - (K - 8));
+    if (k >= K) r = zero8<T>();
+    else if (k > K - 8) move_down(r, k - (K - 8));
     return r;
 }
 
@@ -105,15 +113,6 @@ __device__ __forceinline__ void forget_words(Raw8<T>& r)
 {
 #pragma unroll
     for (int j = 0; j < (int)sizeof(T) / 2; ++j) asm volatile("" : "+v"(r.w[j]));
-}
-
-template <class T>
-__device__ __forceinline__ Raw8<T> zero8()
-{
-    Raw8<T> r;
-#pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = Word4{0, 0, 0, 0};
-    return r;
 }
 
 template <bool STREAM = false, class T>

@@ -66,8 +66,8 @@ int check_norm_operands(const Norm& a, int stream, int dtype)
     return EBSP_OK;
 }
 
-// Threads a row and units a thread, by the row's units.  A forward pass has registers to spare: two units a thread, and half the waves to exchange sums between.
-template <bool FORWARD, class F>
+// Threads a row and units a thread, by the row's units; TWO: with two units a thread.
+template <bool TWO, class F>
 int with_group(int units, F&& f)
 {
 #define GROUP(threads, each) f(std::integral_constant<int, threads>(), std::integral_constant<int, each>())
@@ -75,7 +75,7 @@ int with_group(int units, F&& f)
     if (units <= 16) return GROUP(16, 1);
     if (units <= 32) return GROUP(32, 1);
     if (units <= 64) return GROUP(64, 1);
-    if constexpr (FORWARD) {
+    if constexpr (TWO) {
         if (units <= 128) return GROUP(64, 2);
         if (units <= 256) return GROUP(128, 2);
         if (units <= 512) return GROUP(256, 2);
@@ -101,7 +101,9 @@ int group_threads(int units)
 // How a backward pass is launched.  Every workgroup leaves a row of columns' sums behind, so one a CU takes all rows where there are enough of them.  16-bit operands: 1024 threads with
 // the next row under way (8192 x 4096 94 us; 512 threads two a CU 97).  With a stream in fp32 there are no registers for that: 512 threads, two a CU (fp32 4096 x 4096 92 us, bf16
 // beside it 70; 1024 threads 98 and, with the next row under way in what then spills, 103).  Rows above 8192 have two units a thread: held in 16 bits (3000 x 10000 171 us; read
-// again 225; 2048 x 16384 172 and 167), read again where the stream is fp32 (1024 x 16384 170; held 260).  Few rows: as many workgroups as there are CUs before anything else.
+// again 225; 2048 x 16384 172 and 167), read again where the stream is fp32 (1024 x 16384 170; held 260).
+// Few rows: as many workgroups as there are CUs before anything else, but long rows, whose columns' sums are long too, two to a workgroup from 128 of them on (512 x 4096 19.8 us, so 16.5; 300 x
+// 12000 50 and 42; four to a workgroup 18.5 and 50).
 struct NormCut {
     int threads, blocks;
 };
@@ -112,7 +114,8 @@ NormCut norm_cut(i64 M, i64 K, bool narrow)
     NormCut c = {M >= 1024 / g * 1024 ? big : g < 256 ? 256 : g, 0};
     const int rows = c.threads / g > 0 ? c.threads / g : 1, most = c.threads == 1024 ? 256 : 512;
     const i64 blocks = (M + rows - 1) / rows;
-    c.blocks = (int)(blocks < most ? blocks : most);
+    const i64 half = (blocks + 1) / 2, some = g < 512 ? blocks : half > 128 ? half : blocks < 128 ? blocks : 128;
+    c.blocks = (int)(some < most ? some : most);
     return c;
 }
 
@@ -124,11 +127,14 @@ int norm_forward(const Norm& a, hipStream_t st)
         LAUNCH((tr_norm_forward_wide_kernel<S, T, 1024>), dim3((unsigned)a.M), dim3(1024), a);
         return EBSP_OK;
     }
-    return with_group<true>(units, [&](auto group, auto each) {
+    auto launch = [&](auto group, auto each) {
         constexpr int G = decltype(group)::value, U = decltype(each)::value, NT = G < 256 ? 256 : G;
         LAUNCH((tr_norm_forward_kernel<S, T, G, U, NT>), dim3((unsigned)((a.M + NT / G - 1) / (NT / G))), dim3(NT), a);
         return (int)EBSP_OK;
-    });
+    };
+    // Two units a thread mean half the waves to exchange sums between, one a shorter way through a row.  bf16, us with two / one: 8192 x 4096 50 / 52, 2048 x 4096 15.2 / 15.5, 512 x 4096 6.4 / 6.3,
+    // 128 x 4096 5.1 / 4.4, 1 x 4096 4.5 / 3.8; 1021 x 1003 in fp32 beside fp16 7.1 / 5.9.
+    return a.M > 1024 ? with_group<true>(units, launch) : with_group<false>(units, launch);
 }
 
 template <class S, class T>
