@@ -207,11 +207,11 @@ int token_splits(i64 N, i64 V, int size)
     return (int)(s < most ? s : most);
 }
 
-// Parts for a gradient from statistics, which need no scratch: about eight workgroups a CU, of no less than 512 words.  us with four / eight: 300 x 32000 in bf16 11.1 / 9.8, 1000 x 16000 15.6 / 13.6,
-// 509 x 50021 in fp32 47 / 44; of no less than 256 words 9.7, 13.6 and 44, but 300 x 8000 5.3 where it takes 4.4.
+// Parts for a gradient from statistics, which need no scratch, of no less than 512 words: about eight workgroups a CU, four where rows are long.  us with four / eight: 300 x 32000 in bf16 11.1 / 9.8,
+// 1000 x 16000 15.6 / 13.6, but logp_train_1024 (64000) 71.8 / 74.5; of no less than 256 words 9.7 and 13.6, but 300 x 8000 5.3 where it takes 4.4.
 int token_gradient_splits(i64 N, i64 V, int size)
 {
-    const i64 most = (V * size + 15) / 16 / 512, each = 2048 / (N > 0 ? N : 1), s = each < most ? each : most;
+    const i64 words = (V * size + 15) / 16, most = words / 512, each = (words <= 4096 ? 2048 : 1024) / (N > 0 ? N : 1), s = each < most ? each : most;
     return (int)(s < 1 ? 1 : s);
 }
 
