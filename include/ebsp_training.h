@@ -236,6 +236,17 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
                                 int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
                                 int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
                                 void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * The same from the forward pass' x, not overwritten since, in the place of y, for a stream
+ * of 16 bits that a branch was joined to: the stream is formed again in 32 bits. Such a y
+ * was rounded behind its norm, and dweight shows it at the size of its own rounding. (A
+ * y of EBSP_F32, and one that is x, are as the norm took them: refused here.)
+ */
+int ebsp_residual_norm_backward_from_x(const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* x, int64_t ldx, const void* branch, int64_t ldb,
+                                       int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
+                                       int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
+                                       int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
+                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Dropout: out = x / (1 - p) where an element is kept, otherwise 0 (whatever x is

@@ -23,7 +23,7 @@ struct Norm {
     int K;
     float scale, eps;
     Random random;
-    void *y, *n;                                 // (in the backward pass y is an input)
+    void *y, *n;                                 // (in the backward pass y is an input, or x in its place)
     i64 ldy, ldn;
     float* stats;                                // [M][2]: r, r'
     const void *dy, *dn;
@@ -194,8 +194,8 @@ struct Factor {
     float scale;
     bool gated;
     __device__ __forceinline__ bool kept(int i) const { return keep >> i & 1; }
-    __device__ __forceinline__ float plain(int i) const { return kept(i) ? scale : 0.f; }
-    __device__ __forceinline__ float operator[](int i) const { return !kept(i) ? 0.f : gated ? scale * gate[i] : scale; }
+    __device__ __forceinline__ float whole(int i) const { return gated ? scale * gate[i] : scale; }
+    __device__ __forceinline__ float operator[](int i) const { return kept(i) ? whole(i) : 0.f; }
 };
 
 template <class T>
@@ -342,8 +342,8 @@ __global__ void __launch_bounds__(NT) tr_norm_forward_wide_kernel(Norm a)
     }
 }
 
-// Eight elements of a row in the backward pass: as they lie in memory ...
-template <class S, class T>
+// Eight elements of a row in the backward pass: as they lie in memory ...  JOIN: with x in the place of y.
+template <class S, class T, bool JOIN>
 struct Back8 {
     Raw8<S> y, dy;
     Raw8<T> dn, b, gate;
@@ -376,24 +376,46 @@ struct Back8 {
         forget_words(gate);
     }
 
-    // mean(dn w u), mean(q h (dy + r dn w)) and mean(q h u), not yet divided.
-    __device__ __forceinline__ void sums(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, float r, float rb, float (&sum)[3]) const
+    // u of the eight.  With JOIN from x and what the branch adds, in 32 bits and not rounded: from a y of 16 bits every term of dw is off by half a step of y, and dw by as much again as
+    // its own rounding (8192 x 4096 in bf16 2.28e-3 of dw, from x 1.67e-3).
+    __device__ __forceinline__ void normed(const Norm& a, const Raw8<T>& wp, u32 keep, float r, float rb, float (&u)[8]) const
     {
         const Factor<T> f = factor(a, keep);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float u = y[i] * r, dnw = dn[i] * w[i];
-            sum[0] = fmaf(dnw, u, sum[0]);
-            if (a.post_weight) {
-                const float qh = f[i] * wp[i] * b[i] * rb;
+            const float d = a.post_weight ? b[i] * rb * wp[i] : b[i];
+            u[i] = (JOIN && f.kept(i) ? fmaf(f[i], d, y[i]) : y[i]) * r;
+        }
+    }
+
+    // mean(dn w u), mean(q h (dy + r dn w)) and mean(q h u), not yet divided, and u for the results.  With JOIN q h is what the stream is formed of, so it is computed in any case, and no
+    // branch stands in the way (8192 x 4096 in bf16 89 us for the call with one, 86 without).
+    __device__ __forceinline__ void sums(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, float r, float rb, float (&u)[8], float (&sum)[3]) const
+    {
+        const Factor<T> f = factor(a, keep);
+        if constexpr (!JOIN) normed(a, wp, keep, r, rb, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float dnw = dn[i] * w[i];
+            if constexpr (JOIN) {
+                const float by = a.post_weight ? wp[i] * rb : 1.f, qh = f.kept(i) ? f.whole(i) * b[i] * by : 0.f;
+                u[i] = (y[i] + qh) * r;
+                sum[0] = fmaf(dnw, u[i], sum[0]);
                 sum[1] = fmaf(qh, fmaf(r, dnw, dy[i]), sum[1]);
-                sum[2] = fmaf(qh, u, sum[2]);
+                sum[2] = fmaf(qh, u[i], sum[2]);
+            } else {
+                sum[0] = fmaf(dnw, u[i], sum[0]);
+                if (a.post_weight) {
+                    const float qh = f[i] * wp[i] * b[i] * rb;
+                    sum[1] = fmaf(qh, fmaf(r, dnw, dy[i]), sum[1]);
+                    sum[2] = fmaf(qh, u[i], sum[2]);
+                }
             }
         }
     }
 
     // The row's results, and what it adds to the columns' sums.
-    __device__ __forceinline__ void results(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, i64 row, int unit, float r, float rb,
+    __device__ __forceinline__ void results(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, i64 row, int unit, float r, float rb, const float (&u)[8],
                                             float c1, float c2, float (&dw)[8], float (&dwp)[8], float (&dg)[8]) const
     {
         const Factor<T> f = factor(a, keep);
@@ -401,9 +423,8 @@ struct Back8 {
         float dx[8], db[8], gate[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float u = y[i] * r;
-            dx[i] = fmaf(r, fmaf(-u, c1, dn[i] * w[i]), dy[i]);
-            dw[i] = fmaf(dn[i], u, dw[i]);
+            dx[i] = fmaf(r, fmaf(-u[i], c1, dn[i] * w[i]), dy[i]);
+            dw[i] = fmaf(dn[i], u[i], dw[i]);
         }
         if (a.dx) store8<true>((S*)a.dx + row * a.lddx, k, a.K, dx);
         if (!a.branch) return;
@@ -440,7 +461,7 @@ enum Keep { REREAD, HOLD, AHEAD };
 // Backward: each workgroup takes rows R apart over the whole grid, G threads a row, and keeps its columns' sums in registers until the end.  Memory bounds it, and the sums' way: 8192 x 4096 in bf16
 // with both norms, a gate for each channel and dropout 89 us, 4.5 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 92, 4.4; 262144 x 64 50, 4.0; 2048 x 16384 172, 2.3, with all three sums in registers, most of them spilled, 193).
 // Weights and rows stay as they lie in memory: as floats, which the compiler would keep over the exchange, they took 232 registers a thread, and one workgroup stood where four do.
-template <class S, class T, int G, int U, int NT, Keep KEEP>
+template <class S, class T, bool JOIN, int G, int U, int NT, Keep KEEP>
 __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 {
     constexpr int R = NT / G, COLUMNS = G * U * 8, UNITS = KEEP == REREAD ? 1 : U;
@@ -473,7 +494,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 #pragma unroll
         for (int u = 0; u < U; ++u) load_weights(w[u], wp[u], lane + u * G);
     struct Row {
-        Back8<S, T> e[UNITS];
+        Back8<S, T, JOIN> e[UNITS];
         float r, rb;
     };
     // Groups behind the last row go along with it, for the barriers, and leave nothing.
@@ -491,12 +512,15 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
     for (i64 base = (i64)blockIdx.x * R; base < a.M; base += step) {         // (the same turns for the whole workgroup: barriers)
         if constexpr (KEEP == AHEAD) {
             row = next;
-            if (base + step < a.M) load(next, base + step, false);
+            if (!JOIN && base + step < a.M) load(next, base + step, false);
         } else load(row, base, base < step);
         const i64 n = base + group, held = min(n, a.M - 1);
         const bool in = n < a.M;
         float sum[3] = {0.f, 0.f, 0.f};
         u32 keep[U];
+        // With JOIN u stands from the sums to the results, in the place of x and of forming it again; two units have no registers for that.
+        constexpr bool STANDS = JOIN && KEEP != REREAD && U == 1;
+        float u8[8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
@@ -509,8 +533,10 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
                 forget_words(wp[u]);
             }
             keep[u] = a.random.threshold ? keep_bits(g, a.random.threshold, (u32)unit, (u32)n) : 0xffu;
-            row.e[at].sums(a, w[at], wp[at], keep[u], row.r, row.rb, sum);
+            row.e[at].sums(a, w[at], wp[at], keep[u], row.r, row.rb, u8, sum);
         }
+        if constexpr (KEEP == AHEAD && JOIN)                                 // (before the sums there are no registers for it: 98 us where this takes 86)
+            if (base + step < a.M) load(next, base + step, false);
         group_sum<G, NT>(sum, shared, turn);
         float c1, c2;
         means(a, sum, row.r, c1, c2);
@@ -532,7 +558,8 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
                 fetch(dwp[0], 0, u);
                 fetch(dg[0], 1, u);
             }
-            row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, c1, c2, dw[u], dwp[of], dg[of]);
+            if constexpr (!STANDS) row.e[at].normed(a, wp[at], keep[u], row.r, row.rb, u8);
+            row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, u8, c1, c2, dw[u], dwp[of], dg[of]);
             if constexpr (SHARE) {
                 leave(dwp[0], 0, u);
                 leave(dg[0], 1, u);
@@ -587,7 +614,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
     }
 }
 
-template <class S, class T, int NT>
+template <class S, class T, bool JOIN, int NT>
 __global__ void __launch_bounds__(NT) tr_norm_backward_wide_kernel(Norm a)
 {
     __shared__ float shared[2 * NT / WAVE * 3];
@@ -601,18 +628,22 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_wide_kernel(Norm a)
         float sum[3] = {0.f, 0.f, 0.f}, c1, c2;
         auto each = [&](auto&& f) {
             for (int unit = threadIdx.x; unit * 8 < a.K; unit += NT) {
-                Back8<S, T> e;
+                Back8<S, T, JOIN> e;
                 e.load(a, row, unit, true);
                 const Raw8<T> w = load8((const T*)a.weight, unit * 8, a.K);
                 const Raw8<T> wp = a.post_weight ? load8((const T*)a.post_weight, unit * 8, a.K) : zero8<T>();
                 f(unit, a.random.threshold ? keep_bits(g, a.random.threshold, (u32)unit, (u32)row) : 0xffu, e, w, wp);
             }
         };
-        each([&](int, u32 keep, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) { e.sums(a, w, wp, keep, r, rb, sum); });
+        each([&](int, u32 keep, const Back8<S, T, JOIN>& e, const Raw8<T>& w, const Raw8<T>& wp) {
+            float u[8];
+            e.sums(a, w, wp, keep, r, rb, u, sum);
+        });
         group_sum<NT, NT>(sum, shared, turn);
         means(a, sum, r, c1, c2);
-        each([&](int unit, u32 keep, const Back8<S, T>& e, const Raw8<T>& w, const Raw8<T>& wp) {
-            float v[3][8] = {};
+        each([&](int unit, u32 keep, const Back8<S, T, JOIN>& e, const Raw8<T>& w, const Raw8<T>& wp) {
+            float u[8], v[3][8] = {};
+            e.normed(a, wp, keep, r, rb, u);
             const int place[3] = {a.sum_w, a.sum_post, a.sum_gate};
 #pragma unroll
             for (int s = 0; s < 3; ++s)                                      // (this thread's alone, from its row before)
@@ -621,7 +652,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_wide_kernel(Norm a)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[s][i] = before[i];
                 }
-            e.results(a, w, wp, keep, row, unit, r, rb, c1, c2, v[0], v[1], v[2]);
+            e.results(a, w, wp, keep, row, unit, r, rb, u, c1, c2, v[0], v[1], v[2]);
 #pragma unroll
             for (int s = 0; s < 3; ++s)
                 if (place[s] >= 0) store8(mine + (i64)place[s] * padded, unit * 8, padded, v[s]);

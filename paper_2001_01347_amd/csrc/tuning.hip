@@ -137,22 +137,22 @@ int norm_forward(const Norm& a, hipStream_t st)
     return a.M > 1024 ? with_group<true>(units, launch) : with_group<false>(units, launch);
 }
 
-template <class S, class T>
+template <class S, class T, bool JOIN>
 int norm_backward(const Norm& a, hipStream_t st)
 {
     const int units = (a.K + 7) / 8;
     if (a.M > 0) {
         int rc = EBSP_OK;
         if (units > HELD_UNITS)
-            LAUNCH((tr_norm_backward_wide_kernel<S, T, 1024>), dim3(a.blocks), dim3(1024), a);
+            LAUNCH((tr_norm_backward_wide_kernel<S, T, JOIN, 1024>), dim3(a.blocks), dim3(1024), a);
         else
             rc = with_group<false>(units, [&](auto group, auto each) {
                 constexpr int G = decltype(group)::value, U = decltype(each)::value, SMALL = G < 256 ? 256 : G;
                 constexpr bool NARROW = sizeof(S) == 2;
                 constexpr int BIG = G == 1024 || NARROW ? 1024 : 512;
                 constexpr Keep KEEP = NARROW ? U == 2 ? HOLD : AHEAD : U == 2 ? REREAD : HOLD;
-                if (norm_cut(a.M, a.K, NARROW).threads == BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, BIG, KEEP>), dim3(a.blocks), dim3(BIG), a);
-                else if constexpr (SMALL < BIG) LAUNCH((tr_norm_backward_kernel<S, T, G, U, SMALL, KEEP>), dim3(a.blocks), dim3(SMALL), a);
+                if (norm_cut(a.M, a.K, NARROW).threads == BIG) LAUNCH((tr_norm_backward_kernel<S, T, JOIN, G, U, BIG, KEEP>), dim3(a.blocks), dim3(BIG), a);
+                else if constexpr (SMALL < BIG) LAUNCH((tr_norm_backward_kernel<S, T, JOIN, G, U, SMALL, KEEP>), dim3(a.blocks), dim3(SMALL), a);
                 return (int)EBSP_OK;
             });
         if (rc) return rc;
@@ -386,11 +386,15 @@ int ebsp_residual_norm_forward(const void* x, int64_t ldx, const void* branch, i
     return with_types(stream_dtype, dtype, [&](auto s, auto t) { return norm_forward<typename decltype(s)::type, typename decltype(t)::type>(a, st); });
 }
 
-int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* y, int64_t ldy, const void* branch, int64_t ldb,
-                                int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
-                                int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
-                                int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
-                                void* workspace, size_t workspace_bytes, void* stream)
+}  // extern "C"
+
+namespace {
+
+int norm_backward_call(bool join, const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* y, int64_t ldy, const void* branch, int64_t ldb,
+                       int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
+                       int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
+                       int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
+                       void* workspace, size_t workspace_bytes, void* stream)
 {
     Norm a = {};
     a.branch = branch, a.ldb = ldb, a.M = M, a.K = (int)K, a.weight = weight, a.post_weight = post_weight, a.gate = gate, a.ldgate = ldgate;
@@ -398,6 +402,8 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
     a.dy = dy, a.lddy = lddy, a.dn = dn, a.lddn = lddn, a.dx = dx, a.lddx = lddx, a.dbranch = dbranch, a.lddb = lddb;
     if (int rc = check_random(p, seed, offset, rng, a.random)) return rc;
     if (int rc = check_norm(a, K, stream_dtype, dtype)) return rc;
+    if (M > 0 && join && (!branch || stream_dtype == EBSP_F32))
+        return fail(EBSP_ERR_ARGUMENT, "y is formed again where a branch was joined to a stream of 16 bits: ebsp_residual_norm_backward takes the others");
     if (M > 0 && ((dbranch && !branch) || (dpost_weight && !post_weight) || (dgate && !gate)))
         return fail(EBSP_ERR_ARGUMENT, "a gradient is wanted of an operand that is not there");
     a.sum_w = a.sum_post = a.sum_gate = -1;
@@ -407,7 +413,7 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
     else a.dgate = dgate, a.lddgate = lddgate;
     if (K == 0 || (!dx && !dbranch && !dgate && a.sums == 0)) return EBSP_OK;
     if (M > 0) {
-        if (!y || !stats) return fail(EBSP_ERR_NULL, "y and stats must not be NULL");
+        if (!y || !stats) return fail(EBSP_ERR_NULL, "y (or x) and stats must not be NULL");
         if (!stride_ok(ldy, K) || (dy && !stride_ok(lddy, K)) || (dn && !stride_ok(lddn, K)) || (dx && !stride_ok(lddx, K)) ||
             (dbranch && !stride_ok(lddb, K)) || (a.dgate && !stride_ok(lddgate, K)))
             return fail(EBSP_ERR_ARGUMENT, "a row stride is shorter than the row, or 2^40 and more");
@@ -426,7 +432,37 @@ int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, in
     a.blocks = M > 0 ? norm_cut(M, K, stream_dtype != EBSP_F32).blocks : 0;
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
-    return with_types(stream_dtype, dtype, [&](auto s, auto t) { return norm_backward<typename decltype(s)::type, typename decltype(t)::type>(a, st); });
+    return with_types(stream_dtype, dtype, [&](auto s, auto t) {
+        using S = typename decltype(s)::type;
+        using T = typename decltype(t)::type;
+        if constexpr (sizeof(S) == 2)
+            if (join) return norm_backward<S, T, true>(a, st);
+        return norm_backward<S, T, false>(a, st);
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int ebsp_residual_norm_backward(const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* y, int64_t ldy, const void* branch, int64_t ldb,
+                                int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
+                                int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
+                                int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
+                                void* workspace, size_t workspace_bytes, void* stream)
+{
+    return norm_backward_call(false, dy, lddy, dn, lddn, y, ldy, branch, ldb, M, K, stream_dtype, dtype, weight, post_weight, gate, ldgate, scale, p, seed, offset, rng,
+                              stats, dx, lddx, dbranch, lddb, dweight, dpost_weight, dgate, lddgate, workspace, workspace_bytes, stream);
+}
+
+int ebsp_residual_norm_backward_from_x(const void* dy, int64_t lddy, const void* dn, int64_t lddn, const void* x, int64_t ldx, const void* branch, int64_t ldb,
+                                       int64_t M, int64_t K, int32_t stream_dtype, int32_t dtype, const void* weight, const void* post_weight, const void* gate,
+                                       int64_t ldgate, float scale, float p, uint64_t seed, uint64_t offset, const int64_t* rng, const float* stats, void* dx,
+                                       int64_t lddx, void* dbranch, int64_t lddb, void* dweight, void* dpost_weight, void* dgate, int64_t lddgate,
+                                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    return norm_backward_call(true, dy, lddy, dn, lddn, x, ldx, branch, ldb, M, K, stream_dtype, dtype, weight, post_weight, gate, ldgate, scale, p, seed, offset, rng,
+                              stats, dx, lddx, dbranch, lddb, dweight, dpost_weight, dgate, lddgate, workspace, workspace_bytes, stream);
 }
 
 int ebsp_dropout(const void* x, int64_t ldx, int64_t M, int64_t K, int32_t dtype, float p, uint64_t seed, uint64_t offset, const int64_t* rng,

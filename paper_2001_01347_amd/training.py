@@ -26,7 +26,8 @@ ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_forward_workspace_bytes", "ebsp_gated_ff_forward_split", "ebsp_gated_ff_workspace_bytes",
            "ebsp_gated_ff_split_workspace_bytes", "ebsp_gated_ff_backward", "ebsp_distill_workspace_bytes",
            "ebsp_distill_forward", "ebsp_distill_backward", "ebsp_distill_loss_grad", "ebsp_merge_pushes",
-           "ebsp_residual_norm_workspace_bytes", "ebsp_residual_norm_forward", "ebsp_residual_norm_backward", "ebsp_dropout",
+           "ebsp_residual_norm_workspace_bytes", "ebsp_residual_norm_forward", "ebsp_residual_norm_backward",
+           "ebsp_residual_norm_backward_from_x", "ebsp_dropout",
            "ebsp_token_logp_workspace_bytes", "ebsp_token_logp", "ebsp_token_logp_backward", "ebsp_policy_workspace_bytes",
            "ebsp_policy_forward", "ebsp_policy_backward", "ebsp_policy_loss_grad", "ebsp_preference_workspace_bytes",
            "ebsp_preference_forward", "ebsp_preference_backward", "ebsp_preference_loss_grad")
@@ -74,9 +75,9 @@ def load() -> ctypes.CDLL:
         lib.ebsp_residual_norm_workspace_bytes.argtypes = [i64, i64]
         lib.ebsp_residual_norm_forward.restype = c_int
         lib.ebsp_residual_norm_forward.argtypes = [vp, i64, vp, i64, i64, i64, i32, i32, vp, vp, vp, i64, f32, f32] + random + [vp, i64, vp, i64, vp, vp]
-        lib.ebsp_residual_norm_backward.restype = c_int
-        lib.ebsp_residual_norm_backward.argtypes = [vp, i64] * 4 + [i64, i64, i32, i32, vp, vp, vp, i64, f32] + random + \
-            [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+        for backward in (lib.ebsp_residual_norm_backward, lib.ebsp_residual_norm_backward_from_x):
+            backward.restype = c_int
+            backward.argtypes = [vp, i64] * 4 + [i64, i64, i32, i32, vp, vp, vp, i64, f32] + random + [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
         lib.ebsp_dropout.restype = c_int
         lib.ebsp_dropout.argtypes = [vp, i64, i64, i64, i32] + random + [vp, i64, vp]
         rows = [vp, i64, i64, i64, i32, vp]
@@ -450,17 +451,22 @@ def ebsp_residual_norm_workspace_bytes(M: int, K: int) -> int:
     return int(load().ebsp_residual_norm_workspace_bytes(M, K))
 
 
-def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], y: torch.Tensor, stats: torch.Tensor,
+def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], y: Optional[torch.Tensor], stats: torch.Tensor,
                                 branch: Optional[torch.Tensor], weight: torch.Tensor, post_weight: Optional[torch.Tensor] = None,
                                 gate: Optional[torch.Tensor] = None, scale: float = 1.0, p: float = 0.0, rng=None,
                                 dx: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                                want: Tuple[bool, bool, bool, bool, bool] = (True,) * 5):
+                                want: Tuple[bool, bool, bool, bool, bool] = (True,) * 5, x: Optional[torch.Tensor] = None):
     """Gradients of ``ebsp_residual_norm_forward`` from its ``y`` and ``stats``; ``dy`` or ``dn`` may be None: zero; see the header.
 
-    Returns ``(dx[M, K], dbranch[M, K], dweight[K], dpost_weight[K], dgate)``, None in the place of what there is not or ``want`` leaves out.
+    Of a stream of 16 bits ``y`` was rounded behind its norm: give the forward pass' ``x``, too, and where there is a branch the stream is formed again from it in 32
+    bits, and ``y`` is not looked at.  Returns ``(dx[M, K], dbranch[M, K], dweight[K], dpost_weight[K], dgate)``, None in the place of what there is not or
+    ``want`` leaves out.
     ``dx`` may be ``dy``.  Does not synchronise.
     """
-    _, M, K, ldy = _operand("y", y)
+    name, kept = "ebsp_residual_norm_backward", "y"
+    if x is not None and branch is not None and _dtype("x", x) != DTYPES[torch.float32]:
+        name, kept, y = "ebsp_residual_norm_backward_from_x", "x", x
+    _, M, K, ldy = _operand(kept, y)
     dev, stream = y.device, y.dtype
     dt, operands, random = _norm_operands(branch, M, K, stream, weight, post_weight, gate, scale, p, rng, dev)
     lddy = K if dy is None else _rows("dy", dy, dev, stream, (M, K))
@@ -482,7 +488,7 @@ def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.T
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _check_workspace(workspace, dev, need)
     ptr = [None if t is None else t.data_ptr() for t in (dy, dn, *outs, workspace)]
-    _call("ebsp_residual_norm_backward", dev, ptr[0], lddy, ptr[1], lddn, y.data_ptr(), ldy, *operands, *random, stats.data_ptr(), ptr[2], lddx, ptr[3], K,
+    _call(name, dev, ptr[0], lddy, ptr[1], lddn, y.data_ptr(), ldy, *operands, *random, stats.data_ptr(), ptr[2], lddx, ptr[3], K,
           ptr[4], ptr[5], ptr[6], K, ptr[7], 0 if workspace is None else workspace.numel())
     return tuple(outs)
 
@@ -831,7 +837,9 @@ class _ResidualNorm(torch.autograd.Function):
     def forward(ctx, x, branch, weight, post_weight, gate, scale, p, rng, eps):
         y, n, stats = ebsp_residual_norm_forward(x, branch, weight, post_weight, gate, scale, p, rng, eps)
         if any(ctx.needs_input_grad):
-            ctx.save_for_backward(y, stats, branch, weight, post_weight, gate)
+            # the stream, y as it is or formed again from x: of 16 bits y was rounded behind its norm
+            ctx.from_x = branch is not None and x.dtype is not torch.float32
+            ctx.save_for_backward(x if ctx.from_x else y, stats, branch, weight, post_weight, gate)
             ctx.rng = _kept_place(rng)
         ctx.args = scale, p
         ctx.set_materialize_grads(False)
@@ -840,12 +848,13 @@ class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, *grads):
-        y, stats, branch, weight, post_weight, gate = ctx.saved_tensors
+        kept, stats, branch, weight, post_weight, gate = ctx.saved_tensors
+        y, x = (None, kept) if ctx.from_x else (kept, None)
         scale, p = ctx.args
         dy, dn = [None if g is None else _plain_rows(g) for g in ((None, *grads) if branch is None else grads)]
         if dy is None and dn is None:
             return (None,) * 9
-        out = ebsp_residual_norm_backward(dy, dn, y, stats, branch, weight, post_weight, gate, scale, p, ctx.rng, want=ctx.needs_input_grad[:5])
+        out = ebsp_residual_norm_backward(dy, dn, y, stats, branch, weight, post_weight, gate, scale, p, ctx.rng, want=ctx.needs_input_grad[:5], x=x)
         return (*out, None, None, None, None)
 
 
