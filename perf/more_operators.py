@@ -246,7 +246,7 @@ def _run_norm(state):
         y, n, stats = training.ebsp_residual_norm_forward(x, branch, eps=eps, **args)
         if case["mode"] == "forward":
             return (y, n) if branch is not None else (n,)
-        grads = training.ebsp_residual_norm_backward(state["dy"], state["dn"], y, stats, branch, **args)
+        grads = training.ebsp_residual_norm_backward(state["dy"], state["dn"], y, stats, branch, x=x, **args)
         return tuple(t for t in ((y if branch is not None else None), n, *grads) if t is not None)
     M, K = x.shape
     t, w = weight.dtype, weight.float()
