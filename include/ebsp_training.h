@@ -332,6 +332,7 @@ int ebsp_policy_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, 
 
 /* Kinds of preference loss, of the margin h of a pair. */
 #define EBSP_PREFERENCE_SIGMOID 0  /* -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h) */
+                                   /* (a term of weight 0 is 0, whatever the margin)                           */
 #define EBSP_PREFERENCE_HINGE   1  /* max(0, 1 - beta h)                                                    */
 #define EBSP_PREFERENCE_SQUARE  2  /* (h - 1 / (2 beta))^2                                                  */
 

@@ -552,13 +552,11 @@ __global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
         loss = gap * gap;
         slope = 2. * gap;
     } else {
-        const double z = beta * h, low = exp(-fabs(z));                      // sigmoid(z) is 1 / (1 + low), or low times that
-        loss = (z < 0. ? -z : z == z ? 0. : z) + log1p(low);
-        slope = -beta * (z < 0. ? 1. : low) / (1. + low);
-        if (e != 0.) {
-            loss += e * z;
-            slope += e * beta;
-        }
+        // With low = e^-|z|, -log sigmoid(-|z|) is |z| + log(1 + low) and -log sigmoid(|z|) the second alone: |z| comes with the weight of one side, and not where that is 0 (z may be infinite).
+        const double z = beta * h, low = exp(-fabs(z)), wrong = z < 0. ? 1. - e : e;
+        loss = (wrong != 0. ? wrong * fabs(z) : z == z ? 0. : z) + log1p(low);
+        slope = -beta * (z < 0. ? 1. : low) / (1. + low);                    // (sigmoid(z) is 1 / (1 + low), or low times that)
+        if (e != 0.) slope += e * beta;
     }
     if (a.loss) a.loss[pair] = (float)loss;
     if (a.sums) {
