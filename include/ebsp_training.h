@@ -354,8 +354,9 @@ int ebsp_policy_loss_grad(const void* logits, int64_t ld, int64_t N, int64_t V, 
  *   loss    out [pairs] float;  sums  out [2 pairs] float, or NULL
  *   saved   out [N + pairs][3] float: what ebsp_preference_backward needs; or NULL
  *   status  out [pairs] int32, or NULL: EBSP_STATUS_RANGE where a token of the pair is V
- *               or more (it counts as none) or a start is beyond N or below the one before
- *               (rows that do not exist are left out; the pair's results mean nothing)
+ *               or more (it counts as none), and for every pair where any start is before
+ *               0, beyond N or below the one before: no pair's loss and sums mean anything
+ *               then, and the gradient is 0
  *   dloss   in  [pairs] float: dL/dloss of every pair
  *   workspace   ebsp_preference_workspace_bytes, 256-byte aligned; for ebsp_preference_forward
  *               with `saved`, ebsp_token_logp_workspace_bytes are enough

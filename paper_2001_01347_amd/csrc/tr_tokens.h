@@ -133,6 +133,28 @@ __device__ __forceinline__ Sum part_sum(const T* s, const Words<NT, T> at, float
     return sum;
 }
 
+// Starts that are not those of rows one behind the other (one is before 0, beyond N or below the one before) say of no row whose it is: no pair's results stand then.  They are looked
+// over beside the rows, in as many slices as rows and pairs allow, up to 64; each slice's finding stands in the third place behind the pair of its number, where the pairs' kernel reads them all.
+__device__ __forceinline__ i64 start_slices(const Tokens& d) { return min(d.pairs, d.N > 0 && d.N < WAVE ? d.N : (i64)WAVE); }
+
+__device__ __forceinline__ float* start_finding(const Tokens& d, i64 slice) { return d.stats + (d.N + slice) * 3 + 2; }
+
+template <int NT>
+__device__ __forceinline__ void check_starts(const Tokens& d, i64 slice)
+{
+    const i64 slices = start_slices(d);
+    if (slice >= slices) return;                                             // (the same for the workgroup)
+    const i64 all = 2 * d.pairs + 1, each = (all + slices - 1) / slices, end = min((slice + 1) * each, all);
+    int wrong = 0;
+#pragma unroll 4
+    for (i64 i = slice * each + threadIdx.x; i < end; i += NT) {
+        const i64 at = d.starts[i], before = i > 0 ? d.starts[i - 1] : 0;
+        wrong |= (at < before) | (at > d.N);
+    }
+    wrong = __syncthreads_or(wrong);
+    if (threadIdx.x == 0) *start_finding(d, slice) = wrong ? 1.f : 0.f;
+}
+
 // The row's token, -1 for none: negative, beyond the vocabulary, or a row outside all answers.
 __device__ __forceinline__ int token_of(const Tokens& d, i64 n, bool& bad)
 {
@@ -299,6 +321,7 @@ __global__ void __launch_bounds__(NT) tr_token_value_kernel(Tokens d)
     const T* s = (const T*)d.logits + n * d.ld;
     const float ct = LOG2E / d.temperature;
     bool bad;
+    if (d.kind == TOKEN_PREFERENCE) check_starts<NT>(d, n);
     const int token = token_of(d, n, bad);
     if (leave_row<NT, T>(d, n, token, bad, false)) return;
     const float token_logit = to_float(s[token]);
@@ -435,6 +458,7 @@ __global__ void __launch_bounds__(64) tr_token_join_kernel(Tokens d)
 {
     const i64 n = blockIdx.x;
     bool bad;
+    if (d.kind == TOKEN_PREFERENCE) check_starts<64>(d, n);
     const int token = token_of(d, n, bad);
     if (leave_row<64, T>(d, n, token, bad, false)) return;
     const float token_logit = to_float(((const T*)d.logits)[n * d.ld + token]), ct = LOG2E / d.temperature;
@@ -488,6 +512,9 @@ __global__ void __launch_bounds__(NT) tr_token_gradient_kernel(Tokens d)
     }
 }
 
+// Pairs without any rows: their starts are looked over here.
+__global__ void __launch_bounds__(64) tr_starts_kernel(Tokens d) { check_starts<64>(d, blockIdx.x); }
+
 // The losses of pairs: one workgroup a pair, whose rows' logp stand in the statistics.  Sums over an answer and what follows are in 64 bits.
 struct Preference {
     Tokens d;
@@ -508,9 +535,11 @@ __global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
     const int side = threadIdx.x / HALF;                                     // half of the workgroup for each answer
     const i64* at = a.d.starts + 2 * pair + side;
     const i64 from = at[0] < 0 ? 0 : at[0] < a.d.N ? at[0] : a.d.N, to = at[1] < from ? from : at[1] < a.d.N ? at[1] : a.d.N;
+    const i64 slices = start_slices(a.d);
+    const float finding = (i64)(threadIdx.x % WAVE) < slices ? *start_finding(a.d, threadIdx.x % WAVE) : 0.f;
     double part = 0.;
     i64 tokens = 0;
-    bool bad = from != at[0] || to != at[1];
+    bool bad = false;
     for (i64 n0 = from; n0 < to; n0 += HALF) {                               // (the same turns for a wave)
         const i64 n = n0 + threadIdx.x % HALF;
         bool past = false, has = false;
@@ -523,6 +552,7 @@ __global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) part += __shfl_xor(part, x);
+    const bool astray = __ballot(finding != 0.f) != 0;                       // (the starts, anyone's)
     if (threadIdx.x % WAVE == 0) found[side][threadIdx.x % HALF / WAVE] = Found{part, tokens, bad};
     __syncthreads();
     if (threadIdx.x) return;
@@ -563,11 +593,11 @@ __global__ void __launch_bounds__(NT) tr_preference_kernel(Preference a)
         a.sums[2 * pair] = (float)sum[0];
         a.sums[2 * pair + 1] = (float)sum[1];
     }
-    if (a.status) a.status[pair] = bad ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
+    if (a.status) a.status[pair] = bad || astray ? EBSP_STATUS_RANGE : EBSP_STATUS_OK;
     float* out = a.d.stats + (a.d.N + pair) * 3;
-    out[0] = (float)(slope * share[0]);
-    out[1] = (float)(-slope * share[1]);
-    out[2] = 0.f;
+    out[0] = astray ? 0.f : (float)(slope * share[0]);
+    out[1] = astray ? 0.f : (float)(-slope * share[1]);
+    if (pair >= slices) out[2] = 0.f;
 }
 
 }  // namespace

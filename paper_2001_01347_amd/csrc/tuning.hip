@@ -588,8 +588,9 @@ namespace {
 int run_pairs(const Tokens& d, const float* ref, float beta, int kind, float smoothing, int mean, float* loss, float* sums, int* status, int dtype,
               hipStream_t st)
 {
-    if (d.N > 0)
+    if (d.N > 0) {
         if (int rc = run_tokens(d, dtype, false, st)) return rc;
+    } else LAUNCH(tr_starts_kernel, dim3((unsigned)(d.pairs < WAVE ? d.pairs : WAVE)), dim3(64), d);
     const Preference a = {d, ref, beta, smoothing, kind, mean, loss, sums, status};
     if (d.pairs > 0) LAUNCH((tr_preference_kernel<256>), dim3((unsigned)d.pairs), dim3(256), a);
     return EBSP_OK;

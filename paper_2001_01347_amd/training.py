@@ -32,7 +32,7 @@ EXPORTS = ("ebsp_gated_ff_forward", "ebsp_gated_ff_forward_workspace_bytes", "eb
            "ebsp_policy_forward", "ebsp_policy_backward", "ebsp_policy_loss_grad", "ebsp_preference_workspace_bytes",
            "ebsp_preference_forward", "ebsp_preference_backward", "ebsp_preference_loss_grad")
 
-STATUS_RANGE = 4          # a row's index, label or token lies beyond the vocabulary, or a pair's rows beyond the others
+STATUS_RANGE = 4          # a row's index, label or token lies beyond the vocabulary, or the starts of a preference loss are not in order
 TOP_MAX = 1024            # most teacher entries of a row
 
 _lib = None
@@ -966,8 +966,8 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, starts: torch.Te
     """The preference loss [pairs] of pairs of answers, for the rows [N, V] of all answers one behind the other, with the logits' gradient.
 
     ``starts`` [2 pairs + 1] says where each answer begins (the preferred one of a pair first) and where the last ends; ``tokens`` [N] are negative
-    where a row has none to score; ``ref`` [2 pairs] are the answers' sums under a reference, float32.  Starts or tokens out of range are
-    left out (``ebsp_preference_forward`` flags their pairs)."""
+    where a row has none to score; ``ref`` [2 pairs] are the answers' sums under a reference, float32.  Tokens out of range are
+    left out (``ebsp_preference_forward`` flags their pairs); where a start is out of range or below the one before there is no gradient (it flags all)."""
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
         raise ValueError("logits must be a tensor of shape [N, V]")
     return _Preference.apply(_plain_rows(logits), tokens, starts, ref, beta, kind, smoothing, mean)
