@@ -806,8 +806,13 @@ def _flat_rows(name: str, t: Optional[torch.Tensor], lead: torch.Size) -> Option
     return t.reshape(lead.numel()).contiguous()
 
 
+def _place(rng):
+    """A seed and an offset as they are now, where they are numbers: a program moves its offset on between the passes."""
+    return rng if rng is None or isinstance(rng, torch.Tensor) else tuple(rng)
+
+
 def _kept_place(rng):
-    """A seed and an offset on the device as they are now: a program moves its offset on between the passes."""
+    """The same for what stands on the device."""
     return rng.clone() if isinstance(rng, torch.Tensor) else rng
 
 
@@ -826,10 +831,10 @@ class _Dropout(torch.autograd.Function):
 def dropout(x: torch.Tensor, p: float, rng) -> torch.Tensor:
     """Dropout of x [..., K] with its gradient; which elements are kept is computed from ``rng`` in either pass and stored in none.
 
-    ``rng`` is a seed and an offset, or an int64 tensor of the two on x's device (the backward pass uses what it held in the forward pass).  Calls of one
+    ``rng`` is a seed and an offset, or an int64 tensor of the two on x's device (the backward pass uses what either held in the forward pass).  Calls of one
     seed and offset keep the same elements of the same rows: give every call an offset of its own.  Forward-mode tangents are
     refused (NotImplementedError)."""
-    return _Dropout.apply(_flat("x", x, "K"), p, rng).reshape(x.shape)
+    return _Dropout.apply(_flat("x", x, "K"), float(p), _place(rng)).reshape(x.shape)
 
 
 class _ResidualNorm(torch.autograd.Function):
@@ -881,7 +886,7 @@ def residual_norm(x: torch.Tensor, branch: Optional[torch.Tensor], weight: torch
             except RuntimeError:
                 raise ValueError("gate must broadcast to x") from None
     vectors = [w.contiguous() if isinstance(w, torch.Tensor) else w for w in (weight, post_weight)]
-    out = _ResidualNorm.apply(rows, branch, *vectors, gate, scale, p, rng, eps)
+    out = _ResidualNorm.apply(rows, branch, *vectors, gate, float(scale), float(p), _place(rng), eps)
     if branch is None:
         return x, out.reshape(x.shape)
     return out[0].reshape(x.shape), out[1].reshape(x.shape)
@@ -911,7 +916,7 @@ def token_logp(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 
     lead = logits.shape[:-1]
     if tokens is None:
         raise ValueError("tokens must be a tensor of the leading dimensions of logits, or of those as one")
-    return _TokenLogp.apply(rows, _flat_rows("tokens", tokens, lead), temperature).reshape(lead)
+    return _TokenLogp.apply(rows, _flat_rows("tokens", tokens, lead), float(temperature)).reshape(lead)
 
 
 class _Policy(torch.autograd.Function):
@@ -944,7 +949,7 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tens
         if t is None:
             raise ValueError(f"{name} must be a tensor of the leading dimensions of logits, or of those as one")
     flat = [_flat_rows(name, t, lead) for name, t in (*named, ("ref_logp", ref_logp))]
-    return _Policy.apply(rows, *flat, temperature, clip_low, clip_high, kl_weight).reshape(lead)
+    return _Policy.apply(rows, *flat, float(temperature), float(clip_low), float(clip_high), float(kl_weight)).reshape(lead)
 
 
 class _Preference(torch.autograd.Function):
