@@ -660,26 +660,32 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_wide_kernel(Norm a)
     }
 }
 
-// The columns' sums over the workgroups' parts, in their order: 64 columns a workgroup, the parts spread over its waves and joined.
+// The columns' sums over the workgroups' parts, in their order: 64 columns a workgroup at a time, the parts spread over its waves and joined.  Rows above 2^26 have more columns than a launch has
+// workgroups for.
+constexpr i64 COLUMN_BLOCKS = 1ll << 20;
+
 template <class T>
 __global__ void __launch_bounds__(1024) tr_norm_columns_kernel(Norm a)
 {
     __shared__ float shared[16][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, place = blockIdx.y;
     const int padded = (a.K + 7) / 8 * 8;
-    const i64 k = (i64)blockIdx.x * 64 + lane;
     const int each = (a.blocks + 15) / 16, from = wave * each, to = min(from + each, a.blocks);
-    float sum = 0.f;
-    if (k < a.K)
+    for (i64 k0 = (i64)blockIdx.x * 64; k0 < a.K; k0 += (i64)gridDim.x * 64) {
+        const i64 k = k0 + lane;
+        float sum = 0.f;
+        if (k < a.K)
 #pragma unroll 8
-        for (int b = from; b < to; ++b) sum += a.partial[((i64)b * a.sums + place) * padded + k];
-    shared[wave][lane] = sum;
-    __syncthreads();
-    if (wave || k >= a.K) return;
-    sum = shared[0][lane];
+            for (int b = from; b < to; ++b) sum += a.partial[((i64)b * a.sums + place) * padded + k];
+        __syncthreads();                                                     // the columns before are read
+        shared[wave][lane] = sum;
+        __syncthreads();
+        if (wave || k >= a.K) continue;
+        sum = shared[0][lane];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) sum += shared[w][lane];
-    ((T*)a.column_out[place])[k] = from_float<T>(sum);
+        for (int w = 1; w < 16; ++w) sum += shared[w][lane];
+        ((T*)a.column_out[place])[k] = from_float<T>(sum);
+    }
 }
 
 struct Dropout {

@@ -157,7 +157,8 @@ int norm_backward(const Norm& a, hipStream_t st)
             });
         if (rc) return rc;
     }
-    if (a.sums > 0) LAUNCH((tr_norm_columns_kernel<T>), dim3((a.K + 63) / 64, a.sums), dim3(1024), a);
+    const i64 columns = ((i64)a.K + 63) / 64;
+    if (a.sums > 0) LAUNCH((tr_norm_columns_kernel<T>), dim3((unsigned)(columns < COLUMN_BLOCKS ? columns : COLUMN_BLOCKS), a.sums), dim3(1024), a);
     return EBSP_OK;
 }
 
