@@ -229,7 +229,7 @@ __device__ __forceinline__ void stream8(const Norm& a, const Raw8<S>& x, const R
     }
 }
 
-// Forward: G threads a row, U units of eight elements each.  Memory bounds it: 8192 x 4096 in bf16 53 us, 5.1 TB/s.  y is stored past the caches, for the next block comes first; n is what that reads.
+// Forward: G threads a row, U units of eight elements each.  Memory bounds it: 8192 x 4096 in bf16 54 us, 5.0 TB/s.  y is stored past the caches, for the next block comes first; n is what that reads.
 template <class S, class T, int G, int U, int NT>
 __global__ void __launch_bounds__(NT) tr_norm_forward_kernel(Norm a)
 {
@@ -389,7 +389,7 @@ struct Back8 {
     }
 
     // mean(dn w u), mean(q h (dy + r dn w)) and mean(q h u), not yet divided, and u for the results.  With JOIN q h is what the stream is formed of, so it is computed in any case, and no
-    // branch stands in the way (8192 x 4096 in bf16 89 us for the call with one, 86 without).
+    // branch stands in the way (8192 x 4096 in bf16, one set of operands over and over: 89 us for the call with one, 86 without).
     __device__ __forceinline__ void sums(const Norm& a, const Raw8<T>& w, const Raw8<T>& wp, u32 keep, float r, float rb, float (&u)[8], float (&sum)[3]) const
     {
         const Factor<T> f = factor(a, keep);
@@ -455,23 +455,25 @@ __device__ __forceinline__ void means(const Norm& a, const float (&sum)[3], floa
     c2 = (sum[1] - c1 * r * sum[2]) / (float)a.K;
 }
 
-// How a backward pass keeps its row: not at all (what the results need is read again, from the cache), in registers, or with the next row under way besides.
+// How a backward pass keeps its row: not at all (what the results need is read again, from the cache), in registers, or with the next row under way besides.  Two units a thread are read again.
 enum Keep { REREAD, HOLD, AHEAD };
 
 // Backward: each workgroup takes rows R apart over the whole grid, G threads a row, and keeps its columns' sums in registers until the end.  Memory bounds it, and the sums' way: 8192 x 4096 in bf16
-// with both norms, a gate for each channel and dropout 89 us, 4.5 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 92, 4.4; 262144 x 64 50, 4.0; 2048 x 16384 172, 2.3, with all three sums in registers, most of them spilled, 193).
+// with both norms, a gate for each channel and dropout 87 us with the columns' kernel, 4.6 TB/s beside 25 MB of columns' sums (fp32 4096 x 4096 104, 3.9; 262144 x 64 52, 3.9; 2048 x 16384 165, 2.4, with
+// all three sums in registers, most of them spilled, a ninth more).
 // Weights and rows stay as they lie in memory: as floats, which the compiler would keep over the exchange, they took 232 registers a thread, and one workgroup stood where four do.
 template <class S, class T, bool JOIN, int G, int U, int NT, Keep KEEP>
 __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
 {
-    constexpr int R = NT / G, COLUMNS = G * U * 8, UNITS = KEEP == REREAD ? 1 : U;
+    static_assert(U == 1 || KEEP == REREAD);
+    constexpr int R = NT / G, COLUMNS = G * U * 8;
     __shared__ float shared[2 * NT / WAVE * 3];
     __shared__ float columns[R > 1 ? COLUMNS : 1];
     const int lane = threadIdx.x % G, group = group_of<G>();
     int turn = 0;
     Generator g = {};
     if (a.random.threshold) g = generator(a.random);
-    Raw8<T> w[UNITS], wp[UNITS];
+    Raw8<T> w, wp;
     // Two units a thread have no registers for all three sums: two of them stand in shared memory, each thread's own.
     constexpr bool SHARE = U > 1;
     __shared__ float more[SHARE ? 2 * U * 8 : 1][SHARE ? NT : 1];
@@ -490,11 +492,9 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
         w = load8((const T*)a.weight, unit * 8, a.K);
         wp = a.post_weight ? load8((const T*)a.post_weight, unit * 8, a.K) : zero8<T>();
     };
-    if constexpr (KEEP != REREAD)
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_weights(w[u], wp[u], lane + u * G);
+    if constexpr (KEEP != REREAD) load_weights(w, wp, lane);
     struct Row {
-        Back8<S, T, JOIN> e[UNITS];
+        Back8<S, T, JOIN> e;
         float r, rb;
     };
     // Groups behind the last row go along with it, for the barriers, and leave nothing.
@@ -502,9 +502,7 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
         const i64 row = min(base + group, a.M - 1);
         to.r = a.stats[row * 2];
         to.rb = a.stats[row * 2 + 1];
-        if constexpr (KEEP != REREAD)
-#pragma unroll
-            for (int u = 0; u < U; ++u) to.e[u].load(a, row, lane + u * G, first);
+        if constexpr (KEEP != REREAD) to.e.load(a, row, lane, first);
     };
     const i64 step = (i64)gridDim.x * R;
     Row row, next;
@@ -518,39 +516,38 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
         const bool in = n < a.M;
         float sum[3] = {0.f, 0.f, 0.f};
         u32 keep[U];
-        // With JOIN u stands from the sums to the results, in the place of x and of forming it again; two units have no registers for that.
-        constexpr bool STANDS = JOIN && KEEP != REREAD && U == 1;
+        constexpr bool STANDS = JOIN && KEEP != REREAD;                      // u, from the sums to the results, in the place of x and of forming it again
         float u8[8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            const int unit = lane + u * G;
             if constexpr (SHARE) __builtin_amdgcn_sched_barrier(0);          // a unit after the other: no registers for both
             if constexpr (KEEP == REREAD) {
-                load_weights(w[0], wp[0], unit);
-                row.e[0].load(a, held, unit, true);
+                load_weights(w, wp, unit);
+                row.e.load(a, held, unit, true);
             } else {
-                forget_words(w[u]);
-                forget_words(wp[u]);
+                forget_words(w);
+                forget_words(wp);
             }
             keep[u] = a.random.threshold ? keep_bits(g, a.random.threshold, (u32)unit, (u32)n) : 0xffu;
-            row.e[at].sums(a, w[at], wp[at], keep[u], row.r, row.rb, u8, sum);
+            row.e.sums(a, w, wp, keep[u], row.r, row.rb, u8, sum);
         }
-        if constexpr (KEEP == AHEAD && JOIN)                                 // (before the sums there are no registers for it: 98 us where this takes 86)
+        if constexpr (KEEP == AHEAD && JOIN)                                 // (before the sums there are no registers for it: 98 us where this takes 86, measured likewise)
             if (base + step < a.M) load(next, base + step, false);
         group_sum<G, NT>(sum, shared, turn);
         float c1, c2;
         means(a, sum, row.r, c1, c2);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int at = KEEP == REREAD ? 0 : u, unit = lane + u * G;
+            const int unit = lane + u * G;
             if constexpr (SHARE) __builtin_amdgcn_sched_barrier(0);          // a unit after the other: no registers for both
             if constexpr (KEEP == REREAD) {
-                load_weights(w[0], wp[0], unit);
-                row.e[0].load(a, held, unit, true);
+                load_weights(w, wp, unit);
+                row.e.load(a, held, unit, true);
             } else {
-                row.e[u].forget();
-                forget_words(w[u]);
-                forget_words(wp[u]);
+                row.e.forget();
+                forget_words(w);
+                forget_words(wp);
             }
             if (!in || unit * 8 >= a.K) continue;
             const int of = SHARE ? 0 : u;
@@ -558,8 +555,8 @@ __global__ void __launch_bounds__(NT) tr_norm_backward_kernel(Norm a)
                 fetch(dwp[0], 0, u);
                 fetch(dg[0], 1, u);
             }
-            if constexpr (!STANDS) row.e[at].normed(a, wp[at], keep[u], row.r, row.rb, u8);
-            row.e[at].results(a, w[at], wp[at], keep[u], n, unit, row.r, row.rb, u8, c1, c2, dw[u], dwp[of], dg[of]);
+            if constexpr (!STANDS) row.e.normed(a, wp, keep[u], row.r, row.rb, u8);
+            row.e.results(a, w, wp, keep[u], n, unit, row.r, row.rb, u8, c1, c2, dw[u], dwp[of], dg[of]);
             if constexpr (SHARE) {
                 leave(dwp[0], 0, u);
                 leave(dg[0], 1, u);

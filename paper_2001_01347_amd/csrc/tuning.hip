@@ -98,19 +98,22 @@ int group_threads(int units)
     return 1024;
 }
 
-// How a backward pass is launched.  Every workgroup leaves a row of columns' sums behind, so one a CU takes all rows where there are enough of them.  16-bit operands: 1024 threads with
-// the next row under way (8192 x 4096 94 us; 512 threads two a CU 97).  With a stream in fp32 there are no registers for that: 512 threads, two a CU (fp32 4096 x 4096 92 us, bf16
-// beside it 70; 1024 threads 98 and, with the next row under way in what then spills, 103).  Rows above 8192 have two units a thread: held in 16 bits (3000 x 10000 171 us; read
-// again 225; 2048 x 16384 172 and 167), read again where the stream is fp32 (1024 x 16384 170; held 260).
-// Few rows: as many workgroups as there are CUs before anything else, but long rows, whose columns' sums are long too, two to a workgroup from 128 of them on (512 x 4096 19.8 us, so 16.5; 300 x
-// 12000 50 and 42; four to a workgroup 18.5 and 50).
+// How a backward pass is launched.  Every workgroup leaves a row of columns' sums behind, so one a CU takes all rows where there are enough of them.  us of both kernels in a row, on operands that the
+// last-level cache does not hold, from y / from x where both are: a 16-bit stream of 64 threads a row and more has 1024 threads with the next row under way (8192 x 4096 86 / 87; 512 threads
+// two a CU 89 / 89), of fewer 512, two a CU (100000 x 200 62 / 62, 262144 x 64 52 / 52; with the next row under way 67 / 82 and 54 / 59: from x its registers do not hold that).  With a stream in
+// fp32 there are none for it either: 512 threads, two a CU (fp32 4096 x 4096 104, bf16 beside it 8192 x 4096 123; 1024 threads and the next row 187 and 193).  Rows above 8192 have two units a
+// thread, which are read again (2048 x 16384 171 / 165, 3000 x 10000 181 / 176, 8192 x 12288 460 / 460, fp32 1024 x 16384 173; held 174 / 178, 197 / 195, 503 / 513 and 235).
+// Few rows: as many workgroups as there are CUs before anything else, but long rows, whose columns' sums are long too, two to a workgroup from 128 of them on (operands that the cache
+// holds: 512 x 4096 19.8 us, so 16.5; 300 x 12000 50 and 42; four to a workgroup 18.5 and 50).
 struct NormCut {
     int threads, blocks;
 };
 
+constexpr bool takes_next(bool narrow, int g) { return narrow && g >= WAVE; }
+
 NormCut norm_cut(i64 M, i64 K, bool narrow)
 {
-    const int units = (int)((K + 7) / 8), g = group_threads(units), big = g == 1024 || narrow ? 1024 : 512;
+    const int units = (int)((K + 7) / 8), g = group_threads(units), big = g == 1024 || takes_next(narrow, g) ? 1024 : 512;
     NormCut c = {M >= 1024 / g * 1024 ? big : g < 256 ? 256 : g, 0};
     const int rows = c.threads / g > 0 ? c.threads / g : 1, most = c.threads == 1024 ? 256 : 512;
     const i64 blocks = (M + rows - 1) / rows;
@@ -132,8 +135,8 @@ int norm_forward(const Norm& a, hipStream_t st)
         LAUNCH((tr_norm_forward_kernel<S, T, G, U, NT>), dim3((unsigned)((a.M + NT / G - 1) / (NT / G))), dim3(NT), a);
         return (int)EBSP_OK;
     };
-    // Two units a thread mean half the waves to exchange sums between, one a shorter way through a row.  bf16, us with two / one: 8192 x 4096 50 / 52, 2048 x 4096 15.2 / 15.5, 512 x 4096 6.4 / 6.3,
-    // 128 x 4096 5.1 / 4.4, 1 x 4096 4.5 / 3.8; 1021 x 1003 in fp32 beside fp16 7.1 / 5.9.
+    // Two units a thread mean half the waves to exchange sums between, one a shorter way through a row.  us with two / one, as above: bf16 8192 x 4096 54 / 59 (beside a stream in fp32 68 / 64),
+    // 2048 x 4096 15.6 / 16.2, 512 x 4096 6.9 / 6.7, 128 x 4096 5.6 / 4.7, 1 x 4096 5.0 / 4.2; 1021 x 1003 in fp32 beside fp16 7.9 / 6.5.
     return a.M > 1024 ? with_group<true>(units, launch) : with_group<false>(units, launch);
 }
 
@@ -149,8 +152,8 @@ int norm_backward(const Norm& a, hipStream_t st)
             rc = with_group<false>(units, [&](auto group, auto each) {
                 constexpr int G = decltype(group)::value, U = decltype(each)::value, SMALL = G < 256 ? 256 : G;
                 constexpr bool NARROW = sizeof(S) == 2;
-                constexpr int BIG = G == 1024 || NARROW ? 1024 : 512;
-                constexpr Keep KEEP = NARROW ? U == 2 ? HOLD : AHEAD : U == 2 ? REREAD : HOLD;
+                constexpr int BIG = G == 1024 || takes_next(NARROW, G) ? 1024 : 512;
+                constexpr Keep KEEP = U == 2 ? REREAD : takes_next(NARROW, G) ? AHEAD : HOLD;
                 if (norm_cut(a.M, a.K, NARROW).threads == BIG) LAUNCH((tr_norm_backward_kernel<S, T, JOIN, G, U, BIG, KEEP>), dim3(a.blocks), dim3(BIG), a);
                 else if constexpr (SMALL < BIG) LAUNCH((tr_norm_backward_kernel<S, T, JOIN, G, U, SMALL, KEEP>), dim3(a.blocks), dim3(SMALL), a);
                 return (int)EBSP_OK;
@@ -199,7 +202,9 @@ int dropout(const Dropout& a, hipStream_t st)
     return EBSP_OK;
 }
 
-// Parts that a row is cut into for its sum, as for the distillation loss: several only where rows are few and long.
+// Parts that a row is cut into for its sum: several only where rows are few and long, for they cost a launch or two more.  bf16, us of the loss whole / in parts: 1 x 32000 5.7 / 7.3, 1 x 64000 7.9 / 7.4,
+// 1 x 128000 12.1 / 7.4, 48 x 64000 8.2 / 8.3, 48 x 128000 12.7 / 9.3, 96 x 64000 8.3 / 9.2, 96 x 128000 12.8 / 11.1, 128 x 128000 15.4 / 12.0, 200 x 128000 16.9 / 16.4, 256 x 128000 17.1 / 17.9; of the
+// loss with its gradient 1 x 64000 11.1 / 10.7, 1 x 128000 18.1 / 11.0, 48 x 64000 11.6 / 13.6, 48 x 128000 18.8 / 16.4, 96 x 128000 19.7 / 24.4, 128 x 128000 20.3 / 28.4: one border for both, at 96.
 int token_splits(i64 N, i64 V, int size)
 {
     const i64 words = (V * size + 15) / 16;
