@@ -458,13 +458,15 @@ def ebsp_residual_norm_backward(dy: Optional[torch.Tensor], dn: Optional[torch.T
                                 want: Tuple[bool, bool, bool, bool, bool] = (True,) * 5, x: Optional[torch.Tensor] = None):
     """Gradients of ``ebsp_residual_norm_forward`` from its ``y`` and ``stats``; ``dy`` or ``dn`` may be None: zero; see the header.
 
-    Of a stream of 16 bits ``y`` was rounded behind its norm: give the forward pass' ``x``, too, and where there is a branch the stream is formed again from it in 32
+    Of a stream of 16 bits ``y`` was rounded behind its norm: give the forward pass' ``x``, not overwritten since, too, and where there is a branch the stream is formed again from it in 32
     bits, and ``y`` is not looked at.  Returns ``(dx[M, K], dbranch[M, K], dweight[K], dpost_weight[K], dgate)``, None in the place of what there is not or
     ``want`` leaves out.
     ``dx`` may be ``dy``.  Does not synchronise.
     """
     name, kept = "ebsp_residual_norm_backward", "y"
     if x is not None and branch is not None and _dtype("x", x) != DTYPES[torch.float32]:
+        if isinstance(y, torch.Tensor) and y.data_ptr() == x.data_ptr() and y.numel():
+            raise ValueError("x was overwritten by y: give y alone")
         name, kept, y = "ebsp_residual_norm_backward_from_x", "x", x
     _, M, K, ldy = _operand(kept, y)
     dev, stream = y.device, y.dtype

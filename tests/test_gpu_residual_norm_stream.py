@@ -132,3 +132,14 @@ def test_refusals(tr):
     for bad in (dict(x=x[:3]), dict(x=x.half()), dict(x=x.cpu()), dict(x=x[0]), dict(x=3), dict(x=None), dict(branch=None)):
         with pytest.raises(ValueError):
             tr.ebsp_residual_norm_backward(**{**dict(dy=x, dn=x, y=None, stats=stats, branch=b, weight=w, x=x), **bad})
+
+
+def test_x_that_was_joined_in_place_is_refused(tr):
+    a, dy, dn = make(6, 64, torch.bfloat16, torch.bfloat16, seed=14)
+    x = a["x"].clone()
+    y, n, stats = tr.ebsp_residual_norm_forward(x, a["branch"], *arguments(a), EPS, y=x)
+    with pytest.raises(ValueError, match="overwritten"):
+        tr.ebsp_residual_norm_backward(dy, dn, y, stats, a["branch"], *arguments(a), x=x)
+    from_y = tr.ebsp_residual_norm_backward(dy, dn, y, stats, a["branch"], *arguments(a))
+    kept = tr.ebsp_residual_norm_forward(a["x"], a["branch"], *arguments(a), EPS)
+    assert all(s is None or torch.equal(s, t) for s, t in zip(from_y, tr.ebsp_residual_norm_backward(dy, dn, kept[0], kept[2], a["branch"], *arguments(a))))
